@@ -356,6 +356,56 @@ bigcn_status bigcn_pipeline_close(bigcn_pipeline* pipe);
 bigcn_status bigcn_col_stats(bigcn_ctx* ctx, const float* H, int64_t n, int32_t d, int64_t ld,
                              float eps, float* shift_out, float* scale_out);
 
+/* ---- Dense ends of a classifier that stands on binarized layers --------------------------------------------------------
+ * The paper has no counterpart of these calls: it ends at the last layer's H'.  A program that trains or serves a class
+ * matrix on top of a hidden layer norms the layer's rows, takes the loss of the class matrix and its gradients, and serves
+ * the same matrix in 8-bit integers.  Rows are row-major with any leading dimension >= their length, from any address
+ * aligned to their elements; what a type other than fp32 holds is computed in fp32 and rounded once. */
+enum bigcn_type {
+    BIGCN_F32 = 0,
+    BIGCN_BF16 = 1,
+    BIGCN_F16 = 2,
+    BIGCN_I8 = 3               /* bigcn_quantized_product() only */
+};
+
+/* Layer norm of rows: y_ij = (x_ij - mean_i) rstd_i gain_j + offset_j, mean_i over the d elements of row i, rstd_i =
+ * 1 / sqrt(var_i + eps) with the biased variance about that mean.  x, y of any bigcn_type but BIGCN_I8 each, 1 <= d <=
+ * BIGCN_MAX_D_IN, eps >= 0; gain, offset fp32 [d], nullable (1 and 0); mean, rstd fp32 [n].  A row with a NaN or an
+ * infinity gives NaN in that row alone.  Elements of y past d are left as they were. */
+bigcn_status bigcn_layer_norm(bigcn_ctx* ctx, const void* x, int32_t x_type, int64_t n, int32_t d, int64_t ldx,
+                              const float* gain, const float* offset, float eps, void* y, int32_t y_type, int64_t ldy,
+                              float* mean, float* rstd);
+
+/* Its gradients, from g_y = dL/dy and the mean and rstd of the forward pass:
+ *   g_x_ij = rstd_i (g_ij gain_j - a_i - xhat_ij b_i), a_i = sum_j g_ij gain_j / d, b_i = sum_j g_ij gain_j xhat_ij / d,
+ *   g_gain_j = sum_i g_ij xhat_ij,  g_offset_j = sum_i g_ij,  xhat_ij = (x_ij - mean_i) rstd_i.
+ * g_y, x, g_x of any bigcn_type but BIGCN_I8 each; g_gain, g_offset fp32 [d], nullable.  The sums over the nodes are taken
+ * in fixed parts and order: the same call gives the same bits.  With n = 0, g_gain and g_offset are set to zero.  Needs
+ * bigcn_layer_norm_workspace_bytes(d) of workspace where one of them is wanted. */
+size_t bigcn_layer_norm_workspace_bytes(int32_t d);
+bigcn_status bigcn_layer_norm_backward(bigcn_ctx* ctx, const void* g_y, int32_t g_type, int64_t ldg, const void* x, int32_t x_type,
+                                       int64_t ldx, int64_t n, int32_t d, const float* gain, const float* mean,
+                                       const float* rstd, void* g_x, int32_t g_x_type, int64_t ldgx, float* g_gain,
+                                       float* g_offset);
+
+/* Rows in 8-bit integers, each with a scale of its own: scale_i = max_j |x_ij| / 127 and q_ij the integer nearest to
+ * 127 x_ij / max_j |x_ij| (exactly; halfway goes to the even one), so that x_ij is about q_ij scale_i.  A row of zeros gets
+ * zeros and the scale 0; a row with a NaN or an infinity zeros and the scale NaN.  x of any bigcn_type but BIGCN_I8, 1 <= d
+ * <= BIGCN_MAX_D_IN; q int8 [n x ldq], ldq >= d a multiple of 16 and q on a 16-byte boundary (elements past d are left as
+ * they were); scale fp32 [n].  For the rows of a class matrix, once, and for activations. */
+bigcn_status bigcn_quantize_rows(bigcn_ctx* ctx, const void* x, int32_t type, int64_t n, int32_t d, int64_t ldx, int8_t* q,
+                                 int64_t ldq, float* scale);
+
+/* Product of rows with class rows in 8-bit integers: out_ik = (sum_j q_ij qw_kj) s_i sw_k, k < m, the sum exact.  x of any
+ * bigcn_type: BIGCN_I8 with its scales s_x [n] (rows as bigcn_quantize_rows() lays them out), or another type with s_x
+ * null, which is quantised on the way.  q_w int8 [m x ldqw], s_w fp32 [m]: the class matrix by bigcn_quantize_rows().  out
+ * of any type but BIGCN_I8, [n x ldo].  Serves from one row on.  n, m < 2^31.  Needs
+ * bigcn_quantized_product_workspace_bytes(n, d) of workspace unless x is BIGCN_I8. */
+size_t bigcn_quantized_product_workspace_bytes(int64_t n, int32_t d);
+bigcn_status bigcn_quantized_product(bigcn_ctx* ctx, const void* x, int32_t x_type, const float* s_x, int64_t n, int32_t d,
+                                     int64_t ldx, const int8_t* q_w, int64_t ldqw, const float* s_w, int32_t m, void* out,
+                                     int32_t out_type, int64_t ldo);
+
 /* Bi-GraphSAGE with the mean aggregator (Sec. 4.4.2, Eq. "bisage-conv"):
  *   h_i' = W_theta (*) h_i + (1/|N_i|) sum_{j in N_i} W_n (*) h_j,   no activation,
  * both products by XNOR and bit count on the same binarized input.

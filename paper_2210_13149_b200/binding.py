@@ -24,6 +24,7 @@ OPT_BYTE_AGGREGATION = 4   # rows of 129..256 bytes: 0 = default (3 where only b
 OPT_CONTRACTION = 3     # 0 = auto (default), 1 = XOR / bit-count pipe, 2 = tensor cores wherever the shape is covered
 OPT_WAIT_TRIES = 6      # bound of the waits inside a block of the layer kernels on packed bits (0 = default)
 OPT_ORDER = 5           # 0 = the faster one (default), 1 = contraction first, 2 = aggregation of the packed bits first
+TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.int8: 3}     # enum bigcn_type
 ZETA_AUTO, ZETA_F32, ZETA_I16, ZETA_I8, ZETA_F16, ZETA_I8H = 0, 1, 2, 3, 4, 5
 
 _i32, _i64, _vp, _sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t
@@ -86,6 +87,13 @@ SIGNATURES = {
     "bigcn_backward_workspace_bytes": (_sz, [_i64, _i32, _i32]),
     "bigcn_layer_backward": (ctypes.c_int, [_vp, ctypes.POINTER(bigcn_graph), ctypes.POINTER(bigcn_layer), _vp, _i64,
                                             _vp, _vp, _vp, _i64, _vp, _i64, _vp, _i64]),
+    "bigcn_layer_norm": (ctypes.c_int, [_vp, _vp, _i32, _i64, _i32, _i64, _vp, _vp, ctypes.c_float, _vp, _i32, _i64, _vp, _vp]),
+    "bigcn_layer_norm_workspace_bytes": (_sz, [_i32]),
+    "bigcn_layer_norm_backward": (ctypes.c_int, [_vp, _vp, _i32, _i64, _vp, _i32, _i64, _i64, _i32, _vp, _vp, _vp, _vp, _i32, _i64,
+                                                 _vp, _vp]),
+    "bigcn_quantize_rows": (ctypes.c_int, [_vp, _vp, _i32, _i64, _i32, _i64, _vp, _i64, _vp]),
+    "bigcn_quantized_product_workspace_bytes": (_sz, [_i64, _i32]),
+    "bigcn_quantized_product": (ctypes.c_int, [_vp, _vp, _i32, _vp, _i64, _i32, _i64, _vp, _i64, _vp, _i32, _vp, _i32, _i64]),
     "bigcn_measure_popc_peak": (ctypes.c_int, [_vp, ctypes.POINTER(ctypes.c_double)]),
     "bigcn_measure_gather_peak": (ctypes.c_int, [_vp, _vp, ctypes.c_int32, ctypes.POINTER(ctypes.c_double)]),
     "bigcn_layer_forward_noalloc": (ctypes.c_int, [_vp, ctypes.POINTER(bigcn_graph), ctypes.POINTER(bigcn_layer),
@@ -211,6 +219,7 @@ class BiGCN:
             raise BigcnError(st, self.lib.bigcn_status_string(st).decode())
         self.h = h
         self.workspace: Optional[torch.Tensor] = None
+        self._captured: List[torch.Tensor] = []     # workspaces that captured graphs refer to
 
     def close(self):
         if getattr(self, "h", None):
@@ -430,6 +439,118 @@ class BiGCN:
             _ptr(in_bits), _ptr(in_beta), _ptr(h), d_out,
             ctypes.byref(next_layer.c) if next_layer is not None else None, _ptr(nb), _ptr(nbeta)))
         return {"h": h, "next_bits": nb, "next_beta": nbeta}
+
+    # -- the dense ends: norm of rows, 8-bit products
+    def _rows(self, name: str, t: torch.Tensor, types=(torch.float32, torch.bfloat16, torch.float16), cols: Optional[int] = None,
+              rows: Optional[int] = None):
+        """Checks a matrix argument and returns its leading dimension."""
+        if t.dim() != 2 or t.dtype not in types or t.device != self.device:
+            raise ValueError("%s: a matrix on %s of one of the types %s is wanted" % (name, self.device, [str(x) for x in types]))
+        n, d = t.shape
+        if (rows is not None and n != rows) or (cols is not None and d != cols):
+            raise ValueError("%s: %d x %d elements where %s x %s are wanted" % (name, n, d, "any" if rows is None else rows, "any" if cols is None else cols))
+        if d > 1 and t.stride(1) != 1:
+            raise ValueError("%s: the elements of a row must lie next to each other" % name)
+        if n > 1 and t.stride(0) < d:
+            raise ValueError("%s: rows overlap" % name)
+        return t.stride(0) if n > 1 else d
+
+    def _vector(self, name: str, t: Optional[torch.Tensor], length: int, dtype=torch.float32):
+        if t is not None and (t.dim() != 1 or t.numel() != length or t.dtype != dtype or t.device != self.device or (length > 1 and t.stride(0) != 1)):
+            raise ValueError("%s: %d contiguous elements of %s on %s are wanted" % (name, length, dtype, self.device))
+
+    def _scratch(self, nbytes: int):
+        """Workspace on the context's own stream.  One that a graph capture has used stays alive with the context."""
+        if self.workspace is None or self.workspace.numel() < nbytes:
+            with torch.cuda.stream(self.stream):
+                self.ensure_workspace(nbytes)
+        if torch.cuda.is_current_stream_capturing() and not any(w is self.workspace for w in self._captured):
+            self._captured.append(self.workspace)
+
+    def _out(self, shape, dtype):
+        """An output's memory, in the order of the context's stream."""
+        if torch.cuda.current_stream(self.device) == self.stream:
+            return self._empty(shape, dtype)
+        with torch.cuda.stream(self.stream):
+            return self._empty(shape, dtype)
+
+    def layer_norm(self, X: torch.Tensor, gain: Optional[torch.Tensor] = None, offset: Optional[torch.Tensor] = None,
+                   eps: float = 1e-5, out_dtype: Optional[torch.dtype] = None):
+        """Layer norm of the rows of X: (Y, mean, rstd)."""
+        ldx = self._rows("X", X)
+        n, d = X.shape
+        self._vector("gain", gain, d)
+        self._vector("offset", offset, d)
+        out_dtype = X.dtype if out_dtype is None else out_dtype
+        if out_dtype not in (torch.float32, torch.bfloat16, torch.float16):
+            raise ValueError("layer_norm: no output of type %s" % out_dtype)
+        Y, mean, rstd = self._out((n, d), out_dtype), self._out(n, torch.float32), self._out(n, torch.float32)
+        self._check(self.lib.bigcn_layer_norm(self.h, _ptr(X), TYPES[X.dtype], n, d, ldx, _ptr(gain), _ptr(offset), eps, _ptr(Y),
+                                              TYPES[out_dtype], d, _ptr(mean), _ptr(rstd)))
+        return Y, mean, rstd
+
+    def layer_norm_backward(self, g_y: torch.Tensor, X: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                            gain: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None):
+        """Gradients of layer_norm(): (g_x, g_gain, g_offset); g_x in X's type unless out_dtype says otherwise."""
+        ldx = self._rows("X", X)
+        n, d = X.shape
+        ldg = self._rows("g_y", g_y, cols=d, rows=n)
+        self._vector("gain", gain, d)
+        self._vector("mean", mean, n)
+        self._vector("rstd", rstd, n)
+        out_dtype = X.dtype if out_dtype is None else out_dtype
+        if out_dtype not in (torch.float32, torch.bfloat16, torch.float16):
+            raise ValueError("layer_norm_backward: no output of type %s" % out_dtype)
+        self._scratch(int(self.lib.bigcn_layer_norm_workspace_bytes(d)))
+        g_x, g_gain, g_offset = self._out((n, d), out_dtype), self._out(d, torch.float32), self._out(d, torch.float32)
+        self._check(self.lib.bigcn_layer_norm_backward(
+            self.h, _ptr(g_y), TYPES[g_y.dtype], ldg, _ptr(X), TYPES[X.dtype], ldx, n, d, _ptr(gain), _ptr(mean), _ptr(rstd),
+            _ptr(g_x), TYPES[out_dtype], d, _ptr(g_gain), _ptr(g_offset)))
+        return g_x, g_gain, g_offset
+
+    def quantize_rows(self, X: torch.Tensor):
+        """Rows in 8-bit integers: (q int8 [n x d rounded up to 16], scale [n]); columns of q past d are zero."""
+        ldx = self._rows("X", X)
+        n, d = X.shape
+        ldq = (d + 15) // 16 * 16
+        q, scale = self._out((n, ldq), torch.int8), self._out(n, torch.float32)
+        if ldq != d:
+            with torch.cuda.stream(self.stream):
+                q[:, d:] = 0
+        self._check(self.lib.bigcn_quantize_rows(self.h, _ptr(X), TYPES[X.dtype], n, d, ldx, _ptr(q), ldq, _ptr(scale)))
+        return q, scale
+
+    def quantized_product(self, X: torch.Tensor, q_w: torch.Tensor, s_w: torch.Tensor, s_x: Optional[torch.Tensor] = None,
+                          out_dtype: torch.dtype = torch.float32):
+        """Rows times class rows in 8-bit integers: [n x m].  X in a floating type is quantised on the way; int8 rows come with
+        their scales s_x, both as quantize_rows() returns them; so do q_w and s_w."""
+        ready = X.dtype == torch.int8
+        n = X.shape[0] if X.dim() == 2 else -1
+        m = q_w.shape[0] if q_w.dim() == 2 else -1
+        ldqw = self._rows("q_w", q_w, types=(torch.int8,), rows=m)
+        if ready:
+            ldx = self._rows("X", X, types=(torch.int8,))
+            if s_x is None:
+                raise ValueError("X: int8 rows come with their scales s_x")
+            d = min(X.shape[1], q_w.shape[1])
+            if X.shape[1] != q_w.shape[1] and (X.shape[1] + 15) // 16 != (q_w.shape[1] + 15) // 16:
+                raise ValueError("X: rows of %d for class rows of %d" % (X.shape[1], q_w.shape[1]))
+            self._vector("s_x", s_x, n)
+        else:
+            ldx = self._rows("X", X)
+            if s_x is not None:
+                raise ValueError("s_x goes with int8 rows only")
+            d = X.shape[1]
+            if (d + 15) // 16 * 16 != (q_w.shape[1] + 15) // 16 * 16 or q_w.shape[1] < d:
+                raise ValueError("X: rows of %d for class rows of %d" % (d, q_w.shape[1]))
+            self._scratch(int(self.lib.bigcn_quantized_product_workspace_bytes(n, d)))
+        self._vector("s_w", s_w, m)
+        if out_dtype not in (torch.float32, torch.bfloat16, torch.float16):
+            raise ValueError("quantized_product: no output of type %s" % out_dtype)
+        out = self._out((n, m), out_dtype)
+        self._check(self.lib.bigcn_quantized_product(self.h, _ptr(X), TYPES[X.dtype], _ptr(s_x), n, d, ldx, _ptr(q_w), ldqw, _ptr(s_w), m,
+                                                     _ptr(out), TYPES[out_dtype], m))
+        return out
 
     def measure_popc_peak(self) -> float:
         """32-bit XOR + bit-count + add steps per second of this GPU (register-only probe)."""

@@ -183,6 +183,33 @@ bigcn_status check_layer(bigcn_ctx* ctx, const bigcn_layer* l, const char* name)
     return BIGCN_OK;
 }
 
+bigcn_status check_type(bigcn_ctx* ctx, const char* name, int32_t type)
+{
+    if (type != BIGCN_F32 && type != BIGCN_BF16 && type != BIGCN_F16) return fail(ctx, BIGCN_ERR_UNSUPPORTED, "%s: type %d is not supported", name, type);
+    return BIGCN_OK;
+}
+
+// Rows of a dense operator.
+bigcn_status check_rows(bigcn_ctx* ctx, const char* name, const void* p, int32_t type, int64_t n, int32_t d, int64_t ld)
+{
+    const bigcn_status st = check_type(ctx, name, type);
+    if (st != BIGCN_OK) return st;
+    if (n < 0 || n >= (int64_t(1) << 31) || d < 1 || ld < d) return fail(ctx, BIGCN_ERR_SHAPE, "%s: n=%lld d=%d ld=%lld", name, (long long)n, d, (long long)ld);
+    if (d > BIGCN_MAX_D_IN) return fail(ctx, BIGCN_ERR_UNSUPPORTED, "%s: rows of %d > %d are not supported", name, d, BIGCN_MAX_D_IN);
+    if (n > 0 && !p) return fail(ctx, BIGCN_ERR_NULL, "%s is null", name);
+    if (!aligned(p, type == BIGCN_F32 ? 4 : 2)) return fail(ctx, BIGCN_ERR_ALIGN, "%s is not aligned to its elements", name);
+    return BIGCN_OK;
+}
+// 8-bit rows and their scales.
+bigcn_status check_quantized(bigcn_ctx* ctx, const char* name, const void* q, int64_t n, int32_t d, int64_t ldq, const float* scale)
+{
+    if (n < 0 || n >= (int64_t(1) << 31) || d < 1 || ldq < d) return fail(ctx, BIGCN_ERR_SHAPE, "%s: n=%lld d=%d ld=%lld", name, (long long)n, d, (long long)ldq);
+    if (d > BIGCN_MAX_D_IN) return fail(ctx, BIGCN_ERR_UNSUPPORTED, "%s: rows of %d > %d are not supported", name, d, BIGCN_MAX_D_IN);
+    if (n > 0 && (!q || !scale)) return fail(ctx, BIGCN_ERR_NULL, "%s or its scales are null", name);
+    if (ldq % 16 != 0 || !aligned(q, 16)) return fail(ctx, BIGCN_ERR_ALIGN, "%s: rows must start on 16-byte boundaries (ld=%lld)", name, (long long)ldq);
+    return BIGCN_OK;
+}
+
 // Whether a layer aggregates the packed bits before the contraction (spmm_bits.cu), in `room` bytes of scratch.  Options that
 // name a storage format or a kernel of the other order, and the debug taps on the contraction, keep to that order; so does
 // by default a layer called for H' alone (not hidden), whose values then round as they always did.
@@ -561,6 +588,7 @@ bigcn_status bigcn_sync_check(bigcn_ctx* ctx)
     if (backward_tc_timeouts() != 0) return fail(ctx, BIGCN_ERR_INTERNAL, "a bounded wait on the tensor cores ran out (backward kernel)");
     if (spmm_tc_timeouts() != 0) return fail(ctx, BIGCN_ERR_INTERNAL, "a bounded wait ran out (tensor-core aggregation kernel)");
     if (spmm_bits_timeouts() != 0) return fail(ctx, BIGCN_ERR_INTERNAL, "a bounded wait ran out (layer kernel on packed bits)");
+    if (quant_timeouts() != 0) return fail(ctx, BIGCN_ERR_INTERNAL, "a bounded wait ran out (product of 8-bit rows)");
     return BIGCN_OK;
 }
 
@@ -975,6 +1003,107 @@ bigcn_status bigcn_entropy_bins(bigcn_ctx* ctx, const float* H, int64_t n, int32
                                         ctx->ws, &ctx->launches_i);
     finish_call(ctx);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "entropy estimate launch");
+    return BIGCN_OK;
+}
+
+size_t bigcn_layer_norm_workspace_bytes(int32_t d) { return d < 1 ? 0 : layer_norm_scratch_bytes(d); }
+
+bigcn_status bigcn_layer_norm(bigcn_ctx* ctx, const void* x, int32_t x_type, int64_t n, int32_t d, int64_t ldx,
+                              const float* gain, const float* offset, float eps, void* y, int32_t y_type, int64_t ldy,
+                              float* mean, float* rstd)
+{
+    bigcn_status st = bind_device(ctx);
+    if (st != BIGCN_OK) return st;
+    if ((st = check_rows(ctx, "x", x, x_type, n, d, ldx)) != BIGCN_OK) return st;
+    if ((st = check_rows(ctx, "y", y, y_type, n, d, ldy)) != BIGCN_OK) return st;
+    if (!(eps >= 0.f)) return fail(ctx, BIGCN_ERR_SHAPE, "eps=%g must be >= 0", (double)eps);
+    if (n == 0) return BIGCN_OK;
+    if (!mean || !rstd) return fail(ctx, BIGCN_ERR_NULL, "mean or rstd is null");
+    cudaError_t e = launch_layer_norm(ctx->stream, x, x_type, n, d, ldx, gain, offset, eps, y, y_type, ldy, mean, rstd, &ctx->launches_i);
+    finish_call(ctx);
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "layer norm launch");
+    return BIGCN_OK;
+}
+
+bigcn_status bigcn_layer_norm_backward(bigcn_ctx* ctx, const void* g_y, int32_t g_type, int64_t ldg, const void* x, int32_t x_type,
+                                       int64_t ldx, int64_t n, int32_t d, const float* gain, const float* mean,
+                                       const float* rstd, void* g_x, int32_t g_x_type, int64_t ldgx, float* g_gain,
+                                       float* g_offset)
+{
+    bigcn_status st = bind_device(ctx);
+    if (st != BIGCN_OK) return st;
+    if ((st = check_rows(ctx, "g_y", g_y, g_type, n, d, ldg)) != BIGCN_OK) return st;
+    if ((st = check_rows(ctx, "x", x, x_type, n, d, ldx)) != BIGCN_OK) return st;
+    if ((st = check_rows(ctx, "g_x", g_x, g_x_type, n, d, ldgx)) != BIGCN_OK) return st;
+    if (n == 0) {                                             // no rows: every sum over them is empty
+        if (g_gain) BIGCN_CUDA(ctx, cudaMemsetAsync(g_gain, 0, (size_t)d * 4, ctx->stream));
+        if (g_offset) BIGCN_CUDA(ctx, cudaMemsetAsync(g_offset, 0, (size_t)d * 4, ctx->stream));
+        return BIGCN_OK;
+    }
+    if (!mean || !rstd) return fail(ctx, BIGCN_ERR_NULL, "mean or rstd is null");
+    if ((g_gain || g_offset) && (!ctx->ws || ctx->ws_bytes < layer_norm_scratch_bytes(d)))
+        return fail(ctx, BIGCN_ERR_WORKSPACE, "needs %zu bytes of workspace (bigcn_layer_norm_workspace_bytes)", layer_norm_scratch_bytes(d));
+    cudaError_t e = launch_layer_norm_backward(ctx->stream, g_y, g_type, ldg, x, x_type, ldx, n, d, gain, mean, rstd, g_x, g_x_type, ldgx,
+                                               g_gain, g_offset, ctx->ws, &ctx->launches_i);
+    finish_call(ctx);
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "layer norm backward launch");
+    return BIGCN_OK;
+}
+
+bigcn_status bigcn_quantize_rows(bigcn_ctx* ctx, const void* x, int32_t type, int64_t n, int32_t d, int64_t ldx, int8_t* q,
+                                 int64_t ldq, float* scale)
+{
+    bigcn_status st = bind_device(ctx);
+    if (st != BIGCN_OK) return st;
+    if ((st = check_rows(ctx, "x", x, type, n, d, ldx)) != BIGCN_OK) return st;
+    if ((st = check_quantized(ctx, "q", q, n, d, ldq, scale)) != BIGCN_OK) return st;
+    if (n == 0) return BIGCN_OK;
+    cudaError_t e = launch_quantize_rows(ctx->stream, x, type, n, d, ldx, q, ldq, scale, &ctx->launches_i);
+    finish_call(ctx);
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "quantize launch");
+    return BIGCN_OK;
+}
+
+size_t bigcn_quantized_product_workspace_bytes(int64_t n, int32_t d)
+{
+    if (n < 0 || d < 1) return 0;
+    return up((size_t)n * (size_t)round_up(d, 16)) + up((size_t)n * 4);
+}
+
+bigcn_status bigcn_quantized_product(bigcn_ctx* ctx, const void* x, int32_t x_type, const float* s_x, int64_t n, int32_t d,
+                                     int64_t ldx, const int8_t* q_w, int64_t ldqw, const float* s_w, int32_t m, void* out,
+                                     int32_t out_type, int64_t ldo)
+{
+    bigcn_status st = bind_device(ctx);
+    if (st != BIGCN_OK) return st;
+    if (m < 1) return fail(ctx, BIGCN_ERR_SHAPE, "m=%d must be >= 1", m);
+    const bool ready = x_type == BIGCN_I8;
+    if (ready) st = check_quantized(ctx, "x", x, n, d, ldx, s_x);
+    else if (s_x) return fail(ctx, BIGCN_ERR_UNSUPPORTED, "s_x goes with BIGCN_I8 rows only");
+    else st = check_rows(ctx, "x", x, x_type, n, d, ldx);
+    if (st != BIGCN_OK) return st;
+    if ((st = check_quantized(ctx, "q_w", q_w, m, d, ldqw, s_w)) != BIGCN_OK) return st;
+    if ((st = check_type(ctx, "out", out_type)) != BIGCN_OK) return st;
+    if (ldo < m) return fail(ctx, BIGCN_ERR_SHAPE, "out: ld=%lld < m=%d", (long long)ldo, m);
+    if (n == 0) return BIGCN_OK;
+    if (!out) return fail(ctx, BIGCN_ERR_NULL, "out is null");
+    if (!aligned(out, out_type == BIGCN_F32 ? 4 : 2)) return fail(ctx, BIGCN_ERR_ALIGN, "out is not aligned to its elements");
+    const int8_t* q_x = static_cast<const int8_t*>(x);
+    cudaError_t e = cudaSuccess;
+    if (!ready) {
+        const size_t need = bigcn_quantized_product_workspace_bytes(n, d);
+        if (!ctx->ws || ctx->ws_bytes < need) return fail(ctx, BIGCN_ERR_WORKSPACE, "needs %zu bytes of workspace (bigcn_quantized_product_workspace_bytes)", need);
+        int8_t* q = static_cast<int8_t*>(ctx->ws);
+        const int64_t ldq = round_up(d, 16);
+        float* scale = reinterpret_cast<float*>(q + up((size_t)n * (size_t)ldq));
+        e = launch_quantize_rows(ctx->stream, x, x_type, n, d, ldx, q, ldq, scale, &ctx->launches_i);
+        q_x = q;
+        ldx = ldq;
+        s_x = scale;
+    }
+    if (e == cudaSuccess) e = launch_quantized_product(ctx->stream, q_x, ldx, s_x, n, d, q_w, ldqw, s_w, m, out, out_type, ldo, &ctx->launches_i);
+    finish_call(ctx);
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "quantized product launch");
     return BIGCN_OK;
 }
 

@@ -186,4 +186,18 @@ cudaError_t launch_layer_backward(cudaStream_t s, int64_t n, const int64_t* rowp
                                   int64_t ldgi, float* g_w, int64_t ldgw, int64_t long_row, void* scratch,
                                   int* launches);
 
+// Layer norm of rows (rownorm.cu); types are bigcn_type.  scratch: layer_norm_scratch_bytes().
+size_t layer_norm_scratch_bytes(int d);
+cudaError_t launch_layer_norm(cudaStream_t s, const void* x, int x_type, int64_t n, int d, int64_t ldx, const float* gain, const float* offset,
+                              float eps, void* y, int y_type, int64_t ldy, float* mean, float* rstd, int* launches);
+cudaError_t launch_layer_norm_backward(cudaStream_t s, const void* g, int g_type, int64_t ldg, const void* x, int x_type, int64_t ldx, int64_t n, int d,
+                                       const float* gain, const float* mean, const float* rstd, void* gx, int gx_type, int64_t ldgx,
+                                       float* g_gain, float* g_offset, void* scratch, int* launches);
+
+// Rows in 8-bit integers and their product with 8-bit class rows (quant.cu).
+cudaError_t launch_quantize_rows(cudaStream_t s, const void* x, int type, int64_t n, int d, int64_t ldx, int8_t* q, int64_t ldq, float* scale, int* launches);
+cudaError_t launch_quantized_product(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const float* s_x, int64_t n, int d, const int8_t* q_w, int64_t ldqw,
+                                     const float* s_w, int m, void* out, int out_type, int64_t ldo, int* launches);
+int quant_timeouts();
+
 }  // namespace bigcn

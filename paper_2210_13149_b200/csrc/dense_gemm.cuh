@@ -1,0 +1,414 @@
+// The dense products on the 5th-generation tensor cores: D = A B^T over operands in device memory, with an epilogue of the
+// including file's choice on the accumulators.
+//
+// One persistent block per multiprocessor, its warps in roles: eight warps of the epilogue, one that fetches tiles of 128 bytes of
+// depth by TMA into a ring of shared-memory stages (128-byte swizzle), one that issues tcgen05.mma.  Accumulators lie in tensor
+// memory twice, so that the epilogue of a tile runs beside the products of the next.  CTAS = 2: two blocks of a cluster share a tile of 256
+// rows; each fetches its 128 rows of A and half of B's rows, and the first one issues products over both halves, so that B
+// crosses shared memory once for 256 rows.
+//
+// An operand is K-major (rows of depth-contiguous elements) or MN-major (its depth is the slow axis; bf16 only here).  Elements past the
+// tensor's edges read as zero, which is what pads rows, columns and depth.  The tiles may be split along the depth ("splits").
+//
+// Every wait is bounded.  If one runs out the block raises a flag that bigcn_sync_check() reports, waits (bounded) for its own copies
+// and products in flight, frees its tensor memory and returns.
+#pragma once
+#include <cuda.h>
+
+#include <algorithm>
+
+#include "bigcn_internal.cuh"
+#include "tc_common.cuh"
+
+namespace bigcn {
+namespace gemm {
+
+constexpr int kEpiWarps = 8, kProducer = 8, kIssuer = 9, kThreads = 320;
+constexpr int kRows = 128;                    // rows of a block's tile: the lanes of tensor memory
+constexpr int kDepthBytes = 128;              // depth of a stage
+constexpr int kTries = 1 << 22;               // bound of every wait, in tries of up to about a microsecond
+constexpr int kMaxStages = 8;
+
+// Sizes of a product.  `count`, where given, holds at run time how many of the rows (or, with over_depth, of the depth) there are
+// (at most the m or k given here); A is read through the second map where that is all of them.
+struct Shape {
+    int m, n, k;             // rows, columns, depth (elements)
+    int splits;              // of the depth
+    const int* count;
+    bool over_depth;
+    int alt_a, alt_b;        // 1: the second map is this operand's where *count says that nothing was left out
+};
+
+struct Unit {
+    int row, col;            // first row and column of the (pair's) tile
+    int k0, k1;              // stages of depth [k0, k1)
+    int split;
+};
+
+// Order of the tiles: bands of kBand row tiles, and in a band columns outside, rows inside, so that what runs at a time shares rows
+// and columns in L2.
+struct Walk {
+    int m, tiles_m, tiles_n, stages, per_split, splits, tile_rows, tile_cols;
+    static constexpr int kBand = 8;
+    __device__ Walk(const Shape& s, int tile_rows_, int tile_cols_, int depth)
+    {
+        int mm = s.m, kk = s.k;
+        if (s.count) {
+            const int c = *s.count;
+            if (s.over_depth) kk = min(kk, c); else mm = min(mm, c);
+        }
+        m = mm;
+        tile_rows = tile_rows_;
+        tile_cols = tile_cols_;
+        tiles_m = (mm + tile_rows - 1) / tile_rows;
+        tiles_n = (s.n + tile_cols - 1) / tile_cols;
+        stages = (kk + depth - 1) / depth;
+        splits = s.splits;
+        per_split = (stages + splits - 1) / splits;
+    }
+    __device__ int units() const { return tiles_m * tiles_n * splits; }
+    __device__ Unit at(int u) const
+    {
+        Unit r;
+        const int tiles = tiles_m * tiles_n;
+        r.split = u / tiles;
+        const int t = u - r.split * tiles, band = t / (kBand * tiles_n), in = t - band * kBand * tiles_n;
+        const int rows = min(kBand, tiles_m - band * kBand);
+        r.col = in / rows * tile_cols;
+        r.row = (band * kBand + in % rows) * tile_rows;
+        r.k0 = min(stages, r.split * per_split);
+        r.k1 = min(stages, r.k0 + per_split);
+        return r;
+    }
+};
+
+// ---- device pieces -------------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_meet()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+}
+__device__ __forceinline__ void init_barrier(uint64_t* bar, int count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(tc::smem_u32(bar)), "r"(count) : "memory");
+}
+// true once the phase is complete; false when the block gave up
+__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile int* abort, int* flag)
+{
+    for (int it = 0; it < kTries; ++it) {
+        uint32_t done;
+        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2, 1000;\nselp.u32 %0, 1, 0, p;\n}\n"
+                     : "=r"(done) : "r"(tc::smem_u32(bar)), "r"(parity) : "memory");
+        if (done) return true;
+        if ((it & 15) == 15 && *abort) return false;
+    }
+    atomicExch(flag, 1);
+    *abort = 1;
+    return false;
+}
+template <int CTAS>
+__device__ __forceinline__ void expect_bytes(uint64_t* bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(tc::smem_u32(bar)), "r"(bytes) : "memory");
+}
+// A box of the tensor at (x, y) into shared memory; the bytes are counted at `bar` (of the cluster's first block with CTAS = 2).
+template <int CTAS>
+__device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, int x, int y, uint64_t* bar)
+{
+    if constexpr (CTAS == 2)
+        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n"
+                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(tc::smem_u32(bar) & 0xFEFFFFFFu) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n"
+                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(tc::smem_u32(bar)) : "memory");
+}
+// Counts at `bar` (of every block of the cluster) once all products issued so far are done.
+template <int CTAS>
+__device__ __forceinline__ void commit(uint64_t* bar)
+{
+    if constexpr (CTAS == 2)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n"
+                     ::"r"(tc::smem_u32(bar)), "h"((uint16_t)3) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" ::"r"(tc::smem_u32(bar)) : "memory");
+}
+template <bool I8, int CTAS>
+__device__ __forceinline__ void product(uint32_t acc, uint64_t a, uint64_t b, uint32_t idesc, bool add)
+{
+#define BIGCN_MMA(KIND, GROUP)                                                                                                       \
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], %1, %2, %3, p;\n}\n" \
+                 ::"r"(acc), "l"(a), "l"(b), "r"(idesc), "r"(add ? 1u : 0u) : "memory")
+    if constexpr (I8 && CTAS == 1) BIGCN_MMA("i8", "1");
+    else if constexpr (I8) BIGCN_MMA("i8", "2");
+    else if constexpr (CTAS == 1) BIGCN_MMA("f16", "1");
+    else BIGCN_MMA("f16", "2");
+#undef BIGCN_MMA
+}
+// An arrival at the barrier of the cluster's first block.
+template <int CTAS>
+__device__ __forceinline__ void arrive_first(uint64_t* bar)
+{
+    if constexpr (CTAS == 2) {
+        uint32_t remote;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, 0;\n" : "=r"(remote) : "r"(tc::smem_u32(bar)));
+        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(remote) : "memory");
+    } else {
+        asm volatile("mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];\n" ::"r"(tc::smem_u32(bar)) : "memory");
+    }
+}
+
+// Descriptor of a shared-memory operand with 128-byte swizzle (layout type 2, descriptor version 1).  K-major: groups of 8 rows
+// x 128 bytes follow each other, `sbo` = 1024 bytes apart.  MN-major: blocks of 64 elements x 64 steps of depth, 8192 bytes apart
+// (`lbo`), in which groups of 8 steps are 1024 bytes apart (`sbo`).
+__device__ __forceinline__ uint64_t swizzled_desc(uint32_t addr, uint32_t lbo, uint32_t sbo)
+{
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(lbo >> 4) << 16 | (uint64_t)(sbo >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+
+template <int BN, int CTAS>
+struct Config {
+    static constexpr int kBRows = BN / CTAS;                     // rows of B a block holds
+    static constexpr int kABytes = kRows * kDepthBytes, kBBytes = kBRows * kDepthBytes, kStage = kABytes + kBBytes;
+    static constexpr int kFit = 196608 / kStage;
+    static constexpr int kStages = kFit < kMaxStages ? kFit : kMaxStages;
+    static constexpr size_t kSmem = (size_t)kStages * kStage + 1024;
+};
+
+struct Control {
+    uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drained;
+    uint32_t tmem;
+    int abort;
+};
+
+// Epi: struct with Args, and
+//   static __device__ void tile(const Args&, const Shape&, const Unit&, int row0, int rows_there, uint32_t acc, bool empty)
+// run by the eight epilogue warps: warp w has lanes 32 (w & 3) .. + 31 of tensor memory (rows of the tile) and columns
+// (w >> 2) BN / 2 .. + BN / 2 - 1; `acc` is the address of its lanes and first column.  row0: first row of the block's 128;
+// rows_there: rows of the whole product.  empty: no depth, the accumulators hold nothing.
+template <bool I8, int BN, int CTAS, bool A_MN, bool B_MN, class Epi>
+__global__ void __launch_bounds__(kThreads, 1)
+product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_alt,
+               const __grid_constant__ Shape shape, const __grid_constant__ typename Epi::Args args, int* flag)
+{
+    using C = Config<BN, CTAS>;
+    constexpr int kDepth = I8 ? 128 : 64;
+    extern __shared__ unsigned char raw[];
+    __shared__ Control ctl;
+    unsigned char* stages = raw + ((1024u - (tc::smem_u32(raw) & 1023u)) & 1023u);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = CTAS == 2 ? cluster_rank() : 0u;
+    constexpr int kCols = 2 * BN < 32 ? 32 : 2 * BN;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < C::kStages; ++i) {
+            init_barrier(&ctl.full[i], 1);
+            init_barrier(&ctl.empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            init_barrier(&ctl.acc_full[i], 1);
+            init_barrier(&ctl.acc_empty[i], kEpiWarps * CTAS);
+        }
+        init_barrier(&ctl.drained, 1);
+        ctl.abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+    }
+    if (warp == kIssuer) {
+        if constexpr (CTAS == 2) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(tc::smem_u32(&ctl.tmem)), "r"(kCols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;\n" ::: "memory");
+        } else {
+            tc::tmem_alloc(&ctl.tmem, kCols);
+        }
+    }
+    tc::fence_before_sync();
+    __syncthreads();
+    if constexpr (CTAS == 2) cluster_meet();
+    tc::fence_after_sync();
+    const uint32_t tmem = ctl.tmem;
+    volatile int* abort = &ctl.abort;
+
+    pdl_enter();
+    const Walk walk(shape, kRows * CTAS, BN, kDepth);
+    const int units = walk.units(), first = blockIdx.x / CTAS, step = gridDim.x / CTAS;
+
+    if (warp == kProducer) {
+        if (lane == 0) {
+            const bool whole = shape.count && *shape.count >= (shape.over_depth ? shape.k : shape.m);
+            const CUtensorMap* ma = whole && shape.alt_a ? &map_alt : &map_a;
+            const CUtensorMap* mb = whole && shape.alt_b ? &map_alt : &map_b;
+            int slot = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            int64_t issued = 0;
+            for (int u = first; u < units && ok; u += step) {
+                const Unit t = walk.at(u);
+                const int arow = t.row + (int)rank * kRows, brow = t.col + (int)rank * C::kBRows;
+                for (int k = t.k0; k < t.k1; ++k) {
+                    ok = wait(&ctl.empty[slot], phase ^ 1u, abort, flag);
+                    if (!ok) break;
+                    if (rank == 0) expect_bytes<CTAS>(&ctl.full[slot], C::kStage * CTAS);
+                    const uint32_t sa = tc::smem_u32(stages + slot * C::kStage), sb = sa + C::kABytes;
+                    if constexpr (A_MN) {
+#pragma unroll
+                        for (int i = 0; i < kRows / 64; ++i) copy_box<CTAS>(sa + i * 8192, ma, arow + 64 * i, k * kDepth, &ctl.full[slot]);
+                    } else {
+                        copy_box<CTAS>(sa, ma, k * kDepth, arow, &ctl.full[slot]);
+                    }
+                    if constexpr (B_MN) {
+#pragma unroll
+                        for (int i = 0; i < C::kBRows / 64; ++i) copy_box<CTAS>(sb + i * 8192, mb, brow + 64 * i, k * kDepth, &ctl.full[slot]);
+                    } else {
+                        copy_box<CTAS>(sb, mb, k * kDepth, brow, &ctl.full[slot]);
+                    }
+                    ++issued;
+                    if (++slot == C::kStages) slot = 0, phase ^= 1u;
+                }
+            }
+            // every stage handed back: nothing of the cluster touches this block's barriers or stages any more
+            for (int i = 0; i < C::kStages && ok; ++i) {
+                ok = wait(&ctl.empty[slot], phase ^ 1u, abort, flag);
+                if (++slot == C::kStages) slot = 0, phase ^= 1u;
+            }
+            if (!ok) {
+                // gave up: the copies that were issued have to land first; a second block's are counted at the first's barriers, so time
+                // (a thousand times what a copy takes) stands in for them
+                volatile int none = 0;
+                if (rank == 0)
+                    for (int64_t j = issued > C::kStages ? issued - C::kStages : 0; j < issued; ++j)
+                        wait(&ctl.full[j % C::kStages], (uint32_t)(j / C::kStages) & 1u, &none, flag);
+                for (int i = 0; i < 10; ++i) __nanosleep(1000000);
+            }
+        }
+        __syncwarp();
+    } else if (warp == kIssuer) {
+        if (lane == 0 && rank == 0) {
+            constexpr uint32_t idesc = (I8 ? 2u : 1u) << 4 | 1u << 7 | 1u << 10 | (A_MN ? 1u : 0u) << 15 | (B_MN ? 1u : 0u) << 16 |
+                                       (uint32_t)(BN >> 3) << 17 | (uint32_t)((kRows * CTAS) >> 4) << 24;
+            constexpr uint32_t step_a = A_MN ? 2048 >> 4 : 32 >> 4, step_b = B_MN ? 2048 >> 4 : 32 >> 4;
+            int slot = 0, buf = 0;
+            uint32_t phase = 0, acc_phase = 0;
+            bool ok = true, any = false;
+            for (int u = first; u < units && ok; u += step) {
+                const Unit t = walk.at(u);
+                if (t.k0 >= t.k1) continue;
+                ok = wait(&ctl.acc_empty[buf], acc_phase ^ 1u, abort, flag);
+                if (!ok) break;
+                tc::fence_after_sync();
+                const uint32_t acc = tmem + (uint32_t)(buf * BN);
+                for (int k = t.k0; k < t.k1; ++k) {
+                    ok = wait(&ctl.full[slot], phase, abort, flag);
+                    if (!ok) break;
+                    tc::fence_after_sync();
+                    const uint32_t sa = tc::smem_u32(stages + slot * C::kStage), sb = sa + C::kABytes;
+                    const uint64_t da = A_MN ? swizzled_desc(sa, 8192, 1024) : swizzled_desc(sa, 16, 1024);
+                    const uint64_t db = B_MN ? swizzled_desc(sb, 8192, 1024) : swizzled_desc(sb, 16, 1024);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) product<I8, CTAS>(acc, da + i * step_a, db + i * step_b, idesc, k > t.k0 || i > 0);
+                    any = true;
+                    commit<CTAS>(&ctl.empty[slot]);
+                    if (++slot == C::kStages) slot = 0, phase ^= 1u;
+                }
+                if (!ok) break;
+                commit<CTAS>(&ctl.acc_full[buf]);
+                if ((buf ^= 1) == 0) acc_phase ^= 1u;
+            }
+            if (!ok && any) {
+                volatile int none = 0;
+                if constexpr (CTAS == 2)
+                    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" ::"r"(tc::smem_u32(&ctl.drained)) : "memory");
+                else
+                    commit<1>(&ctl.drained);
+                wait(&ctl.drained, 0, &none, flag);
+            }
+        }
+        __syncwarp();
+    } else {
+        int buf = 0;
+        uint32_t acc_phase = 0;
+        for (int u = first; u < units; u += step) {
+            const Unit t = walk.at(u);
+            const bool empty = t.k0 >= t.k1;
+            if (!empty) {
+                if (!__all_sync(0xffffffffu, wait(&ctl.acc_full[buf], acc_phase, abort, flag))) break;
+                tc::fence_after_sync();
+            }
+            const uint32_t acc = tmem + (uint32_t)(buf * BN + (warp >> 2) * (BN / 2)) + ((uint32_t)((warp & 3) * 32) << 16);
+            Epi::template tile<BN>(args, shape, t, t.row + (int)rank * kRows, walk.m, acc, empty);
+            if (!empty) {
+                tc::fence_before_sync();
+                __syncwarp();
+                if (lane == 0) arrive_first<CTAS>(&ctl.acc_empty[buf]);
+                if ((buf ^= 1) == 0) acc_phase ^= 1u;
+            }
+        }
+    }
+    tc::fence_before_sync();
+    __syncthreads();
+    if constexpr (CTAS == 2) cluster_meet();
+    if (warp == kIssuer) {
+        tc::fence_after_sync();
+        if constexpr (CTAS == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(kCols) : "memory");
+        else tc::tmem_free(tmem, kCols);
+    }
+}
+
+// 32 consecutive 32-bit columns of this thread's lane; tmem_wait32() before they are used
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&v)[32])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+                   "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
+                   "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
+                   "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+                 : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_wait32(uint32_t (&v)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;\n"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+                   "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]),
+                   "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]),
+                   "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])
+                 :: "memory");
+}
+
+// ---- host pieces ---------------------------------------------------------------------------------------------------------
+
+// Tensor map of a row-major matrix (rows x cols elements of `elt` bytes, `pitch` bytes from row to row; base and pitch on 16-byte
+// boundaries), read in swizzled boxes of box_cols x box_rows.
+cudaError_t encode_map(CUtensorMap* map, const void* base, int elt, bool integers, int64_t rows, int64_t cols, int64_t pitch, int box_cols, int box_rows);
+
+template <bool I8, int BN, int CTAS, bool A_MN, bool B_MN, class Epi>
+cudaError_t launch(cudaStream_t s, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& alt, const Shape& shape, const typename Epi::Args& args, int* flag)
+{
+    using C = Config<BN, CTAS>;
+    auto* kernel = product_kernel<I8, BN, CTAS, A_MN, B_MN, Epi>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
+    if (e != cudaSuccess) return e;
+    const int64_t units = ceil_div(shape.m, kRows * CTAS) * ceil_div(shape.n, BN) * shape.splits;
+    const int clusters = (int)std::max<int64_t>(1, std::min<int64_t>(units, sm_count() / CTAS));
+    cudaLaunchAttribute attr[2] = {};
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = CTAS;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(clusters * CTAS));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = C::kSmem;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, a, b, alt, shape, args, flag);
+}
+
+}  // namespace gemm
+}  // namespace bigcn

@@ -1,0 +1,119 @@
+// Element types of the dense operators (layer norm, 8-bit products, class loss): loads to fp32 and rounded stores.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+#include "bigcn_internal.cuh"
+
+namespace bigcn {
+namespace dense {
+
+__host__ __device__ constexpr int type_bytes(int type) { return type == BIGCN_F32 ? 4 : 2; }
+
+template <int TYPE> struct Elt;
+template <> struct Elt<BIGCN_F32> { using T = float; };
+template <> struct Elt<BIGCN_BF16> { using T = __nv_bfloat16; };
+template <> struct Elt<BIGCN_F16> { using T = __half; };
+
+template <int TYPE>
+__device__ __forceinline__ float to_float(typename Elt<TYPE>::T v)
+{
+    if constexpr (TYPE == BIGCN_F32) return v;
+    else if constexpr (TYPE == BIGCN_BF16) return __bfloat162float(v);
+    else return __half2float(v);
+}
+template <int TYPE>
+__device__ __forceinline__ typename Elt<TYPE>::T from_float(float v)
+{
+    if constexpr (TYPE == BIGCN_F32) return v;
+    else if constexpr (TYPE == BIGCN_BF16) return __float2bfloat16_rn(v);
+    else return __float2half_rn(v);
+}
+// two values as one 32-bit word of a 16-bit type, the first in the low half
+template <int TYPE>
+__device__ __forceinline__ uint32_t pack2(float a, float b)
+{
+    if constexpr (TYPE == BIGCN_BF16) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    } else {
+        const __half2 h = __floats2half2_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+}
+template <int TYPE>
+__device__ __forceinline__ float2 unpack2(uint32_t w)
+{
+    if constexpr (TYPE == BIGCN_BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    else return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+
+// V (4 or 8) consecutive elements, of which the first `count` exist; the rest read as 0.  `whole`: the pointer is aligned to V
+// elements, and they can be moved as whole words where all of them exist.
+template <int TYPE, int V>
+__device__ __forceinline__ void load_elts(const typename Elt<TYPE>::T* __restrict__ p, int count, bool whole, float (&v)[V])
+{
+    if (whole && count >= V) {
+        if constexpr (TYPE == BIGCN_F32) {
+#pragma unroll
+            for (int i = 0; i < V; i += 4) {
+                const float4 w = *reinterpret_cast<const float4*>(p + i);
+                v[i] = w.x; v[i + 1] = w.y; v[i + 2] = w.z; v[i + 3] = w.w;
+            }
+        } else if constexpr (V == 4) {
+            const uint2 w = *reinterpret_cast<const uint2*>(p);
+            const float2 a = unpack2<TYPE>(w.x), b = unpack2<TYPE>(w.y);
+            v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+        } else {
+            const uint4 w = *reinterpret_cast<const uint4*>(p);
+            const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 a = unpack2<TYPE>(ws[i]);
+                v[2 * i] = a.x;
+                v[2 * i + 1] = a.y;
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = i < count ? to_float<TYPE>(p[i]) : 0.f;
+}
+
+template <int TYPE, int V>
+__device__ __forceinline__ void store_elts(typename Elt<TYPE>::T* __restrict__ p, int count, bool whole, const float (&v)[V])
+{
+    if (whole && count >= V) {
+        if constexpr (TYPE == BIGCN_F32) {
+#pragma unroll
+            for (int i = 0; i < V; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+        } else if constexpr (V == 4) {
+            *reinterpret_cast<uint2*>(p) = make_uint2(pack2<TYPE>(v[0], v[1]), pack2<TYPE>(v[2], v[3]));
+        } else {
+            *reinterpret_cast<uint4*>(p) = make_uint4(pack2<TYPE>(v[0], v[1]), pack2<TYPE>(v[2], v[3]), pack2<TYPE>(v[4], v[5]), pack2<TYPE>(v[6], v[7]));
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        if (i < count) p[i] = from_float<TYPE>(v[i]);
+}
+// the same with the type known at run time
+template <int V>
+__device__ __forceinline__ void store_as(void* base, int type, int64_t at, int count, bool whole, const float (&v)[V])
+{
+    if (type == BIGCN_F32) store_elts<BIGCN_F32, V>(static_cast<float*>(base) + at, count, whole, v);
+    else if (type == BIGCN_BF16) store_elts<BIGCN_BF16, V>(static_cast<__nv_bfloat16*>(base) + at, count, whole, v);
+    else store_elts<BIGCN_F16, V>(static_cast<__half*>(base) + at, count, whole, v);
+}
+
+// Whether rows of `ld` elements from `base` on can be moved in words of V elements.
+inline bool rows_whole(const void* base, int64_t ld, int type, int V)
+{
+    const int64_t bytes = (int64_t)V * type_bytes(type), word = bytes < 16 ? bytes : 16;
+    return reinterpret_cast<uintptr_t>(base) % word == 0 && ld * type_bytes(type) % word == 0;
+}
+
+}  // namespace dense
+}  // namespace bigcn

@@ -1,0 +1,206 @@
+// Rows in 8-bit integers and their product with 8-bit class rows.
+//
+//   s_i = max_j |x_ij| / 127,  q_ij = the integer nearest to 127 x_ij / max_j |x_ij| (halfway: the even one)
+//   out_ik = (sum_j q_ij qw_kj) s_i sw_k
+//
+// The integers are exact: the sum of 16,384 products of 127 stays below 2^31.  The three roundings of an output (the sum to fp32, and
+// two products) are fp32's, then one to the output's type.  The scales are multiplied first: a row with fp32's lowest value in it has a
+// scale of 2^121, which times the sum would overflow where the output does not.
+#include "dense_gemm.cuh"
+#include "dense_types.cuh"
+
+namespace bigcn {
+
+namespace {
+
+using namespace dense;
+
+__device__ int g_quant_timeout;               // set when a wait ran out
+
+struct QuantArgs {
+    const void* x;
+    int64_t ldx, n;
+    int d;
+    bool whole;
+    int8_t* q;
+    int64_t ldq;
+    float* scale;
+};
+
+// The nearest integer to 127 x / top.  In fp32 the quotient is off by 127 * 3 * 2^-24 at most; where that could decide the rounding, it is
+// taken in 64 bits, where 127 x is exact and a quotient halfway between integers cannot be met or missed by its rounding: with x and
+// top of 24 bits it is halfway, or at least 2^-32 of its size away from it.
+__device__ __forceinline__ int nearest(float x, float factor, float top, bool tiny)
+{
+    const float t = x * factor, r = rintf(t);
+    if (!tiny && fabsf(t - r) < 0.4999f) return (int)r;
+    return (int)rint(127.0 * (double)x / (double)top);
+}
+
+// One row to LANES threads (a warp or a block), V values at a time, NV times.
+template <int TYPE, int V, int LANES, int NV>
+__global__ void __launch_bounds__(LANES > 32 ? LANES : 256) quantize_kernel(const QuantArgs a)
+{
+    pdl_enter();
+    constexpr int B = LANES > 32 ? LANES : 256, GROUPS = B / LANES;
+    __shared__ uint32_t slot[LANES > 32 ? LANES / 32 : 1];
+    const int lane = threadIdx.x % LANES;
+    const int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES;
+    const auto* x = static_cast<const typename Elt<TYPE>::T*>(a.x) + row * a.ldx;
+    float v[NV][V];
+    uint32_t top = 0u;                        // as bits, which order magnitudes, infinity and NaN
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int c = (k * LANES + lane) * V;
+        load_elts<TYPE, V>(x + c, row < a.n ? a.d - c : 0, a.whole, v[k]);
+#pragma unroll
+        for (int i = 0; i < V; ++i) top = max(top, __float_as_uint(v[k][i]) & 0x7fffffffu);
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    if constexpr (LANES > 32) {
+        if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = top;
+        __syncthreads();
+        top = (threadIdx.x & 31) < LANES / 32 ? slot[threadIdx.x & 31] : 0u;
+        top = __reduce_max_sync(0xffffffffu, top);
+    }
+    if (row >= a.n) return;
+    const bool finite = top < 0x7f800000u;
+    const float t = __uint_as_float(top), factor = 127.f / t;
+    const bool tiny = t < 1e-30f;             // 127 / t would overflow
+    if (lane == 0) a.scale[row] = finite ? t / 127.f : __uint_as_float(0x7fc00000u);
+    int8_t* q = a.q + row * a.ldq;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int c = (k * LANES + lane) * V;
+        if (c >= a.d) break;
+        uint32_t w[V / 4];
+#pragma unroll
+        for (int j = 0; j < V / 4; ++j) {
+            w[j] = 0u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int qi = finite && top ? nearest(v[k][4 * j + i], factor, t, tiny) : 0;
+                w[j] |= ((uint32_t)qi & 255u) << (8 * i);
+            }
+        }
+        if (c + V <= a.d) {                   // rows of q start on 16-byte boundaries
+            if constexpr (V == 4) *reinterpret_cast<uint32_t*>(q + c) = w[0];
+            else *reinterpret_cast<uint2*>(q + c) = make_uint2(w[0], w[1]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (c + i < a.d) q[c + i] = (int8_t)(w[i >> 2] >> (8 * (i & 3)));
+        }
+    }
+}
+
+template <int TYPE, int V, int LANES, int NV>
+cudaError_t launch_quantize_as(cudaStream_t s, const QuantArgs& a, int* launches)
+{
+    constexpr int B = LANES > 32 ? LANES : 256;
+    ++*launches;
+    return launch_kernel(quantize_kernel<TYPE, V, LANES, NV>, dim3((unsigned)ceil_div(a.n, B / LANES)), dim3(B), 0, s, a);
+}
+template <int TYPE, int V>
+cudaError_t pick_quantize(cudaStream_t s, const QuantArgs& a, int* launches)
+{
+    constexpr int Q = 16 / V;
+    const int64_t words = ceil_div(a.d, V);
+    if (words <= 32) return launch_quantize_as<TYPE, V, 32, 1>(s, a, launches);
+    if (words <= 32 * Q) return launch_quantize_as<TYPE, V, 32, Q>(s, a, launches);
+    if (words <= 128 * Q) return launch_quantize_as<TYPE, V, 128, Q>(s, a, launches);
+    if (words <= 512 * Q) return launch_quantize_as<TYPE, V, 512, Q>(s, a, launches);
+    return launch_quantize_as<TYPE, V, 1024, Q>(s, a, launches);
+}
+
+// Epilogue: the sums times both scales, in the output's type.
+struct ScaledOut {
+    struct Args {
+        const float* s_x;
+        const float* s_w;
+        bool s_w_whole;
+        void* out;
+        int type;
+        int64_t ldo;
+        bool whole;          // rows of out on 16-byte boundaries
+    };
+    template <int BN>
+    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit& u, int row0, int rows, uint32_t acc, bool)
+    {
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        const int row = row0 + (warp & 3) * 32 + lane;
+        const float sx = row < rows ? __ldg(a.s_x + row) : 0.f;
+#pragma unroll 1
+        for (int c = 0; c < BN / 2; c += 32) {
+            const int col = u.col + (warp >> 2) * (BN / 2) + c;
+            if (col >= sh.n) break;
+            uint32_t v[32];
+            __syncwarp();
+            gemm::tmem_ld32(acc + c, v);
+            float sw[32];
+            if (a.s_w_whole && col + 32 <= sh.n) {
+#pragma unroll
+                for (int i = 0; i < 32; i += 4) {
+                    const float4 w = __ldg(reinterpret_cast<const float4*>(a.s_w + col + i));
+                    sw[i] = w.x; sw[i + 1] = w.y; sw[i + 2] = w.z; sw[i + 3] = w.w;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) sw[i] = col + i < sh.n ? __ldg(a.s_w + col + i) : 0.f;
+            }
+            gemm::tmem_wait32(v);
+            if (row < rows) {
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) {
+                    float f[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) f[j] = (float)(int)v[i + j] * (sx * sw[i + j]);
+                    store_as<8>(a.out, a.type, (int64_t)row * a.ldo + col + i, sh.n - (col + i), a.whole, f);
+                }
+            }
+        }
+    }
+};
+
+template <int BN>
+cudaError_t launch_product_as(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const int8_t* q_w, int64_t ldqw, const gemm::Shape& shape, const ScaledOut::Args& args, int* flag)
+{
+    CUtensorMap ma, mb;
+    cudaError_t e = gemm::encode_map(&ma, q_x, 1, true, shape.m, shape.k, ldqx, 128, gemm::kRows);
+    if (e == cudaSuccess) e = gemm::encode_map(&mb, q_w, 1, true, shape.n, shape.k, ldqw, 128, BN);
+    if (e != cudaSuccess) return e;
+    return gemm::launch<true, BN, 1, false, false, ScaledOut>(s, ma, mb, ma, shape, args, flag);
+}
+
+}  // namespace
+
+int quant_timeouts()
+{
+    int v = 0;
+    if (cudaMemcpyFromSymbol(&v, g_quant_timeout, sizeof(int)) != cudaSuccess) return -1;
+    return v;
+}
+
+cudaError_t launch_quantize_rows(cudaStream_t s, const void* x, int type, int64_t n, int d, int64_t ldx, int8_t* q, int64_t ldq, float* scale, int* launches)
+{
+    const QuantArgs a = {x, ldx, n, d, rows_whole(x, ldx, type, type == BIGCN_F32 ? 4 : 8), q, ldq, scale};
+    if (type == BIGCN_F32) return pick_quantize<BIGCN_F32, 4>(s, a, launches);
+    if (type == BIGCN_BF16) return pick_quantize<BIGCN_BF16, 8>(s, a, launches);
+    return pick_quantize<BIGCN_F16, 8>(s, a, launches);
+}
+
+cudaError_t launch_quantized_product(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const float* s_x, int64_t n, int d, const int8_t* q_w, int64_t ldqw,
+                                     const float* s_w, int m, void* out, int out_type, int64_t ldo, int* launches)
+{
+    int* flag = nullptr;
+    cudaError_t e = cudaGetSymbolAddress(reinterpret_cast<void**>(&flag), g_quant_timeout);
+    if (e != cudaSuccess) return e;
+    const ScaledOut::Args args = {s_x, s_w, reinterpret_cast<uintptr_t>(s_w) % 16 == 0, out, out_type, ldo, rows_whole(out, ldo, out_type, 8)};
+    const gemm::Shape shape = {(int)n, m, d, 1, nullptr, false, 0, 0};
+    ++*launches;
+    if (m <= 64) return launch_product_as<64>(s, q_x, ldqx, q_w, ldqw, shape, args, flag);
+    if (m <= 128) return launch_product_as<128>(s, q_x, ldqx, q_w, ldqw, shape, args, flag);
+    return launch_product_as<256>(s, q_x, ldqx, q_w, ldqw, shape, args, flag);
+}
+
+}  // namespace bigcn

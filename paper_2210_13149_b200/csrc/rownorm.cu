@@ -1,0 +1,439 @@
+// Layer norm of rows and its gradients.
+//
+//   y_ij = xhat_ij gain_j + offset_j,  xhat_ij = (x_ij - mean_i) rstd_i,  rstd_i = 1 / sqrt(var_i + eps)
+//   g_x_ij = rstd_i (g_ij gain_j - a_i - xhat_ij b_i),  a_i = sum_j g_ij gain_j / d,  b_i = sum_j g_ij gain_j xhat_ij / d
+//   g_gain_j = sum_i g_ij xhat_ij,  g_offset_j = sum_i g_ij                        (g = the gradient of y)
+//
+// Both directions are bound by the bytes of the rows.  A row is held in the registers of the lanes that read it (4 to 32 lanes of a
+// warp, or a whole block for long rows), so that it is read once: the mean first, then the squares about it, which lose nothing to
+// cancellation.  The columns' sums of the backward pass ride along in registers, one pair per column a thread owns, over the rows that
+// its lanes take; blocks leave theirs in the workspace, and a second kernel adds them in 64 bits in a fixed order.
+#include <algorithm>
+
+#include "dense_types.cuh"
+
+namespace bigcn {
+
+namespace {
+
+using namespace dense;
+
+constexpr int kThreads = 256;
+
+// Sum over the LANES threads of a group; every thread gets it.  `slot`: for groups of several warps (the whole block), two sets of
+// words that calls alternate between.
+template <int LANES, int COUNT>
+__device__ __forceinline__ void group_sum(float (&v)[COUNT], float* slot)
+{
+#pragma unroll
+    for (int m = (LANES < 32 ? LANES : 32) / 2; m >= 1; m >>= 1)
+#pragma unroll
+        for (int c = 0; c < COUNT; ++c) v[c] += __shfl_xor_sync(0xffffffffu, v[c], m);
+    if constexpr (LANES > 32) {
+        constexpr int W = LANES / 32;
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        if (lane == 0)
+#pragma unroll
+            for (int c = 0; c < COUNT; ++c) slot[c * W + warp] = v[c];
+        __syncthreads();
+#pragma unroll
+        for (int c = 0; c < COUNT; ++c) {
+            float s = lane < W ? slot[c * W + lane] : 0.f;
+#pragma unroll
+            for (int m = 16; m >= 1; m >>= 1) s += __shfl_xor_sync(0xffffffffu, s, m);
+            v[c] = s;
+        }
+    }
+}
+
+struct NormArgs {
+    const void* x;
+    int64_t ldx;
+    int64_t n;
+    int d;
+    bool x_whole, y_whole;
+    const float* gain;       // nullable: 1
+    const float* offset;     // nullable: 0
+    float eps;
+    void* y;
+    int y_type;
+    int64_t ldy;
+    float* mean;
+    float* rstd;
+};
+
+template <int TYPE, int V, int LANES, int NV>
+__global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads) norm_kernel(const NormArgs a)
+{
+    pdl_enter();
+    constexpr int B = LANES > 32 ? LANES : kThreads, GROUPS = B / LANES;
+    __shared__ float slots[2][LANES > 32 ? LANES / 32 : 1];
+    const int lane = threadIdx.x % LANES;
+    const auto* x = static_cast<const typename Elt<TYPE>::T*>(a.x);
+    const float inv_d = 1.f / (float)a.d;
+    constexpr bool kHold = NV * V <= 8;          // gain and offset stay in registers over the rows
+    float gain[kHold ? NV * V : 1], offset[kHold ? NV * V : 1];
+    auto column_words = [&](const float* p, float none, int c, float (&v)[V]) {
+        if (p) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = c + i < a.d ? __ldg(p + c + i) : 0.f;
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = none;
+        }
+    };
+    if constexpr (kHold) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            float v[V];
+            column_words(a.gain, 1.f, (k * LANES + lane) * V, v);
+#pragma unroll
+            for (int i = 0; i < V; ++i) gain[k * V + i] = v[i];
+            column_words(a.offset, 0.f, (k * LANES + lane) * V, v);
+#pragma unroll
+            for (int i = 0; i < V; ++i) offset[k * V + i] = v[i];
+        }
+    }
+    const int64_t step = (int64_t)gridDim.x * GROUPS;
+    int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES;
+    const int64_t first_of_block = (int64_t)blockIdx.x * GROUPS;
+    float next[NV][V];
+    auto fetch = [&](int64_t r) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * LANES + lane) * V;
+            load_elts<TYPE, V>(x + r * a.ldx + c, r < a.n ? a.d - c : 0, a.x_whole, next[k]);
+        }
+    };
+    fetch(row);
+    for (int64_t base = first_of_block; base < a.n; base += step, row += step) {   // the same trips for all threads of a block
+        float v[NV][V], sum[1] = {0.f};
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[k][i] = next[k][i], sum[0] += next[k][i];
+        if constexpr (kHold) fetch(row + step);
+        group_sum<LANES, 1>(sum, slots[0]);
+        const float mu = sum[0] * inv_d;
+        float sq[1] = {0.f};
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                v[k][i] = (k * LANES + lane) * V + i < a.d ? v[k][i] - mu : 0.f;
+                sq[0] = fmaf(v[k][i], v[k][i], sq[0]);
+            }
+        group_sum<LANES, 1>(sq, slots[1]);
+        const float r = 1.f / sqrtf(fmaf(sq[0], inv_d, a.eps));
+        if (row < a.n) {
+            if (lane == 0) {
+                a.mean[row] = mu;
+                a.rstd[row] = r;
+            }
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int c = (k * LANES + lane) * V;
+                if (c >= a.d) break;
+                float g[V], o[V];
+                if constexpr (kHold) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) g[i] = gain[k * V + i], o[i] = offset[k * V + i];
+                } else {
+                    column_words(a.gain, 1.f, c, g);
+                    column_words(a.offset, 0.f, c, o);
+                }
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[k][i] = fmaf(v[k][i] * r, g[i], o[i]);
+                store_as<V>(a.y, a.y_type, row * a.ldy + c, a.d - c, a.y_whole, v[k]);
+            }
+        }
+        if constexpr (!kHold) fetch(row + step);
+    }
+}
+
+struct NormBackArgs {
+    const void* g;
+    int64_t ldg;
+    const void* x;
+    int64_t ldx;
+    int64_t n;
+    int d;
+    bool g_whole, x_whole, gx_whole;
+    const float* gain;
+    const float* mean;
+    const float* rstd;
+    void* gx;
+    int gx_type;
+    int64_t ldgx;
+    float* part;             // [blocks][2][d]: the columns' sums of every block (null: not wanted)
+};
+
+template <int GTYPE, int TYPE, int V, int LANES, int NV>
+__global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads) norm_backward_kernel(const NormBackArgs a)
+{
+    pdl_enter();
+    constexpr int B = LANES > 32 ? LANES : kThreads, GROUPS = B / LANES;
+    constexpr bool kHold = NV * V <= 8;
+    constexpr bool kShared = LANES >= 1024;      // no registers left for the columns' sums: each thread keeps its own in shared memory
+    extern __shared__ float dyn[];               // [2][d] for the block's sums
+    __shared__ float slots[2][LANES > 32 ? 2 * (LANES / 32) : 1];
+    const int lane = threadIdx.x % LANES;
+    const auto* x = static_cast<const typename Elt<TYPE>::T*>(a.x);
+    const auto* g = static_cast<const typename Elt<GTYPE>::T*>(a.g);
+    const float inv_d = 1.f / (float)a.d;
+    float gain[kHold ? NV * V : 1], dgain[kShared ? 1 : NV * V], doff[kShared ? 1 : NV * V];
+    if constexpr (kHold) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int c = (k * LANES + lane) * V + i;
+                gain[k * V + i] = c < a.d && a.gain ? __ldg(a.gain + c) : 1.f;
+            }
+    }
+    if constexpr (!kShared) {
+#pragma unroll
+        for (int k = 0; k < NV * V; ++k) dgain[k] = 0.f, doff[k] = 0.f;
+    } else {
+        for (int c = threadIdx.x; c < 2 * a.d; c += B) dyn[c] = 0.f;
+        __syncthreads();
+    }
+    const int64_t step = (int64_t)gridDim.x * GROUPS;
+    int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES;
+    float nx[kHold ? NV : 1][V], ng[kHold ? NV : 1][V], nmean = 0.f, nrstd = 0.f;
+    auto fetch = [&](int64_t r) {
+        if constexpr (kHold) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int c = (k * LANES + lane) * V;
+                load_elts<TYPE, V>(x + r * a.ldx + c, r < a.n ? a.d - c : 0, a.x_whole, nx[k]);
+                load_elts<GTYPE, V>(g + r * a.ldg + c, r < a.n ? a.d - c : 0, a.g_whole, ng[k]);
+            }
+        }
+        nmean = r < a.n ? __ldg(a.mean + r) : 0.f;
+        nrstd = r < a.n ? __ldg(a.rstd + r) : 0.f;
+    };
+    fetch(row);
+    for (int64_t base = (int64_t)blockIdx.x * GROUPS, trip = 0; base < a.n; base += step, row += step, ++trip) {
+        float xh[NV][V], gv[NV][V], sums[2] = {0.f, 0.f};
+        const float mu = nmean, r = nrstd;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * LANES + lane) * V;
+            if constexpr (kHold) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) xh[k][i] = nx[k][i], gv[k][i] = ng[k][i];
+            } else {
+                load_elts<TYPE, V>(x + row * a.ldx + c, row < a.n ? a.d - c : 0, a.x_whole, xh[k]);
+                load_elts<GTYPE, V>(g + row * a.ldg + c, row < a.n ? a.d - c : 0, a.g_whole, gv[k]);
+            }
+        }
+        fetch(row + step);
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * LANES + lane) * V;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const bool in = row < a.n && c + i < a.d;
+                xh[k][i] = in ? (xh[k][i] - mu) * r : 0.f;
+                const float gi = gv[k][i];                       // 0 where there is no element
+                if constexpr (kShared) {
+                    if (in) {
+                        dyn[c + i] = fmaf(gi, xh[k][i], dyn[c + i]);
+                        dyn[a.d + c + i] += gi;
+                    }
+                } else {
+                    dgain[k * V + i] = fmaf(gi, xh[k][i], dgain[k * V + i]);
+                    doff[k * V + i] += gi;
+                }
+                float w;
+                if constexpr (kHold) w = gain[k * V + i];
+                else w = in && a.gain ? __ldg(a.gain + c + i) : 1.f;
+                gv[k][i] = gi * w;
+                sums[0] += gv[k][i];
+                sums[1] = fmaf(gv[k][i], xh[k][i], sums[1]);
+            }
+        }
+        group_sum<LANES, 2>(sums, slots[trip & 1]);
+        if (row < a.n) {
+            const float sa = sums[0] * inv_d, sb = sums[1] * inv_d;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int c = (k * LANES + lane) * V;
+                if (c >= a.d) break;
+#pragma unroll
+                for (int i = 0; i < V; ++i) gv[k][i] = (gv[k][i] - sa - xh[k][i] * sb) * r;
+                store_as<V>(a.gx, a.gx_type, row * a.ldgx + c, a.d - c, a.gx_whole, gv[k]);
+            }
+        }
+    }
+    if (!a.part) return;
+    float* out = a.part + (int64_t)blockIdx.x * 2 * a.d;
+    if constexpr (kShared) {
+        __syncthreads();
+        for (int c = threadIdx.x; c < 2 * a.d; c += B) out[c] = dyn[c];
+    } else if constexpr (LANES > 32) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int c = (k * LANES + lane) * V + i;
+                if (c < a.d) {
+                    out[c] = dgain[k * V + i];
+                    out[a.d + c] = doff[k * V + i];
+                }
+            }
+    } else {
+        // the groups of a warp first, then the warps one after the other
+#pragma unroll
+        for (int m = LANES; m < 32; m <<= 1)
+#pragma unroll
+            for (int k = 0; k < NV * V; ++k) {
+                dgain[k] += __shfl_xor_sync(0xffffffffu, dgain[k], m);
+                doff[k] += __shfl_xor_sync(0xffffffffu, doff[k], m);
+            }
+        for (int w = 0; w < B / 32; ++w) {
+            if ((int)(threadIdx.x >> 5) == w && (threadIdx.x & 31) < LANES) {
+#pragma unroll
+                for (int k = 0; k < NV; ++k)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const int c = (k * LANES + lane) * V + i;
+                        if (c < a.d) {
+                            dyn[c] = w ? dyn[c] + dgain[k * V + i] : dgain[k * V + i];
+                            dyn[a.d + c] = w ? dyn[a.d + c] + doff[k * V + i] : doff[k * V + i];
+                        }
+                    }
+            }
+            __syncthreads();
+        }
+        for (int c = threadIdx.x; c < 2 * a.d; c += B) out[c] = dyn[c];
+    }
+}
+
+// out[c] = sum over the parts of part[b][c], in 64 bits: 32 columns to a block, its warps take every eighth part.
+__global__ void __launch_bounds__(256) column_sums_kernel(const float* __restrict__ part, int parts, int d, float* __restrict__ g_gain, float* __restrict__ g_offset)
+{
+    pdl_enter();
+    __shared__ double s[8][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    double v = 0.0;
+    if (c < 2 * d)
+        for (int b = warp; b < parts; b += 8) v += (double)__ldg(part + (int64_t)b * 2 * d + c);
+    s[warp][lane] = v;
+    __syncthreads();
+    if (warp == 0 && c < 2 * d) {
+#pragma unroll
+        for (int w = 1; w < 8; ++w) v += s[w][lane];
+        float* out = c < d ? g_gain : g_offset;
+        if (out) out[c < d ? c : c - d] = (float)v;
+    }
+}
+
+// Blocks of the backward pass: two for every multiprocessor (a block of 256 threads and long rows fills half of it), or as many as
+// there are rows.
+constexpr int kMaxParts = 512;
+int backward_blocks(int64_t n, int groups)
+{
+    return (int)std::min<int64_t>(ceil_div(n, groups), std::min(kMaxParts, 2 * sm_count()));
+}
+
+template <int TYPE, int V, int LANES, int NV>
+cudaError_t launch_norm(cudaStream_t s, const NormArgs& a, int* launches)
+{
+    constexpr int B = LANES > 32 ? LANES : kThreads;
+    const int64_t blocks = std::min<int64_t>(ceil_div(a.n, B / LANES), (int64_t)sm_count() * (2048 / B));
+    ++*launches;
+    return launch_kernel(norm_kernel<TYPE, V, LANES, NV>, dim3((unsigned)blocks), dim3(B), 0, s, a);
+}
+
+template <int TYPE, int V>
+cudaError_t pick_norm(cudaStream_t s, const NormArgs& a, int* launches)
+{
+    const int64_t words = ceil_div(a.d, V);
+    constexpr int Q = 16 / V;                    // words per lane of the longer forms: 16 values
+    if (words <= 4) return launch_norm<TYPE, V, 4, 1>(s, a, launches);
+    if (words <= 8) return launch_norm<TYPE, V, 8, 1>(s, a, launches);
+    if (words <= 16) return launch_norm<TYPE, V, 16, 1>(s, a, launches);
+    if (words <= 32) return launch_norm<TYPE, V, 32, 1>(s, a, launches);
+    if (words <= 64) return launch_norm<TYPE, V, 32, 2>(s, a, launches);
+    if (words <= 32 * Q) return launch_norm<TYPE, V, 32, Q>(s, a, launches);
+    if (words <= 128 * Q) return launch_norm<TYPE, V, 128, Q>(s, a, launches);
+    if (words <= 256 * Q) return launch_norm<TYPE, V, 256, Q>(s, a, launches);
+    if (words <= 512 * Q) return launch_norm<TYPE, V, 512, Q>(s, a, launches);
+    return launch_norm<TYPE, V, 1024, Q>(s, a, launches);
+}
+
+template <int GTYPE, int TYPE, int V, int LANES, int NV>
+cudaError_t launch_back(cudaStream_t s, const NormBackArgs& a, float* g_gain, float* g_offset, int* launches)
+{
+    constexpr int B = LANES > 32 ? LANES : kThreads;
+    const int blocks = backward_blocks(a.n, B / LANES);
+    const size_t smem = a.part && (LANES <= 32 || LANES >= 1024) ? (size_t)2 * a.d * 4 : LANES >= 1024 ? (size_t)2 * a.d * 4 : 0;
+    auto* kernel = norm_backward_kernel<GTYPE, TYPE, V, LANES, NV>;
+    if (smem > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
+    ++*launches;
+    cudaError_t e = launch_kernel(kernel, dim3((unsigned)blocks), dim3(B), smem, s, a);
+    if (e == cudaSuccess && a.part) {
+        ++*launches;
+        e = launch_kernel(column_sums_kernel, dim3((unsigned)ceil_div(2 * a.d, 32)), dim3(256), 0, s, (const float*)a.part, blocks, a.d, g_gain, g_offset);
+    }
+    return e;
+}
+
+template <int GTYPE, int TYPE>
+cudaError_t pick_back(cudaStream_t s, const NormBackArgs& a, float* g_gain, float* g_offset, int* launches)
+{
+    constexpr int V = TYPE == BIGCN_F32 || GTYPE == BIGCN_F32 ? 4 : 8;
+    constexpr int Q = 16 / V;
+    const int64_t words = ceil_div(a.d, V);
+    if (words <= 4) return launch_back<GTYPE, TYPE, V, 4, 1>(s, a, g_gain, g_offset, launches);
+    if (words <= 8) return launch_back<GTYPE, TYPE, V, 8, 1>(s, a, g_gain, g_offset, launches);
+    if (words <= 16) return launch_back<GTYPE, TYPE, V, 16, 1>(s, a, g_gain, g_offset, launches);
+    if (words <= 32) return launch_back<GTYPE, TYPE, V, 32, 1>(s, a, g_gain, g_offset, launches);
+    if (words <= 64) return launch_back<GTYPE, TYPE, V, 32, 2>(s, a, g_gain, g_offset, launches);
+    if (words <= 32 * Q) return launch_back<GTYPE, TYPE, V, 32, Q>(s, a, g_gain, g_offset, launches);
+    if (words <= 128 * Q) return launch_back<GTYPE, TYPE, V, 128, Q>(s, a, g_gain, g_offset, launches);
+    if (words <= 256 * Q) return launch_back<GTYPE, TYPE, V, 256, Q>(s, a, g_gain, g_offset, launches);
+    if (words <= 512 * Q) return launch_back<GTYPE, TYPE, V, 512, Q>(s, a, g_gain, g_offset, launches);
+    return launch_back<GTYPE, TYPE, V, 1024, Q>(s, a, g_gain, g_offset, launches);
+}
+
+template <int GTYPE>
+cudaError_t pick_back_x(cudaStream_t s, int x_type, const NormBackArgs& a, float* g_gain, float* g_offset, int* launches)
+{
+    if (x_type == BIGCN_F32) return pick_back<GTYPE, BIGCN_F32>(s, a, g_gain, g_offset, launches);
+    if (x_type == BIGCN_BF16) return pick_back<GTYPE, BIGCN_BF16>(s, a, g_gain, g_offset, launches);
+    return pick_back<GTYPE, BIGCN_F16>(s, a, g_gain, g_offset, launches);
+}
+
+}  // namespace
+
+size_t layer_norm_scratch_bytes(int d) { return (size_t)kMaxParts * 2 * (size_t)d * sizeof(float); }
+
+cudaError_t launch_layer_norm(cudaStream_t s, const void* x, int x_type, int64_t n, int d, int64_t ldx, const float* gain, const float* offset,
+                              float eps, void* y, int y_type, int64_t ldy, float* mean, float* rstd, int* launches)
+{
+    const int V = x_type == BIGCN_F32 ? 4 : 8;
+    const NormArgs a = {x, ldx, n, d, rows_whole(x, ldx, x_type, V), rows_whole(y, ldy, y_type, V), gain, offset, eps, y, y_type, ldy, mean, rstd};
+    if (x_type == BIGCN_F32) return pick_norm<BIGCN_F32, 4>(s, a, launches);
+    if (x_type == BIGCN_BF16) return pick_norm<BIGCN_BF16, 8>(s, a, launches);
+    return pick_norm<BIGCN_F16, 8>(s, a, launches);
+}
+
+cudaError_t launch_layer_norm_backward(cudaStream_t s, const void* g, int g_type, int64_t ldg, const void* x, int x_type, int64_t ldx, int64_t n, int d,
+                                       const float* gain, const float* mean, const float* rstd, void* gx, int gx_type, int64_t ldgx,
+                                       float* g_gain, float* g_offset, void* scratch, int* launches)
+{
+    const int V = x_type == BIGCN_F32 || g_type == BIGCN_F32 ? 4 : 8;
+    const NormBackArgs a = {g, ldg, x, ldx, n, d, rows_whole(g, ldg, g_type, V), rows_whole(x, ldx, x_type, V), rows_whole(gx, ldgx, gx_type, V),
+                            gain, mean, rstd, gx, gx_type, ldgx, g_gain || g_offset ? static_cast<float*>(scratch) : nullptr};
+    if (g_type == BIGCN_F32) return pick_back_x<BIGCN_F32>(s, x_type, a, g_gain, g_offset, launches);
+    if (g_type == BIGCN_BF16) return pick_back_x<BIGCN_BF16>(s, x_type, a, g_gain, g_offset, launches);
+    return pick_back_x<BIGCN_F16>(s, x_type, a, g_gain, g_offset, launches);
+}
+
+}  // namespace bigcn

@@ -388,6 +388,25 @@ bigcn_status bigcn_layer_norm_backward(bigcn_ctx* ctx, const void* g_y, int32_t 
                                        const float* rstd, void* g_x, int32_t g_x_type, int64_t ldgx, float* g_gain,
                                        float* g_offset);
 
+/* Softmax cross entropy of rows against a class matrix: z_ik = sum_j x_ij w_kj over k < classes, lse_i = log sum_k exp z_ik,
+ * loss_i = lse_i - z_i,label(i).  The logits z are never stored.  x [n x d], w [classes x d] (a row to a class) of type
+ * BIGCN_BF16, products and sums in fp32; 1 <= d <= BIGCN_MAX_D_IN; n, classes < 2^31 - 512.  labels int64 [n]: a negative
+ * one marks a row without a label, whose loss and lse are 0 and which takes no part in anything, whatever it holds; one
+ * >= classes is an error that shows as NaN in loss_i and lse_i and is otherwise a row without a label.  loss, lse fp32 [n].
+ * Needs bigcn_class_loss_workspace_bytes(n, d, classes, 0) of workspace.
+ *
+ * bigcn_class_loss_backward(): the gradients for g_loss = dL/dloss (fp32 [n]) and the lse of the forward pass,
+ *   G_ik = (exp(z_ik - lse_i) - [k = label(i)]) g_loss_i,  g_x = G w,  g_w = G^T x,
+ * g_x [n x ldgx] and g_w [classes x ldgw] in the operands' type, nullable each.  z is computed again and G held a piece of
+ * rows and classes at a time, in the operands' type; sums in fp32.  Rows without a label get zero.  The same call gives the
+ * same bits.  Needs bigcn_class_loss_workspace_bytes(n, d, classes, 1) of workspace. */
+size_t bigcn_class_loss_workspace_bytes(int64_t n, int32_t d, int32_t classes, int32_t backward);
+bigcn_status bigcn_class_loss(bigcn_ctx* ctx, const void* x, const void* w, int32_t type, int64_t n, int32_t d, int32_t classes,
+                              int64_t ldx, int64_t ldw, const int64_t* labels, float* loss, float* lse);
+bigcn_status bigcn_class_loss_backward(bigcn_ctx* ctx, const void* x, const void* w, int32_t type, int64_t n, int32_t d,
+                                       int32_t classes, int64_t ldx, int64_t ldw, const int64_t* labels, const float* lse,
+                                       const float* g_loss, void* g_x, int64_t ldgx, void* g_w, int64_t ldgw);
+
 /* Rows in 8-bit integers, each with a scale of its own: scale_i = max_j |x_ij| / 127 and q_ij the integer nearest to
  * 127 x_ij / max_j |x_ij| (exactly; halfway goes to the even one), so that x_ij is about q_ij scale_i.  A row of zeros gets
  * zeros and the scale 0; a row with a NaN or an infinity zeros and the scale NaN.  x of any bigcn_type but BIGCN_I8, 1 <= d
@@ -399,7 +418,7 @@ bigcn_status bigcn_quantize_rows(bigcn_ctx* ctx, const void* x, int32_t type, in
 /* Product of rows with class rows in 8-bit integers: out_ik = (sum_j q_ij qw_kj) s_i sw_k, k < m, the sum exact.  x of any
  * bigcn_type: BIGCN_I8 with its scales s_x [n] (rows as bigcn_quantize_rows() lays them out), or another type with s_x
  * null, which is quantised on the way.  q_w int8 [m x ldqw], s_w fp32 [m]: the class matrix by bigcn_quantize_rows().  out
- * of any type but BIGCN_I8, [n x ldo].  Serves from one row on.  n, m < 2^31.  Needs
+ * of any type but BIGCN_I8, [n x ldo].  Serves from one row on.  n, m < 2^31 - 512.  Needs
  * bigcn_quantized_product_workspace_bytes(n, d) of workspace unless x is BIGCN_I8. */
 size_t bigcn_quantized_product_workspace_bytes(int64_t n, int32_t d);
 bigcn_status bigcn_quantized_product(bigcn_ctx* ctx, const void* x, int32_t x_type, const float* s_x, int64_t n, int32_t d,

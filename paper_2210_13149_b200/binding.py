@@ -91,6 +91,9 @@ SIGNATURES = {
     "bigcn_layer_norm_workspace_bytes": (_sz, [_i32]),
     "bigcn_layer_norm_backward": (ctypes.c_int, [_vp, _vp, _i32, _i64, _vp, _i32, _i64, _i64, _i32, _vp, _vp, _vp, _vp, _i32, _i64,
                                                  _vp, _vp]),
+    "bigcn_class_loss_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32]),
+    "bigcn_class_loss": (ctypes.c_int, [_vp, _vp, _vp, _i32, _i64, _i32, _i32, _i64, _i64, _vp, _vp, _vp]),
+    "bigcn_class_loss_backward": (ctypes.c_int, [_vp, _vp, _vp, _i32, _i64, _i32, _i32, _i64, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _i64]),
     "bigcn_quantize_rows": (ctypes.c_int, [_vp, _vp, _i32, _i64, _i32, _i64, _vp, _i64, _vp]),
     "bigcn_quantized_product_workspace_bytes": (_sz, [_i64, _i32]),
     "bigcn_quantized_product": (ctypes.c_int, [_vp, _vp, _i32, _vp, _i64, _i32, _i64, _vp, _i64, _vp, _i32, _vp, _i32, _i64]),
@@ -507,6 +510,35 @@ class BiGCN:
             self.h, _ptr(g_y), TYPES[g_y.dtype], ldg, _ptr(X), TYPES[X.dtype], ldx, n, d, _ptr(gain), _ptr(mean), _ptr(rstd),
             _ptr(g_x), TYPES[out_dtype], d, _ptr(g_gain), _ptr(g_offset)))
         return g_x, g_gain, g_offset
+
+    def _class_rows(self, X: torch.Tensor, W: torch.Tensor, labels: torch.Tensor):
+        types = (torch.bfloat16,)
+        ldx = self._rows("X", X, types)
+        ldw = self._rows("W", W, types, cols=X.shape[1])
+        self._vector("labels", labels, X.shape[0], torch.int64)
+        return ldx, ldw, X.shape[0], X.shape[1], W.shape[0]
+
+    def class_loss(self, X: torch.Tensor, W: torch.Tensor, labels: torch.Tensor):
+        """Softmax cross entropy of the rows of X against the class rows of W, the logits never stored: (loss, lse) per row.
+        A negative label marks a row that takes no part."""
+        ldx, ldw, n, d, classes = self._class_rows(X, W, labels)
+        self._scratch(int(self.lib.bigcn_class_loss_workspace_bytes(n, d, classes, 0)))
+        loss, lse = self._out(n, torch.float32), self._out(n, torch.float32)
+        self._check(self.lib.bigcn_class_loss(self.h, _ptr(X), _ptr(W), TYPES[X.dtype], n, d, classes, ldx, ldw, _ptr(labels), _ptr(loss), _ptr(lse)))
+        return loss, lse
+
+    def class_loss_backward(self, X: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, lse: torch.Tensor, g_loss: torch.Tensor,
+                            want_g_x: bool = True, want_g_w: bool = True):
+        """Gradients of class_loss() for the gradient g_loss of every row's loss: (g_x or None, g_w or None)."""
+        ldx, ldw, n, d, classes = self._class_rows(X, W, labels)
+        self._vector("lse", lse, n)
+        self._vector("g_loss", g_loss, n)
+        self._scratch(int(self.lib.bigcn_class_loss_workspace_bytes(n, d, classes, 1)))
+        g_x = self._out((n, d), X.dtype) if want_g_x else None
+        g_w = self._out((classes, d), X.dtype) if want_g_w else None
+        self._check(self.lib.bigcn_class_loss_backward(self.h, _ptr(X), _ptr(W), TYPES[X.dtype], n, d, classes, ldx, ldw, _ptr(labels), _ptr(lse),
+                                                       _ptr(g_loss), _ptr(g_x), d, _ptr(g_w), d))
+        return g_x, g_w
 
     def quantize_rows(self, X: torch.Tensor):
         """Rows in 8-bit integers: (q int8 [n x d rounded up to 16], scale [n]); columns of q past d are zero."""

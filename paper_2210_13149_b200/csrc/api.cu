@@ -189,12 +189,13 @@ bigcn_status check_type(bigcn_ctx* ctx, const char* name, int32_t type)
     return BIGCN_OK;
 }
 
-// Rows of a dense operator.
+// Rows of a dense operator; counts stay far enough below 2^31 for tiles that reach past them.
+constexpr int64_t kMaxRows = (int64_t(1) << 31) - 512;
 bigcn_status check_rows(bigcn_ctx* ctx, const char* name, const void* p, int32_t type, int64_t n, int32_t d, int64_t ld)
 {
     const bigcn_status st = check_type(ctx, name, type);
     if (st != BIGCN_OK) return st;
-    if (n < 0 || n >= (int64_t(1) << 31) || d < 1 || ld < d) return fail(ctx, BIGCN_ERR_SHAPE, "%s: n=%lld d=%d ld=%lld", name, (long long)n, d, (long long)ld);
+    if (n < 0 || n >= kMaxRows || d < 1 || ld < d) return fail(ctx, BIGCN_ERR_SHAPE, "%s: n=%lld d=%d ld=%lld", name, (long long)n, d, (long long)ld);
     if (d > BIGCN_MAX_D_IN) return fail(ctx, BIGCN_ERR_UNSUPPORTED, "%s: rows of %d > %d are not supported", name, d, BIGCN_MAX_D_IN);
     if (n > 0 && !p) return fail(ctx, BIGCN_ERR_NULL, "%s is null", name);
     if (!aligned(p, type == BIGCN_F32 ? 4 : 2)) return fail(ctx, BIGCN_ERR_ALIGN, "%s is not aligned to its elements", name);
@@ -203,10 +204,23 @@ bigcn_status check_rows(bigcn_ctx* ctx, const char* name, const void* p, int32_t
 // 8-bit rows and their scales.
 bigcn_status check_quantized(bigcn_ctx* ctx, const char* name, const void* q, int64_t n, int32_t d, int64_t ldq, const float* scale)
 {
-    if (n < 0 || n >= (int64_t(1) << 31) || d < 1 || ldq < d) return fail(ctx, BIGCN_ERR_SHAPE, "%s: n=%lld d=%d ld=%lld", name, (long long)n, d, (long long)ldq);
+    if (n < 0 || n >= kMaxRows || d < 1 || ldq < d) return fail(ctx, BIGCN_ERR_SHAPE, "%s: n=%lld d=%d ld=%lld", name, (long long)n, d, (long long)ldq);
     if (d > BIGCN_MAX_D_IN) return fail(ctx, BIGCN_ERR_UNSUPPORTED, "%s: rows of %d > %d are not supported", name, d, BIGCN_MAX_D_IN);
     if (n > 0 && (!q || !scale)) return fail(ctx, BIGCN_ERR_NULL, "%s or its scales are null", name);
     if (ldq % 16 != 0 || !aligned(q, 16)) return fail(ctx, BIGCN_ERR_ALIGN, "%s: rows must start on 16-byte boundaries (ld=%lld)", name, (long long)ldq);
+    return BIGCN_OK;
+}
+
+bigcn_status check_class_loss(bigcn_ctx* ctx, const void* x, const void* w, int32_t type, int64_t n, int32_t d, int32_t classes, int64_t ldx, int64_t ldw,
+                              const int64_t* labels)
+{
+    if (type != BIGCN_BF16) return fail(ctx, BIGCN_ERR_UNSUPPORTED, "type %d: the class loss takes BIGCN_BF16", type);
+    if (classes < 1) return fail(ctx, BIGCN_ERR_SHAPE, "classes=%d must be >= 1", classes);
+    bigcn_status st = check_rows(ctx, "x", x, type, n, d, ldx);
+    if (st == BIGCN_OK) st = check_rows(ctx, "w", w, type, classes, d, ldw);
+    if (st != BIGCN_OK) return st;
+    if (n > 0 && !labels) return fail(ctx, BIGCN_ERR_NULL, "labels are null");
+    if (!aligned(labels, 8)) return fail(ctx, BIGCN_ERR_ALIGN, "labels must be 8-byte aligned");
     return BIGCN_OK;
 }
 
@@ -588,6 +602,7 @@ bigcn_status bigcn_sync_check(bigcn_ctx* ctx)
     if (backward_tc_timeouts() != 0) return fail(ctx, BIGCN_ERR_INTERNAL, "a bounded wait on the tensor cores ran out (backward kernel)");
     if (spmm_tc_timeouts() != 0) return fail(ctx, BIGCN_ERR_INTERNAL, "a bounded wait ran out (tensor-core aggregation kernel)");
     if (spmm_bits_timeouts() != 0) return fail(ctx, BIGCN_ERR_INTERNAL, "a bounded wait ran out (layer kernel on packed bits)");
+    if (class_loss_timeouts() != 0) return fail(ctx, BIGCN_ERR_INTERNAL, "a bounded wait ran out (class loss)");
     if (quant_timeouts() != 0) return fail(ctx, BIGCN_ERR_INTERNAL, "a bounded wait ran out (product of 8-bit rows)");
     return BIGCN_OK;
 }
@@ -1050,6 +1065,51 @@ bigcn_status bigcn_layer_norm_backward(bigcn_ctx* ctx, const void* g_y, int32_t 
     return BIGCN_OK;
 }
 
+size_t bigcn_class_loss_workspace_bytes(int64_t n, int32_t d, int32_t classes, int32_t backward)
+{
+    if (n < 0 || n >= kMaxRows || d < 1 || d > BIGCN_MAX_D_IN || classes < 1 || classes >= kMaxRows) return 0;
+    return class_loss_scratch_bytes(n, d, classes, backward != 0);
+}
+
+bigcn_status bigcn_class_loss(bigcn_ctx* ctx, const void* x, const void* w, int32_t type, int64_t n, int32_t d, int32_t classes,
+                              int64_t ldx, int64_t ldw, const int64_t* labels, float* loss, float* lse)
+{
+    bigcn_status st = bind_device(ctx);
+    if (st != BIGCN_OK) return st;
+    if ((st = check_class_loss(ctx, x, w, type, n, d, classes, ldx, ldw, labels)) != BIGCN_OK) return st;
+    if (n == 0) return BIGCN_OK;
+    if (!loss || !lse) return fail(ctx, BIGCN_ERR_NULL, "loss or lse is null");
+    const size_t need = class_loss_scratch_bytes(n, d, classes, false);
+    if (!ctx->ws || ctx->ws_bytes < need) return fail(ctx, BIGCN_ERR_WORKSPACE, "needs %zu bytes of workspace (bigcn_class_loss_workspace_bytes)", need);
+    cudaError_t e = launch_class_loss(ctx->stream, x, ldx, w, ldw, n, d, classes, labels, loss, lse, ctx->ws, &ctx->launches_i);
+    finish_call(ctx);
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "class loss launch");
+    return BIGCN_OK;
+}
+
+bigcn_status bigcn_class_loss_backward(bigcn_ctx* ctx, const void* x, const void* w, int32_t type, int64_t n, int32_t d,
+                                       int32_t classes, int64_t ldx, int64_t ldw, const int64_t* labels, const float* lse,
+                                       const float* g_loss, void* g_x, int64_t ldgx, void* g_w, int64_t ldgw)
+{
+    bigcn_status st = bind_device(ctx);
+    if (st != BIGCN_OK) return st;
+    if ((st = check_class_loss(ctx, x, w, type, n, d, classes, ldx, ldw, labels)) != BIGCN_OK) return st;
+    if ((g_x && ldgx < d) || (g_w && ldgw < d)) return fail(ctx, BIGCN_ERR_SHAPE, "ldgx=%lld ldgw=%lld for rows of %d", (long long)ldgx, (long long)ldgw, d);
+    if (!aligned(g_x, 2) || !aligned(g_w, 2)) return fail(ctx, BIGCN_ERR_ALIGN, "g_x or g_w is not aligned to its elements");
+    if (!g_x && !g_w) return fail(ctx, BIGCN_ERR_NULL, "neither g_x nor g_w is given: nothing to compute");
+    if (n == 0) {                                             // no rows: every sum over them is empty
+        if (g_w) BIGCN_CUDA(ctx, cudaMemset2DAsync(g_w, (size_t)ldgw * 2, 0, (size_t)d * 2, (size_t)classes, ctx->stream));
+        return BIGCN_OK;
+    }
+    if (!lse || !g_loss) return fail(ctx, BIGCN_ERR_NULL, "lse or g_loss is null");
+    const size_t need = class_loss_scratch_bytes(n, d, classes, true);
+    if (!ctx->ws || ctx->ws_bytes < need) return fail(ctx, BIGCN_ERR_WORKSPACE, "needs %zu bytes of workspace (bigcn_class_loss_workspace_bytes)", need);
+    cudaError_t e = launch_class_loss_backward(ctx->stream, x, ldx, w, ldw, n, d, classes, labels, lse, g_loss, g_x, ldgx, g_w, ldgw, ctx->ws, &ctx->launches_i);
+    finish_call(ctx);
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "class loss backward launch");
+    return BIGCN_OK;
+}
+
 bigcn_status bigcn_quantize_rows(bigcn_ctx* ctx, const void* x, int32_t type, int64_t n, int32_t d, int64_t ldx, int8_t* q,
                                  int64_t ldq, float* scale)
 {
@@ -1076,7 +1136,7 @@ bigcn_status bigcn_quantized_product(bigcn_ctx* ctx, const void* x, int32_t x_ty
 {
     bigcn_status st = bind_device(ctx);
     if (st != BIGCN_OK) return st;
-    if (m < 1) return fail(ctx, BIGCN_ERR_SHAPE, "m=%d must be >= 1", m);
+    if (m < 1 || m >= kMaxRows) return fail(ctx, BIGCN_ERR_SHAPE, "m=%d out of range", m);
     const bool ready = x_type == BIGCN_I8;
     if (ready) st = check_quantized(ctx, "x", x, n, d, ldx, s_x);
     else if (s_x) return fail(ctx, BIGCN_ERR_UNSUPPORTED, "s_x goes with BIGCN_I8 rows only");

@@ -1,0 +1,712 @@
+// Softmax cross entropy of rows against a class matrix, without storing the logits, and its gradients.
+//
+//   z_ik = sum_j x_ij w_kj,  lse_i = log sum_k exp z_ik,  loss_i = lse_i - z_i,label(i)
+//   G_ik = (exp(z_ik - lse_i) - [k = label(i)]) g_i,  g_x = G W,  g_w = G^T X            (g_i = the gradient of loss_i)
+//
+// All four products run on the tensor cores (dense_gemm.cuh).  The first leaves, for every row and half a tile of columns, the
+// maximum and the sum of exp(z - maximum); a second kernel joins them.  The backward pass computes z once more, a piece of rows and classes at a time
+// (kPieceBytes of G), turns it into G in its epilogue, and multiplies that piece into g_x and g_w; sums over pieces, and over
+// parts of a long depth, are kept in fp32 in the workspace and added in a fixed order.  G is rounded to the operands' type, the one
+// rounding besides the outputs' own: a relative error of half a step for each term of sums whose terms' errors are independent,
+// which is the size of the output's rounding.
+//
+// Rows without a label take no part: the labelled ones are listed first and, unless that is all of them, copied together, so that what
+// the others hold (NaN, infinities) reaches nothing and their work is not done.  How many there are is known on the GPU only; the
+// kernels read it there.
+#include <algorithm>
+
+#include "dense_gemm.cuh"
+#include "dense_types.cuh"
+
+namespace bigcn {
+
+namespace {
+
+using namespace dense;
+
+__device__ int g_loss_timeout;                // set when a wait ran out
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kScan = 4096;                   // labels of a block of the listing: 1024 threads, four each
+
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// ---- the labelled rows ---------------------------------------------------------------------------------------------------
+
+// Four consecutive labels of a thread: which are classes.
+__device__ __forceinline__ void read_labels(const int64_t* labels, int64_t n, int classes, int64_t at, int64_t (&v)[4], bool (&in)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[i] = at + i < n ? __ldg(labels + at + i) : -1;
+        in[i] = v[i] >= 0 && v[i] < classes;
+    }
+}
+__device__ __forceinline__ int block_sum(int v, int* slot)
+{
+    v = __reduce_add_sync(0xffffffffu, v);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = v;
+    __syncthreads();
+    return __reduce_add_sync(0xffffffffu, (threadIdx.x & 31) < (blockDim.x >> 5) ? slot[threadIdx.x & 31] : 0);
+}
+__global__ void __launch_bounds__(1024) count_labels_kernel(const int64_t* __restrict__ labels, int64_t n, int classes, int* __restrict__ counts)
+{
+    pdl_enter();
+    __shared__ int slot[32];
+    int64_t v[4];
+    bool in[4];
+    read_labels(labels, n, classes, ((int64_t)blockIdx.x * 1024 + threadIdx.x) * 4, v, in);
+    const int c = block_sum(in[0] + in[1] + in[2] + in[3], slot);
+    if (threadIdx.x == 0) counts[blockIdx.x] = c;
+}
+
+struct ListArgs {
+    const int64_t* labels;
+    int64_t n;
+    int classes;
+    const int* counts;       // of the blocks (more than one)
+    int* kept;               // [n] the labelled rows, ascending
+    int* label;              // [n] their classes
+    int* place;              // [n] of every row: where it is in `kept`, or -1
+    int* count;              // how many
+    float* loss;             // nullable: 0 (NaN for a label that is no class) for the others
+    float* lse;
+};
+__global__ void __launch_bounds__(1024) list_labels_kernel(const ListArgs a)
+{
+    pdl_enter();
+    __shared__ int slot[32];
+    int before = 0;
+    for (int b = threadIdx.x; b < (int)blockIdx.x; b += 1024) before += __ldg(a.counts + b);
+    before = gridDim.x > 1 ? block_sum(before, slot) : 0;
+    const int64_t at = ((int64_t)blockIdx.x * 1024 + threadIdx.x) * 4;
+    int64_t v[4];
+    bool in[4];
+    read_labels(a.labels, a.n, a.classes, at, v, in);
+    const int mine = in[0] + in[1] + in[2] + in[3], lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int upto = mine;
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) {
+        const int o = __shfl_up_sync(0xffffffffu, upto, m);
+        if (lane >= m) upto += o;
+    }
+    __syncthreads();
+    if (lane == 31) slot[warp] = upto;
+    __syncthreads();
+    int base = before;
+    for (int w = 0; w < warp; ++w) base += slot[w];
+    int next = base + upto - mine;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (at + i >= a.n) break;
+        a.place[at + i] = in[i] ? next : -1;
+        if (in[i]) {
+            a.kept[next] = (int)(at + i);
+            a.label[next] = (int)v[i];
+            ++next;
+        } else if (a.loss) {
+            const float none = v[i] < 0 ? 0.f : __uint_as_float(0x7fc00000u);
+            a.loss[at + i] = none;
+            a.lse[at + i] = none;
+        }
+    }
+    if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 1023) *a.count = base + upto;
+}
+
+struct GatherArgs {
+    const uint16_t* x;
+    int64_t ldx, n;
+    int d;
+    bool whole;              // rows of x on 16-byte boundaries: where all are labelled they are read where they are
+    const int* place;
+    const int* count;
+    uint16_t* to;            // [n rounded up to 128] rows of ldt (a multiple of 8)
+    int64_t ldt;
+    uint16_t* g_x;           // nullable: rows without a label become zero
+    int64_t ldgx;
+    bool g_whole;
+};
+// A warp to a row: labelled rows are copied together, the gradient of the others is zero; rows up to the next multiple of 128 are zero.
+__global__ void __launch_bounds__(256) gather_rows_kernel(const GatherArgs a)
+{
+    pdl_enter();
+    const int lane = threadIdx.x & 31;
+    const int count = __ldg(a.count);
+    const bool copy = !(a.whole && count == a.n);
+    const int64_t step = (int64_t)gridDim.x * 8;
+    const int words = (a.d + 7) / 8;
+    if (count == a.n && !copy) return;
+    for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < a.n; row += step) {
+        const int p = __ldg(a.place + row);
+        if (p >= 0) {
+            const uint16_t* from = a.x + row * a.ldx;
+            uint16_t* to = a.to + (int64_t)p * a.ldt;
+            if (a.whole) {
+                for (int w = lane; w < words; w += 32) {
+                    if (8 * w + 8 <= a.d) *reinterpret_cast<uint4*>(to + 8 * w) = __ldg(reinterpret_cast<const uint4*>(from + 8 * w));
+                    else
+                        for (int i = 8 * w; i < a.d; ++i) to[i] = __ldg(from + i);
+                }
+            } else {
+                for (int i = lane; i < a.d; i += 32) to[i] = __ldg(from + i);
+            }
+        } else if (a.g_x) {
+            uint16_t* to = a.g_x + row * a.ldgx;
+            if (a.g_whole) {
+                for (int w = lane; w < words; w += 32) {
+                    if (8 * w + 8 <= a.d) *reinterpret_cast<uint4*>(to + 8 * w) = make_uint4(0u, 0u, 0u, 0u);
+                    else
+                        for (int i = 8 * w; i < a.d; ++i) to[i] = 0;
+                }
+            } else {
+                for (int i = lane; i < a.d; i += 32) to[i] = 0;
+            }
+        }
+    }
+    const int64_t end = ((int64_t)count + 127) / 128 * 128;
+    for (int64_t row = count + (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < end; row += step)
+        for (int i = lane; i < a.d; i += 32) a.to[row * a.ldt + i] = 0;
+}
+
+// Rows copied to 16-byte boundaries (a class matrix that does not start its rows there).
+__global__ void __launch_bounds__(256) align_rows_kernel(const uint16_t* __restrict__ w, int64_t ldw, int64_t n, int d, uint16_t* __restrict__ to, int64_t ldt)
+{
+    pdl_enter();
+    const int lane = threadIdx.x & 31;
+    for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < n; row += (int64_t)gridDim.x * 8)
+        for (int i = lane; i < d; i += 32) to[row * ldt + i] = __ldg(w + row * ldw + i);
+}
+
+// ---- epilogues -----------------------------------------------------------------------------------------------------------
+
+// Maximum and sum of exp(z - maximum) of half a tile's columns, and the label's z.  An argument of exp2 is the difference times
+// log2 e: the difference first, so that the largest term is exactly 1 and a loss near 0 keeps its digits.
+struct SumExp {
+    struct Args {
+        const int* label;    // of the rows
+        float2* part;        // [2 * column tiles][rows]
+        int64_t rows;
+        float* at;           // [rows]
+    };
+    template <int BN>
+    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit& u, int row0, int rows, uint32_t acc, bool)
+    {
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = warp >> 2;
+        const int row = row0 + (warp & 3) * 32 + lane;
+        const int label = row < rows ? __ldg(a.label + row) : -1;
+        float m = -INFINITY, s = 0.f;
+#pragma unroll 1
+        for (int c = 0; c < BN / 2; c += 32) {
+            const int col = u.col + half * (BN / 2) + c;
+            if (col >= sh.n) break;
+            uint32_t v[32];
+            __syncwarp();
+            gemm::tmem_ld32(acc + c, v);
+            gemm::tmem_wait32(v);
+            if (col + 32 > sh.n) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (col + i >= sh.n) v[i] = 0xff800000u;
+            }
+            float top = m;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(v[i]));
+            const float t = top == -INFINITY ? 0.f : top;
+            float s4[4] = {s * exp2_fast((m - t) * kLog2e), 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < 32; ++i) s4[i & 3] += exp2_fast((__uint_as_float(v[i]) - t) * kLog2e);
+            s = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+            m = top;
+            if ((unsigned)(label - col) < 32u) {
+                float z = 0.f;
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (label - col == i) z = __uint_as_float(v[i]);
+                a.at[row] = z;
+            }
+        }
+        if (row < rows) a.part[(int64_t)(u.col / BN * 2 + half) * a.rows + row] = make_float2(m, s);
+    }
+};
+
+// G of a tile, rounded to the operands' type; zero past the last class and the last row, which pads the depth of what reads it.
+struct Gradient {
+    struct Args {
+        const int* kept;
+        const int* label;
+        const float* lse;    // of all rows
+        const float* g_loss;
+        int first_class;     // of the piece
+        uint16_t* g;
+        int64_t ldg;         // a multiple of 64
+    };
+    template <int BN>
+    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit& u, int row0, int rows, uint32_t acc, bool)
+    {
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = warp >> 2;
+        const int row = row0 + (warp & 3) * 32 + lane;
+        const bool there = row < rows;
+        const int source = there ? __ldg(a.kept + row) : 0;
+        const int label = there ? __ldg(a.label + row) - a.first_class : -1;
+        const float lse = there ? __ldg(a.lse + source) : 0.f, weight = there ? __ldg(a.g_loss + source) : 0.f;
+#pragma unroll 1
+        for (int c = 0; c < BN / 2; c += 32) {
+            const int col = u.col + half * (BN / 2) + c;
+            if (col >= a.ldg) break;
+            uint32_t v[32];
+            __syncwarp();
+            gemm::tmem_ld32(acc + c, v);
+            gemm::tmem_wait32(v);
+            float f[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) f[i] = exp2_fast((__uint_as_float(v[i]) - lse) * kLog2e);
+            if ((unsigned)(label - col) < 32u) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (label - col == i) f[i] -= 1.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 32; ++i) f[i] *= weight;
+            if (!there || col + 32 > sh.n) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (!there || col + i >= sh.n) f[i] = 0.f;
+            }
+            uint4* to = reinterpret_cast<uint4*>(a.g + (int64_t)row * a.ldg + col);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                to[i] = make_uint4(pack2<BIGCN_BF16>(f[8 * i], f[8 * i + 1]), pack2<BIGCN_BF16>(f[8 * i + 2], f[8 * i + 3]),
+                                   pack2<BIGCN_BF16>(f[8 * i + 4], f[8 * i + 5]), pack2<BIGCN_BF16>(f[8 * i + 6], f[8 * i + 7]));
+        }
+    }
+};
+
+// The accumulators as they are: rounded to the output, or into fp32 parts.
+struct Store {
+    struct Args {
+        const int* map;      // nullable: the output row of every row
+        uint16_t* out;       // where there are no parts
+        int64_t ldo;
+        bool whole;
+        float* part;         // [splits][rows][pitch], pitch a multiple of 8
+        int64_t pitch, split_stride;
+        bool add;            // parts: to what is there
+    };
+    template <int BN>
+    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit& u, int row0, int rows, uint32_t acc, bool empty)
+    {
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = warp >> 2;
+        const int row = row0 + (warp & 3) * 32 + lane;
+        if (empty && a.part && a.add) return;
+        const int64_t to_row = row < rows && a.map && !a.part ? __ldg(a.map + row) : row;
+#pragma unroll 1
+        for (int c = 0; c < BN / 2; c += 32) {
+            const int col = u.col + half * (BN / 2) + c;
+            if (col >= sh.n) break;
+            uint32_t v[32];
+            __syncwarp();
+            if (!empty) {
+                gemm::tmem_ld32(acc + c, v);
+                gemm::tmem_wait32(v);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = 0u;
+            }
+            if (row >= rows) continue;
+            if (a.part) {
+                float* p = a.part + u.split * a.split_stride + (int64_t)row * a.pitch + col;
+#pragma unroll
+                for (int i = 0; i < 32; i += 4) {
+                    if (col + i >= a.pitch) break;
+                    float4 f = make_float4(__uint_as_float(v[i]), __uint_as_float(v[i + 1]), __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
+                    if (a.add) {
+                        const float4 o = *reinterpret_cast<const float4*>(p + i);
+                        f.x += o.x; f.y += o.y; f.z += o.z; f.w += o.w;
+                    }
+                    *reinterpret_cast<float4*>(p + i) = f;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) {
+                    float f[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(v[i + j]);
+                    store_elts<BIGCN_BF16, 8>(reinterpret_cast<__nv_bfloat16*>(a.out) + to_row * a.ldo + col + i, sh.n - (col + i), a.whole, f);
+                }
+            }
+        }
+    }
+};
+
+// ---- joining the parts -----------------------------------------------------------------------------------------------------
+
+// 256 threads to kRows rows: the parts of a row are shared among 256 / kRows threads.
+template <int kRows>
+__global__ void __launch_bounds__(256) join_loss_kernel(const float2* __restrict__ part, int parts, int64_t pitch, const int* __restrict__ count, int base, int rows,
+                                                        const int* __restrict__ kept, const float* __restrict__ at, float* __restrict__ loss, float* __restrict__ lse)
+{
+    pdl_enter();
+    constexpr int kSlices = 256 / kRows;
+    __shared__ float ms[kSlices][kRows], ss[kSlices][kRows];
+    const int r = threadIdx.x % kRows, slice = threadIdx.x / kRows;
+    const int there = min(rows, __ldg(count) - base);
+    for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < there; row0 += (int64_t)gridDim.x * kRows) {
+        const int64_t row = row0 + r;
+        float m = -INFINITY, s = 0.f;
+        if (row < there) {
+            for (int p = slice; p < parts; p += kSlices) {
+                const float2 q = __ldg(part + (int64_t)p * pitch + row);
+                const float top = fmaxf(m, q.x), t = top == -INFINITY ? 0.f : top;
+                s = s * exp2_fast((m - t) * kLog2e) + q.y * exp2_fast((q.x - t) * kLog2e);
+                m = top;
+            }
+        }
+        __syncthreads();
+        ms[slice][r] = m;
+        ss[slice][r] = s;
+        __syncthreads();
+        if (slice == 0 && row < there) {
+            float top = -INFINITY, sum = 0.f;
+#pragma unroll 4
+            for (int i = 0; i < kSlices; ++i) top = fmaxf(top, ms[i][r]);
+            const float t = top == -INFINITY ? 0.f : top;
+#pragma unroll 4
+            for (int i = 0; i < kSlices; ++i) sum += ss[i][r] * exp2_fast((ms[i][r] - t) * kLog2e);
+            const float l = logf(sum);
+            const int to = kept[base + row];
+            loss[to] = (top - at[row]) + l;
+            lse[to] = top + l;
+        }
+        __syncthreads();
+    }
+}
+
+struct FinishArgs {
+    const float* part;
+    int splits;
+    int64_t split_stride, pitch;
+    const int* count;        // nullable
+    int base;
+    int64_t rows;
+    int d;
+    const int* map;          // nullable
+    uint16_t* out;
+    int64_t ldo;
+    bool whole;
+};
+// The parts of a gradient, added in order and rounded: eight columns to a thread.
+__global__ void __launch_bounds__(256) finish_parts_kernel(const FinishArgs a)
+{
+    pdl_enter();
+    const int64_t rows = a.count ? min(a.rows, (int64_t)max(0, __ldg(a.count) - a.base)) : a.rows;
+    const int words = (a.d + 7) / 8;
+    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < rows * words; t += (int64_t)gridDim.x * 256) {
+        const int64_t row = t / words;
+        const int c = (int)(t - row * words) * 8;
+        float f[8] = {};
+        for (int s = 0; s < a.splits; ++s) {
+            const float4* p = reinterpret_cast<const float4*>(a.part + s * a.split_stride + row * a.pitch + c);
+            const float4 u = __ldg(p), v = __ldg(p + 1);
+            f[0] += u.x; f[1] += u.y; f[2] += u.z; f[3] += u.w;
+            f[4] += v.x; f[5] += v.y; f[6] += v.z; f[7] += v.w;
+        }
+        const int64_t to = a.map ? __ldg(a.map + row) : row;
+        store_elts<BIGCN_BF16, 8>(reinterpret_cast<__nv_bfloat16*>(a.out) + to * a.ldo + c, a.d - c, a.whole, f);
+    }
+}
+
+// ---- plan ------------------------------------------------------------------------------------------------------------------
+
+constexpr int64_t kPieceBytes = int64_t(256) << 20;      // of G, and of the forward pass's parts
+constexpr size_t kAlign = 256;
+size_t up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
+
+int tile_cols(int columns) { return columns <= 64 ? 64 : columns <= 128 ? 128 : 256; }
+
+// How many parts a product's depth is split into, so that its tiles fill the machine: the fewest rounds of the 148 multiprocessors,
+// counted in whole products, of parts of at least 8 stages, where a part more must save a twentieth.
+int pick_splits(int64_t tiles, int64_t stages, int most)
+{
+    const int sms = 148;
+    int best = 1;
+    double cost = 1e30;
+    for (int s = 1; s <= most && (s == 1 || stages / s >= 8); ++s) {
+        const double c = (double)ceil_div(tiles * s, sms) / s * (1.0 + 0.02 * s / std::max<int64_t>(1, most));
+        if (c < cost * 0.95) cost = c, best = s;
+    }
+    return best;
+}
+
+struct Plan {
+    int64_t n_pad, ldt;                       // copied rows
+    int64_t rows;                             // of a piece (a multiple of 128)
+    int64_t cols;                             // classes of a piece (a multiple of 64; of 256 where there are several)
+    int row_pieces, col_pieces;
+    int bn, parts;                            // forward: column tile and parts of a row
+    int splits_x, splits_w;
+    int bn_d;                                 // column tile of the gradients' products
+    int64_t pitch;                            // of fp32 parts
+    size_t bytes;
+    // offsets
+    size_t kept, label, place, count, counts, x, w, at, part, g, px, pw;
+};
+
+Plan make_plan(int64_t n, int d, int classes, bool backward, bool align_w)
+{
+    Plan p = {};
+    p.n_pad = round_up(std::max<int64_t>(n, 1), 128);
+    p.ldt = round_up(d, 8);
+    p.bn = tile_cols(classes);
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t at = off; off += up(bytes); return at; };
+    p.count = take(sizeof(int));
+    p.counts = take((size_t)ceil_div(p.n_pad, kScan) * 4);
+    p.kept = take((size_t)p.n_pad * 4);
+    p.label = take((size_t)p.n_pad * 4);
+    p.place = take((size_t)p.n_pad * 4);
+    p.x = take((size_t)p.n_pad * p.ldt * 2);
+    if (align_w) p.w = take((size_t)classes * p.ldt * 2);
+    if (!backward) {
+        p.parts = 2 * (int)ceil_div(classes, p.bn);
+        p.rows = std::min(p.n_pad, std::max<int64_t>(2048, kPieceBytes / (8 * (int64_t)p.parts) / 128 * 128));
+        p.row_pieces = (int)ceil_div(p.n_pad, p.rows);
+        p.col_pieces = 1;
+        p.at = take((size_t)p.rows * 4);
+        p.part = take((size_t)p.rows * p.parts * 8);
+    } else {
+        const int64_t all = round_up(classes, 64);
+        p.rows = std::min(p.n_pad, std::max<int64_t>(16384, kPieceBytes / (2 * all) / 128 * 128));
+        p.cols = std::min(all, std::max<int64_t>(256, kPieceBytes / (2 * p.rows) / 256 * 256));
+        p.row_pieces = (int)ceil_div(p.n_pad, p.rows);
+        p.col_pieces = (int)ceil_div(classes, p.cols);
+        p.bn_d = tile_cols(d);
+        p.pitch = round_up(d, 8);
+        const int64_t tiles_d = ceil_div(d, p.bn_d);
+        p.splits_x = pick_splits(ceil_div(p.rows, 128) * tiles_d, p.cols / 64, 8);
+        p.splits_w = pick_splits(ceil_div(p.cols, 128) * tiles_d, p.rows / 64, 148);
+        p.g = take((size_t)p.rows * p.cols * 2);
+        if (p.splits_x > 1 || p.col_pieces > 1) p.px = take((size_t)p.splits_x * p.n_pad * p.pitch * 4);
+        if (p.splits_w > 1 || p.row_pieces > 1) p.pw = take((size_t)p.splits_w * round_up(p.cols, 128) * p.pitch * 4);
+    }
+    p.bytes = off;
+    return p;
+}
+
+struct Operands {
+    const void* x;
+    int64_t ldx;
+    bool x_whole;
+    const uint16_t* copied;
+    const void* w;
+    int64_t ldw;
+};
+
+// Lists the labelled rows, copies them together where that is needed, and lays the class matrix on 16-byte boundaries.
+cudaError_t prepare(cudaStream_t s, const Plan& p, char* ws, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n, int d, int classes,
+                    const int64_t* labels, float* loss, float* lse, void* g_x, int64_t ldgx, Operands* o, int* launches)
+{
+    int* counts = reinterpret_cast<int*>(ws + p.counts);
+    const int blocks = (int)ceil_div(n, kScan);
+    cudaError_t e = cudaSuccess;
+    if (blocks > 1) {
+        ++*launches;
+        e = launch_kernel(count_labels_kernel, dim3(blocks), dim3(1024), 0, s, labels, n, classes, counts);
+        if (e != cudaSuccess) return e;
+    }
+    const ListArgs list = {labels, n, classes, counts, reinterpret_cast<int*>(ws + p.kept), reinterpret_cast<int*>(ws + p.label),
+                           reinterpret_cast<int*>(ws + p.place), reinterpret_cast<int*>(ws + p.count), loss, lse};
+    ++*launches;
+    e = launch_kernel(list_labels_kernel, dim3(blocks), dim3(1024), 0, s, list);
+    if (e != cudaSuccess) return e;
+    *o = {x, ldx, rows_whole(x, ldx, BIGCN_BF16, 8), reinterpret_cast<const uint16_t*>(ws + p.x), w, ldw};
+    const GatherArgs gather = {static_cast<const uint16_t*>(x), ldx, n, d, o->x_whole, list.place, list.count, reinterpret_cast<uint16_t*>(ws + p.x), p.ldt,
+                               static_cast<uint16_t*>(g_x), ldgx, rows_whole(g_x, ldgx, BIGCN_BF16, 8)};
+    ++*launches;
+    e = launch_kernel(gather_rows_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(n, 8), 8 * sm_count())), dim3(256), 0, s, gather);
+    if (e != cudaSuccess) return e;
+    if (!rows_whole(w, ldw, BIGCN_BF16, 8)) {
+        ++*launches;
+        e = launch_kernel(align_rows_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(classes, 8), 8 * sm_count())), dim3(256), 0, s, static_cast<const uint16_t*>(w), ldw, (int64_t)classes, d,
+                          reinterpret_cast<uint16_t*>(ws + p.w), p.ldt);
+        o->w = ws + p.w;
+        o->ldw = p.ldt;
+    }
+    return e;
+}
+
+// Maps of the labelled rows from `first` on: the copied ones, and the rows where they are.
+cudaError_t row_maps(CUtensorMap* copied, CUtensorMap* own, const Plan& p, const Operands& o, int64_t n, int d, int64_t first, int box_cols, int box_rows)
+{
+    cudaError_t e = gemm::encode_map(copied, o.copied + first * p.ldt, 2, false, p.n_pad - first, d, p.ldt * 2, box_cols, box_rows);
+    if (e != cudaSuccess) return e;
+    if (!o.x_whole) {
+        *own = *copied;
+        return e;
+    }
+    return gemm::encode_map(own, static_cast<const uint16_t*>(o.x) + first * o.ldx, 2, false, n - first, d, o.ldx * 2, box_cols, box_rows);
+}
+
+template <int BN, class Epi>
+cudaError_t launch_logits(cudaStream_t s, const Plan& p, const Operands& o, int64_t n, int d, int classes, int64_t first_row, int64_t rows, int64_t first_class,
+                          const int* count, const typename Epi::Args& args, int* flag, int* launches)
+{
+    CUtensorMap a, b, own;
+    cudaError_t e = row_maps(&a, &own, p, o, n, d, first_row, 64, gemm::kRows);
+    if (e == cudaSuccess) e = gemm::encode_map(&b, static_cast<const uint16_t*>(o.w) + first_class * o.ldw, 2, false, classes, d, o.ldw * 2, 64, BN);
+    if (e != cudaSuccess) return e;
+    gemm::Shape sh;
+    sh.m = (int)rows;
+    sh.n = classes;
+    sh.k = d;
+    sh.count = count;
+    sh.of = (int)n;
+    sh.base = (int)first_row;
+    sh.alt_a = o.x_whole;
+    ++*launches;
+    return gemm::launch<false, BN, 1, false, false, Epi>(s, a, b, own, sh, args, flag);
+}
+template <class Epi>
+cudaError_t pick_logits(cudaStream_t s, int bn, const Plan& p, const Operands& o, int64_t n, int d, int classes, int64_t first_row, int64_t rows, int64_t first_class,
+                        const int* count, const typename Epi::Args& args, int* flag, int* launches)
+{
+    if (bn == 64) return launch_logits<64, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, args, flag, launches);
+    if (bn == 128) return launch_logits<128, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, args, flag, launches);
+    return launch_logits<256, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, args, flag, launches);
+}
+
+// g_x = G W (columns of W outside, its rows the depth) and g_w = G^T X.
+template <int BN>
+cudaError_t launch_gx(cudaStream_t s, const CUtensorMap& g, const CUtensorMap& w, const gemm::Shape& sh, const Store::Args& args, int* flag)
+{
+    return gemm::launch<false, BN, 1, false, true, Store>(s, g, w, w, sh, args, flag);
+}
+template <int BN>
+cudaError_t launch_gw(cudaStream_t s, const CUtensorMap& g, const CUtensorMap& x, const CUtensorMap& own, const gemm::Shape& sh, const Store::Args& args, int* flag)
+{
+    return gemm::launch<false, BN, 1, true, true, Store>(s, g, x, own, sh, args, flag);
+}
+
+}  // namespace
+
+int class_loss_timeouts()
+{
+    int v = 0;
+    if (cudaMemcpyFromSymbol(&v, g_loss_timeout, sizeof(int)) != cudaSuccess) return -1;
+    return v;
+}
+
+size_t class_loss_scratch_bytes(int64_t n, int d, int classes, bool backward) { return make_plan(n, d, classes, backward, true).bytes; }
+
+cudaError_t launch_class_loss(cudaStream_t s, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n, int d, int classes, const int64_t* labels,
+                              float* loss, float* lse, void* scratch, int* launches)
+{
+    char* ws = static_cast<char*>(scratch);
+    int* flag = nullptr;
+    cudaError_t e = cudaGetSymbolAddress(reinterpret_cast<void**>(&flag), g_loss_timeout);
+    if (e != cudaSuccess) return e;
+    const Plan p = make_plan(n, d, classes, false, true);
+    Operands o;
+    e = prepare(s, p, ws, x, ldx, w, ldw, n, d, classes, labels, loss, lse, nullptr, 0, &o, launches);
+    const int* count = reinterpret_cast<const int*>(ws + p.count);
+    const int* kept = reinterpret_cast<const int*>(ws + p.kept);
+    float* at = reinterpret_cast<float*>(ws + p.at);
+    float2* part = reinterpret_cast<float2*>(ws + p.part);
+    for (int r = 0; r < p.row_pieces && e == cudaSuccess; ++r) {
+        const int64_t first = r * p.rows, rows = std::min(p.rows, n - first);
+        if (rows <= 0) break;
+        const SumExp::Args args = {reinterpret_cast<const int*>(ws + p.label) + first, part, p.rows, at};
+        e = pick_logits<SumExp>(s, p.bn, p, o, n, d, classes, first, rows, 0, count, args, flag, launches);
+        if (e != cudaSuccess) break;
+        ++*launches;
+        const auto blocks = [&](int rows_per_block) { return dim3((unsigned)std::min<int64_t>(ceil_div(rows, rows_per_block), 16 * sm_count())); };
+        // rows side by side where there are enough of them, else threads side by side over a row's parts
+        if (p.parts <= 16) e = launch_kernel(join_loss_kernel<256>, blocks(256), dim3(256), 0, s, (const float2*)part, p.parts, p.rows, count, (int)first, (int)rows, kept, (const float*)at, loss, lse);
+        else if (rows >= 32) e = launch_kernel(join_loss_kernel<32>, blocks(32), dim3(256), 0, s, (const float2*)part, p.parts, p.rows, count, (int)first, (int)rows, kept, (const float*)at, loss, lse);
+        else e = launch_kernel(join_loss_kernel<4>, blocks(4), dim3(256), 0, s, (const float2*)part, p.parts, p.rows, count, (int)first, (int)rows, kept, (const float*)at, loss, lse);
+    }
+    return e;
+}
+
+cudaError_t launch_class_loss_backward(cudaStream_t s, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n, int d, int classes, const int64_t* labels,
+                                       const float* lse, const float* g_loss, void* g_x, int64_t ldgx, void* g_w, int64_t ldgw, void* scratch, int* launches)
+{
+    char* ws = static_cast<char*>(scratch);
+    int* flag = nullptr;
+    cudaError_t e = cudaGetSymbolAddress(reinterpret_cast<void**>(&flag), g_loss_timeout);
+    if (e != cudaSuccess) return e;
+    const Plan p = make_plan(n, d, classes, true, true);
+    Operands o;
+    e = prepare(s, p, ws, x, ldx, w, ldw, n, d, classes, labels, nullptr, nullptr, g_x, ldgx, &o, launches);
+    const int* count = reinterpret_cast<const int*>(ws + p.count);
+    const int* kept = reinterpret_cast<const int*>(ws + p.kept);
+    const int* label = reinterpret_cast<const int*>(ws + p.label);
+    uint16_t* g = reinterpret_cast<uint16_t*>(ws + p.g);
+    const bool parts_x = p.splits_x > 1 || p.col_pieces > 1, parts_w = p.splits_w > 1 || p.row_pieces > 1;
+    const unsigned finish_blocks = 8 * sm_count();
+    for (int c = 0; c < p.col_pieces && e == cudaSuccess; ++c) {
+        const int64_t first_class = c * p.cols;
+        const int here = (int)std::min<int64_t>(p.cols, classes - first_class);
+        const int64_t ldg = round_up(here, 64);
+        for (int r = 0; r < p.row_pieces && e == cudaSuccess; ++r) {
+            const int64_t first = r * p.rows, rows = std::min(p.rows, n - first);
+            if (rows <= 0) break;
+            const Gradient::Args ga = {kept + first, label + first, lse, g_loss, (int)first_class, g, ldg};
+            e = pick_logits<Gradient>(s, tile_cols(here), p, o, n, d, here, first, rows, first_class, count, ga, flag, launches);
+            if (e != cudaSuccess) break;
+            gemm::Shape sh;
+            sh.n = d;
+            sh.count = count;
+            sh.of = (int)n;
+            sh.base = (int)first;
+            if (g_x) {
+                CUtensorMap mg, mw;
+                e = gemm::encode_map(&mg, g, 2, false, round_up(rows, 128), ldg, ldg * 2, 64, gemm::kRows);
+                if (e == cudaSuccess) e = gemm::encode_map(&mw, static_cast<const uint16_t*>(o.w) + first_class * o.ldw, 2, false, here, d, o.ldw * 2, 64, 64);
+                if (e != cudaSuccess) break;
+                sh.m = (int)rows;
+                sh.k = here;
+                sh.splits = p.splits_x;
+                const Store::Args args = {kept + first, static_cast<uint16_t*>(g_x), ldgx, rows_whole(g_x, ldgx, BIGCN_BF16, 8),
+                                          parts_x ? reinterpret_cast<float*>(ws + p.px) + first * p.pitch : nullptr, p.pitch, p.n_pad * p.pitch, c > 0};
+                ++*launches;
+                e = p.bn_d == 64 ? launch_gx<64>(s, mg, mw, sh, args, flag) : p.bn_d == 128 ? launch_gx<128>(s, mg, mw, sh, args, flag) : launch_gx<256>(s, mg, mw, sh, args, flag);
+                if (e == cudaSuccess && parts_x && c == p.col_pieces - 1) {
+                    const FinishArgs fa = {args.part, p.splits_x, args.split_stride, p.pitch, count, (int)first, rows, d, kept + first, static_cast<uint16_t*>(g_x), ldgx, args.whole};
+                    ++*launches;
+                    e = launch_kernel(finish_parts_kernel, dim3((unsigned)std::min<int64_t>(finish_blocks, ceil_div(rows * ceil_div(d, 8), 256))), dim3(256), 0, s, fa);
+                }
+                if (e != cudaSuccess) break;
+            }
+            if (g_w) {
+                CUtensorMap mg, mx, own;
+                e = gemm::encode_map(&mg, g, 2, false, round_up(rows, 128), ldg, ldg * 2, 64, 64);
+                if (e == cudaSuccess) e = row_maps(&mx, &own, p, o, n, d, first, 64, 64);
+                if (e != cudaSuccess) break;
+                sh.m = here;
+                sh.k = (int)rows;
+                sh.splits = p.splits_w;
+                sh.over_depth = true;
+                sh.alt_b = o.x_whole;
+                uint16_t* out = static_cast<uint16_t*>(g_w) + first_class * ldgw;
+                const Store::Args args = {nullptr, out, ldgw, rows_whole(out, ldgw, BIGCN_BF16, 8), parts_w ? reinterpret_cast<float*>(ws + p.pw) : nullptr, p.pitch,
+                                          round_up(p.cols, 128) * p.pitch, r > 0};
+                ++*launches;
+                e = p.bn_d == 64 ? launch_gw<64>(s, mg, mx, own, sh, args, flag) : p.bn_d == 128 ? launch_gw<128>(s, mg, mx, own, sh, args, flag) : launch_gw<256>(s, mg, mx, own, sh, args, flag);
+                if (e == cudaSuccess && parts_w && r == p.row_pieces - 1) {
+                    const FinishArgs fa = {args.part, p.splits_w, args.split_stride, p.pitch, nullptr, 0, here, d, nullptr, out, ldgw, args.whole};
+                    ++*launches;
+                    e = launch_kernel(finish_parts_kernel, dim3((unsigned)std::min<int64_t>(finish_blocks, ceil_div((int64_t)here * ceil_div(d, 8), 256))), dim3(256), 0, s, fa);
+                }
+            }
+        }
+    }
+    return e;
+}
+
+}  // namespace bigcn

@@ -29,14 +29,16 @@ constexpr int kDepthBytes = 128;              // depth of a stage
 constexpr int kTries = 1 << 22;               // bound of every wait, in tries of up to about a microsecond
 constexpr int kMaxStages = 8;
 
-// Sizes of a product.  `count`, where given, holds at run time how many of the rows (or, with over_depth, of the depth) there are
-// (at most the m or k given here); A is read through the second map where that is all of them.
+// Sizes of a product.  `count`, where given, holds at run time how many rows (or, with over_depth, steps of depth) the whole matrix
+// has of at most `of`; this product's begin at `base` of it, so that it has at most m (or k) and at least none.  Where nothing was left
+// out, an operand marked alt is read through the second map.
 struct Shape {
     int m, n, k;             // rows, columns, depth (elements)
-    int splits;              // of the depth
-    const int* count;
-    bool over_depth;
-    int alt_a, alt_b;        // 1: the second map is this operand's where *count says that nothing was left out
+    int splits = 1;          // of the depth
+    int half = 0;            // 16-bit operands: 1 for fp16, 0 for bf16
+    const int* count = nullptr;
+    int of = 0, base = 0;
+    bool over_depth = false, alt_a = false, alt_b = false;
 };
 
 struct Unit {
@@ -54,7 +56,7 @@ struct Walk {
     {
         int mm = s.m, kk = s.k;
         if (s.count) {
-            const int c = *s.count;
+            const int c = max(0, *s.count - s.base);
             if (s.over_depth) kk = min(kk, c); else mm = min(mm, c);
         }
         m = mm;
@@ -239,7 +241,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 
     if (warp == kProducer) {
         if (lane == 0) {
-            const bool whole = shape.count && *shape.count >= (shape.over_depth ? shape.k : shape.m);
+            const bool whole = shape.count && *shape.count >= shape.of;
             const CUtensorMap* ma = whole && shape.alt_a ? &map_alt : &map_a;
             const CUtensorMap* mb = whole && shape.alt_b ? &map_alt : &map_b;
             int slot = 0;
@@ -288,7 +290,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         __syncwarp();
     } else if (warp == kIssuer) {
         if (lane == 0 && rank == 0) {
-            constexpr uint32_t idesc = (I8 ? 2u : 1u) << 4 | 1u << 7 | 1u << 10 | (A_MN ? 1u : 0u) << 15 | (B_MN ? 1u : 0u) << 16 |
+            const uint32_t fmt = I8 || !shape.half ? 1u : 0u;
+            const uint32_t idesc = (I8 ? 2u : 1u) << 4 | fmt << 7 | fmt << 10 | (A_MN ? 1u : 0u) << 15 | (B_MN ? 1u : 0u) << 16 |
                                        (uint32_t)(BN >> 3) << 17 | (uint32_t)((kRows * CTAS) >> 4) << 24;
             constexpr uint32_t step_a = A_MN ? 2048 >> 4 : 32 >> 4, step_b = B_MN ? 2048 >> 4 : 32 >> 4;
             int slot = 0, buf = 0;

@@ -196,7 +196,10 @@ cudaError_t launch_quantized_product(cudaStream_t s, const int8_t* q_x, int64_t 
     cudaError_t e = cudaGetSymbolAddress(reinterpret_cast<void**>(&flag), g_quant_timeout);
     if (e != cudaSuccess) return e;
     const ScaledOut::Args args = {s_x, s_w, reinterpret_cast<uintptr_t>(s_w) % 16 == 0, out, out_type, ldo, rows_whole(out, ldo, out_type, 8)};
-    const gemm::Shape shape = {(int)n, m, d, 1, nullptr, false, 0, 0};
+    gemm::Shape shape;
+    shape.m = (int)n;
+    shape.n = m;
+    shape.k = d;
     ++*launches;
     if (m <= 64) return launch_product_as<64>(s, q_x, ldqx, q_w, ldqw, shape, args, flag);
     if (m <= 128) return launch_product_as<128>(s, q_x, ldqx, q_w, ldqw, shape, args, flag);

@@ -552,13 +552,13 @@ cudaError_t row_maps(CUtensorMap* copied, CUtensorMap* own, const Plan& p, const
     return gemm::encode_map(own, static_cast<const uint16_t*>(o.x) + first * o.ldx, 2, false, n - first, d, o.ldx * 2, box_cols, box_rows);
 }
 
-template <int BN, class Epi>
+template <int BN, int CTAS, class Epi>
 cudaError_t launch_logits(cudaStream_t s, const Plan& p, const Operands& o, int64_t n, int d, int classes, int64_t first_row, int64_t rows, int64_t first_class,
                           const int* count, const typename Epi::Args& args, int* flag, int* launches)
 {
     CUtensorMap a, b, own;
     cudaError_t e = row_maps(&a, &own, p, o, n, d, first_row, 64, gemm::kRows);
-    if (e == cudaSuccess) e = gemm::encode_map(&b, static_cast<const uint16_t*>(o.w) + first_class * o.ldw, 2, false, classes, d, o.ldw * 2, 64, BN);
+    if (e == cudaSuccess) e = gemm::encode_map(&b, static_cast<const uint16_t*>(o.w) + first_class * o.ldw, 2, false, classes, d, o.ldw * 2, 64, BN / CTAS);
     if (e != cudaSuccess) return e;
     gemm::Shape sh;
     sh.m = (int)rows;
@@ -569,27 +569,26 @@ cudaError_t launch_logits(cudaStream_t s, const Plan& p, const Operands& o, int6
     sh.base = (int)first_row;
     sh.alt_a = o.x_whole;
     ++*launches;
-    return gemm::launch<false, BN, 1, false, false, Epi>(s, a, b, own, sh, args, flag);
+    return gemm::launch<false, BN, CTAS, false, false, Epi>(s, a, b, own, sh, args, flag);
 }
 template <class Epi>
 cudaError_t pick_logits(cudaStream_t s, int bn, const Plan& p, const Operands& o, int64_t n, int d, int classes, int64_t first_row, int64_t rows, int64_t first_class,
                         const int* count, const typename Epi::Args& args, int* flag, int* launches)
 {
-    if (bn == 64) return launch_logits<64, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, args, flag, launches);
-    if (bn == 128) return launch_logits<128, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, args, flag, launches);
-    return launch_logits<256, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, args, flag, launches);
+    if (bn == 64) return launch_logits<64, 1, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, args, flag, launches);
+    if (bn == 128) return launch_logits<128, 1, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, args, flag, launches);
+    if (rows > gemm::kRows) return launch_logits<256, 2, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, args, flag, launches);
+    return launch_logits<256, 1, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, args, flag, launches);
 }
 
 // g_x = G W (columns of W outside, its rows the depth) and g_w = G^T X.
-template <int BN>
-cudaError_t launch_gx(cudaStream_t s, const CUtensorMap& g, const CUtensorMap& w, const gemm::Shape& sh, const Store::Args& args, int* flag)
+template <bool A_MN>
+cudaError_t launch_gradient(cudaStream_t s, int bn, const CUtensorMap& g, const CUtensorMap& b, const CUtensorMap& own, const gemm::Shape& sh, const Store::Args& args, int* flag)
 {
-    return gemm::launch<false, BN, 1, false, true, Store>(s, g, w, w, sh, args, flag);
-}
-template <int BN>
-cudaError_t launch_gw(cudaStream_t s, const CUtensorMap& g, const CUtensorMap& x, const CUtensorMap& own, const gemm::Shape& sh, const Store::Args& args, int* flag)
-{
-    return gemm::launch<false, BN, 1, true, true, Store>(s, g, x, own, sh, args, flag);
+    if (bn == 64) return gemm::launch<false, 64, 1, A_MN, true, Store>(s, g, b, own, sh, args, flag);
+    if (bn == 128) return gemm::launch<false, 128, 1, A_MN, true, Store>(s, g, b, own, sh, args, flag);
+    if (sh.m > gemm::kRows) return gemm::launch<false, 256, 2, A_MN, true, Store>(s, g, b, own, sh, args, flag);
+    return gemm::launch<false, 256, 1, A_MN, true, Store>(s, g, b, own, sh, args, flag);
 }
 
 }  // namespace
@@ -675,7 +674,7 @@ cudaError_t launch_class_loss_backward(cudaStream_t s, const void* x, int64_t ld
                 const Store::Args args = {kept + first, static_cast<uint16_t*>(g_x), ldgx, rows_whole(g_x, ldgx, BIGCN_BF16, 8),
                                           parts_x ? reinterpret_cast<float*>(ws + p.px) + first * p.pitch : nullptr, p.pitch, p.n_pad * p.pitch, c > 0};
                 ++*launches;
-                e = p.bn_d == 64 ? launch_gx<64>(s, mg, mw, sh, args, flag) : p.bn_d == 128 ? launch_gx<128>(s, mg, mw, sh, args, flag) : launch_gx<256>(s, mg, mw, sh, args, flag);
+                e = launch_gradient<false>(s, p.bn_d, mg, mw, mw, sh, args, flag);
                 if (e == cudaSuccess && parts_x && c == p.col_pieces - 1) {
                     const FinishArgs fa = {args.part, p.splits_x, args.split_stride, p.pitch, count, (int)first, rows, d, kept + first, static_cast<uint16_t*>(g_x), ldgx, args.whole};
                     ++*launches;
@@ -697,7 +696,7 @@ cudaError_t launch_class_loss_backward(cudaStream_t s, const void* x, int64_t ld
                 const Store::Args args = {nullptr, out, ldgw, rows_whole(out, ldgw, BIGCN_BF16, 8), parts_w ? reinterpret_cast<float*>(ws + p.pw) : nullptr, p.pitch,
                                           round_up(p.cols, 128) * p.pitch, r > 0};
                 ++*launches;
-                e = p.bn_d == 64 ? launch_gw<64>(s, mg, mx, own, sh, args, flag) : p.bn_d == 128 ? launch_gw<128>(s, mg, mx, own, sh, args, flag) : launch_gw<256>(s, mg, mx, own, sh, args, flag);
+                e = launch_gradient<true>(s, p.bn_d, mg, mx, own, sh, args, flag);
                 if (e == cudaSuccess && parts_w && r == p.row_pieces - 1) {
                     const FinishArgs fa = {args.part, p.splits_w, args.split_stride, p.pitch, nullptr, 0, here, d, nullptr, out, ldgw, args.whole};
                     ++*launches;

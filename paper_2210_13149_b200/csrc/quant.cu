@@ -162,14 +162,14 @@ struct ScaledOut {
     }
 };
 
-template <int BN>
+template <int BN, int CTAS>
 cudaError_t launch_product_as(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const int8_t* q_w, int64_t ldqw, const gemm::Shape& shape, const ScaledOut::Args& args, int* flag)
 {
     CUtensorMap ma, mb;
     cudaError_t e = gemm::encode_map(&ma, q_x, 1, true, shape.m, shape.k, ldqx, 128, gemm::kRows);
-    if (e == cudaSuccess) e = gemm::encode_map(&mb, q_w, 1, true, shape.n, shape.k, ldqw, 128, BN);
+    if (e == cudaSuccess) e = gemm::encode_map(&mb, q_w, 1, true, shape.n, shape.k, ldqw, 128, BN / CTAS);
     if (e != cudaSuccess) return e;
-    return gemm::launch<true, BN, 1, false, false, ScaledOut>(s, ma, mb, ma, shape, args, flag);
+    return gemm::launch<true, BN, CTAS, false, false, ScaledOut>(s, ma, mb, ma, shape, args, flag);
 }
 
 }  // namespace
@@ -201,9 +201,10 @@ cudaError_t launch_quantized_product(cudaStream_t s, const int8_t* q_x, int64_t 
     shape.n = m;
     shape.k = d;
     ++*launches;
-    if (m <= 64) return launch_product_as<64>(s, q_x, ldqx, q_w, ldqw, shape, args, flag);
-    if (m <= 128) return launch_product_as<128>(s, q_x, ldqx, q_w, ldqw, shape, args, flag);
-    return launch_product_as<256>(s, q_x, ldqx, q_w, ldqw, shape, args, flag);
+    if (m <= 64) return launch_product_as<64, 1>(s, q_x, ldqx, q_w, ldqw, shape, args, flag);
+    if (m <= 128) return launch_product_as<128, 1>(s, q_x, ldqx, q_w, ldqw, shape, args, flag);
+    if (n > gemm::kRows) return launch_product_as<256, 2>(s, q_x, ldqx, q_w, ldqw, shape, args, flag);
+    return launch_product_as<256, 1>(s, q_x, ldqx, q_w, ldqw, shape, args, flag);
 }
 
 }  // namespace bigcn

@@ -194,44 +194,37 @@ struct SumExp {
         int64_t rows;
         float* at;           // [rows]
     };
-    template <int BN>
-    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit& u, int row0, int rows, uint32_t acc, bool)
+    template <int BN, class Done>
+    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit& u, const gemm::Part& p, const Done& done)
     {
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = warp >> 2;
-        const int row = row0 + (warp & 3) * 32 + lane;
-        const int label = row < rows ? __ldg(a.label + row) : -1;
+        const int row = p.row + (threadIdx.x & 31);
+        const int label = row < p.rows ? __ldg(a.label + row) - p.col : -1;
         float m = -INFINITY, s = 0.f;
-#pragma unroll 1
-        for (int c = 0; c < BN / 2; c += 32) {
-            const int col = u.col + half * (BN / 2) + c;
-            if (col >= sh.n) break;
-            uint32_t v[32];
-            __syncwarp();
-            gemm::tmem_ld32(acc + c, v);
-            gemm::tmem_wait32(v);
-            if (col + 32 > sh.n) {
+        gemm::each_chunk<BN>(p, sh.n, done, [&](int c, uint32_t (&v)[32]) {
+            const int left = sh.n - (p.col + c);
+            if (left < 32) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
-                    if (col + i >= sh.n) v[i] = 0xff800000u;
+                    if (i >= left) v[i] = 0xff800000u;
             }
-            float top = m;
+            float tops[4] = {m, __uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2])};
 #pragma unroll
-            for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(v[i]));
-            const float t = top == -INFINITY ? 0.f : top;
+            for (int i = 3; i < 32; ++i) tops[i & 3] = fmaxf(tops[i & 3], __uint_as_float(v[i]));
+            const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), t = top == -INFINITY ? 0.f : top;
             float s4[4] = {s * exp2_fast((m - t) * kLog2e), 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < 32; ++i) s4[i & 3] += exp2_fast((__uint_as_float(v[i]) - t) * kLog2e);
             s = (s4[0] + s4[1]) + (s4[2] + s4[3]);
             m = top;
-            if ((unsigned)(label - col) < 32u) {
+            if ((unsigned)(label - c) < 32u) {
                 float z = 0.f;
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
-                    if (label - col == i) z = __uint_as_float(v[i]);
+                    if (label - c == i) z = __uint_as_float(v[i]);
                 a.at[row] = z;
             }
-        }
-        if (row < rows) a.part[(int64_t)(u.col / BN * 2 + half) * a.rows + row] = make_float2(m, s);
+        });
+        if (row < p.rows) a.part[(int64_t)(u.col / BN * 2 + (threadIdx.x >> 7)) * a.rows + row] = make_float2(m, s);
     }
 };
 
@@ -246,44 +239,37 @@ struct Gradient {
         uint16_t* g;
         int64_t ldg;         // a multiple of 64
     };
-    template <int BN>
-    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit& u, int row0, int rows, uint32_t acc, bool)
+    template <int BN, class Done>
+    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit&, const gemm::Part& p, const Done& done)
     {
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = warp >> 2;
-        const int row = row0 + (warp & 3) * 32 + lane;
-        const bool there = row < rows;
+        const int row = p.row + (threadIdx.x & 31);
+        const bool there = row < p.rows;
         const int source = there ? __ldg(a.kept + row) : 0;
-        const int label = there ? __ldg(a.label + row) - a.first_class : -1;
+        const int label = there ? __ldg(a.label + row) - a.first_class - p.col : -1;
         const float lse = there ? __ldg(a.lse + source) : 0.f, weight = there ? __ldg(a.g_loss + source) : 0.f;
-#pragma unroll 1
-        for (int c = 0; c < BN / 2; c += 32) {
-            const int col = u.col + half * (BN / 2) + c;
-            if (col >= a.ldg) break;
-            uint32_t v[32];
-            __syncwarp();
-            gemm::tmem_ld32(acc + c, v);
-            gemm::tmem_wait32(v);
+        gemm::each_chunk<BN>(p, (int)a.ldg, done, [&](int c, uint32_t (&v)[32]) {
+            const int left = sh.n - (p.col + c);
             float f[32];
 #pragma unroll
             for (int i = 0; i < 32; ++i) f[i] = exp2_fast((__uint_as_float(v[i]) - lse) * kLog2e);
-            if ((unsigned)(label - col) < 32u) {
+            if ((unsigned)(label - c) < 32u) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
-                    if (label - col == i) f[i] -= 1.f;
+                    if (label - c == i) f[i] -= 1.f;
             }
+            uint32_t w[16];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) f[i] *= weight;
-            if (!there || col + 32 > sh.n) {
+            for (int i = 0; i < 16; ++i) w[i] = pack2<BIGCN_BF16>(f[2 * i] * weight, f[2 * i + 1] * weight);
+            if (!there || left < 32) {
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if (!there || col + i >= sh.n) f[i] = 0.f;
+                for (int i = 0; i < 16; ++i) {
+                    if (!there || 2 * i >= left) w[i] = 0u;
+                    else if (2 * i + 1 >= left) w[i] &= 0xffffu;
+                }
             }
-            uint4* to = reinterpret_cast<uint4*>(a.g + (int64_t)row * a.ldg + col);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                to[i] = make_uint4(pack2<BIGCN_BF16>(f[8 * i], f[8 * i + 1]), pack2<BIGCN_BF16>(f[8 * i + 2], f[8 * i + 3]),
-                                   pack2<BIGCN_BF16>(f[8 * i + 4], f[8 * i + 5]), pack2<BIGCN_BF16>(f[8 * i + 6], f[8 * i + 7]));
-        }
+            uint16_t* to = a.g + (int64_t)p.row * a.ldg + p.col + c;
+            gemm::write_strip(p.strip, w, [&](int r, int piece, const uint4& q) { *reinterpret_cast<uint4*>(to + r * a.ldg + 8 * piece) = q; });
+        });
     }
 };
 
@@ -298,49 +284,51 @@ struct Store {
         int64_t pitch, split_stride;
         bool add;            // parts: to what is there
     };
-    template <int BN>
-    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit& u, int row0, int rows, uint32_t acc, bool empty)
+    template <int BN, class Done>
+    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit& u, const gemm::Part& p, const Done& done)
     {
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = warp >> 2;
-        const int row = row0 + (warp & 3) * 32 + lane;
-        if (empty && a.part && a.add) return;
-        const int64_t to_row = row < rows && a.map && !a.part ? __ldg(a.map + row) : row;
-#pragma unroll 1
-        for (int c = 0; c < BN / 2; c += 32) {
-            const int col = u.col + half * (BN / 2) + c;
-            if (col >= sh.n) break;
-            uint32_t v[32];
-            __syncwarp();
-            if (!empty) {
-                gemm::tmem_ld32(acc + c, v);
-                gemm::tmem_wait32(v);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = 0u;
-            }
-            if (row >= rows) continue;
+        if (p.empty && a.part && a.add) return;
+        const int row = p.row + (threadIdx.x & 31);
+        const int mapped = row < p.rows && a.map ? __ldg(a.map + row) : row;
+        gemm::each_chunk<BN>(p, sh.n, done, [&](int c, uint32_t (&v)[32]) {
+            const int col = p.col + c;
+            uint32_t w[16];
             if (a.part) {
-                float* p = a.part + u.split * a.split_stride + (int64_t)row * a.pitch + col;
+                float* to = a.part + u.split * a.split_stride + (int64_t)p.row * a.pitch + col;
 #pragma unroll
-                for (int i = 0; i < 32; i += 4) {
-                    if (col + i >= a.pitch) break;
-                    float4 f = make_float4(__uint_as_float(v[i]), __uint_as_float(v[i + 1]), __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
-                    if (a.add) {
-                        const float4 o = *reinterpret_cast<const float4*>(p + i);
-                        f.x += o.x; f.y += o.y; f.z += o.z; f.w += o.w;
-                    }
-                    *reinterpret_cast<float4*>(p + i) = f;
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) w[i] = v[16 * h + i];
+                    gemm::write_strip(p.strip, w, [&](int r, int piece, const uint4& q) {
+                        if (p.row + r >= p.rows || col + 16 * h + 4 * piece >= a.pitch) return;
+                        float4* at = reinterpret_cast<float4*>(to + r * a.pitch + 16 * h + 4 * piece);
+                        float4 f = make_float4(__uint_as_float(q.x), __uint_as_float(q.y), __uint_as_float(q.z), __uint_as_float(q.w));
+                        if (a.add) {
+                            const float4 o = *at;
+                            f.x += o.x; f.y += o.y; f.z += o.z; f.w += o.w;
+                        }
+                        *at = f;
+                    });
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < 32; i += 8) {
-                    float f[8];
+                for (int i = 0; i < 16; ++i) w[i] = pack2<BIGCN_BF16>(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+                gemm::write_strip(p.strip, w, [&](int r, int piece, const uint4& q) {
+                    const int64_t to_row = __shfl_sync(0xffffffffu, mapped, r);
+                    const int at = col + 8 * piece;
+                    if (p.row + r >= p.rows || at >= sh.n) return;
+                    uint16_t* to = a.out + to_row * a.ldo + at;
+                    if (a.whole && at + 8 <= sh.n) {
+                        *reinterpret_cast<uint4*>(to) = q;
+                    } else {
+                        const uint16_t* e = reinterpret_cast<const uint16_t*>(&q);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(v[i + j]);
-                    store_elts<BIGCN_BF16, 8>(reinterpret_cast<__nv_bfloat16*>(a.out) + to_row * a.ldo + col + i, sh.n - (col + i), a.whole, f);
-                }
+                        for (int i = 0; i < 8; ++i)
+                            if (at + i < sh.n) to[i] = e[i];
+                    }
+                });
             }
-        }
+        });
     }
 };
 

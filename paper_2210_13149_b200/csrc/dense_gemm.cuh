@@ -28,6 +28,7 @@ constexpr int kRows = 128;                    // rows of a block's tile: the lan
 constexpr int kDepthBytes = 128;              // depth of a stage
 constexpr int kTries = 1 << 22;               // bound of every wait, in tries of up to about a microsecond
 constexpr int kMaxStages = 8;
+constexpr int kStripPitch = 80, kStripBytes = 32 * kStripPitch;      // a warp's strip of 32 rows x 64 bytes on its way out; see write_strip()
 
 // Sizes of a product.  `count`, where given, holds at run time how many rows (or, with over_depth, steps of depth) the whole matrix
 // has of at most `of`; this product's begin at `base` of it, so that it has at most m (or k) and at least none.  Where nothing was left
@@ -179,7 +180,7 @@ struct Config {
     static constexpr int kABytes = kRows * kDepthBytes, kBBytes = kBRows * kDepthBytes, kStage = kABytes + kBBytes;
     static constexpr int kFit = 196608 / kStage;
     static constexpr int kStages = kFit < kMaxStages ? kFit : kMaxStages;
-    static constexpr size_t kSmem = (size_t)kStages * kStage + 1024;
+    static constexpr size_t kSmem = (size_t)kStages * kStage + 1024 + kEpiWarps * kStripBytes;
 };
 
 struct Control {
@@ -188,11 +189,85 @@ struct Control {
     int abort;
 };
 
-// Epi: struct with Args, and
-//   static __device__ void tile(const Args&, const Shape&, const Unit&, int row0, int rows_there, uint32_t acc, bool empty)
-// run by the eight epilogue warps: warp w has lanes 32 (w & 3) .. + 31 of tensor memory (rows of the tile) and columns
-// (w >> 2) BN / 2 .. + BN / 2 - 1; `acc` is the address of its lanes and first column.  row0: first row of the block's 128;
-// rows_there: rows of the whole product.  empty: no depth, the accumulators hold nothing.
+// 32 consecutive 32-bit columns of this thread's lane; tmem_wait32() before they are used
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&v)[32])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+                   "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
+                   "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
+                   "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+                 : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_wait32(uint32_t (&v)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;\n"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+                   "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]),
+                   "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]),
+                   "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])
+                 :: "memory");
+}
+
+// What an epilogue warp works with: warp w has lanes 32 (w & 3) .. + 31 of tensor memory (rows of the tile) and columns
+// (w >> 2) BN / 2 .. + BN / 2 - 1 of it.
+struct Part {
+    int row;                 // first of the warp's 32 rows
+    int rows;                // rows of the whole product
+    int col;                 // first column
+    uint32_t acc;            // its lanes and first column
+    bool empty;              // no depth: the accumulators hold nothing, the sums are 0
+    unsigned char* strip;    // kStripBytes of shared memory
+};
+
+// body(c, v) for every 32 columns c, c + 1, .. of the warp's, as far as there are `columns`: v is the row of this lane.  The next columns are
+// read from tensor memory while body works on these; done() once all are read.
+template <int BN, class Done, class Body>
+__device__ __forceinline__ void each_chunk(const Part& p, int columns, const Done& done, const Body& body)
+{
+    constexpr int kChunks = BN / 2 / 32;
+    const int chunks = min(kChunks, (columns - p.col + 31) >> 5);
+    uint32_t v[2][32];
+    if (p.empty) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[0][i] = 0u;
+        for (int c = 0; c < chunks; ++c) body(32 * c, v[0]);
+        return;
+    }
+    __syncwarp();
+    if (chunks > 0) tmem_ld32(p.acc, v[0]);
+    else done();
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+        if (c >= chunks) break;
+        __syncwarp();
+        tmem_wait32(v[c & 1]);
+        if (c + 1 < chunks) tmem_ld32(p.acc + 32 * (c + 1), v[(c + 1) & 1]);
+        else done();
+        body(32 * c, v[c & 1]);
+    }
+}
+
+// 64 bytes of each lane's row, turned through shared memory so that four lanes hold the pieces of one row: put(r, piece, 16 bytes)
+// for eight rows at a time.  A lane's own 64 bytes of 32 rows would be 32 half-written pairs of sectors an instruction.
+template <class Put>
+__device__ __forceinline__ void write_strip(unsigned char* strip, const uint32_t (&w)[16], const Put& put)
+{
+    const int lane = threadIdx.x & 31;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(strip + lane * kStripPitch + 16 * i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = 8 * i + (lane >> 2), piece = lane & 3;
+        put(r, piece, *reinterpret_cast<const uint4*>(strip + r * kStripPitch + 16 * piece));
+    }
+}
+
+// Epi: struct with Args, and  template <int BN, class Done> static __device__ void tile(const Args&, const Shape&, const Unit&, const Part&,
+// const Done& done)  that the eight epilogue warps run; done() once the accumulators are read, unless they are empty.
 template <bool I8, int BN, int CTAS, bool A_MN, bool B_MN, class Epi>
 __global__ void __launch_bounds__(kThreads, 1)
 product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_alt,
@@ -341,14 +416,19 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 if (!__all_sync(0xffffffffu, wait(&ctl.acc_full[buf], acc_phase, abort, flag))) break;
                 tc::fence_after_sync();
             }
-            const uint32_t acc = tmem + (uint32_t)(buf * BN + (warp >> 2) * (BN / 2)) + ((uint32_t)((warp & 3) * 32) << 16);
-            Epi::template tile<BN>(args, shape, t, t.row + (int)rank * kRows, walk.m, acc, empty);
-            if (!empty) {
+            Part part;
+            part.row = t.row + (int)rank * kRows + (warp & 3) * 32;
+            part.rows = walk.m;
+            part.col = t.col + (warp >> 2) * (BN / 2);
+            part.acc = tmem + (uint32_t)(buf * BN + (warp >> 2) * (BN / 2)) + ((uint32_t)((warp & 3) * 32) << 16);
+            part.empty = empty;
+            part.strip = stages + C::kStages * C::kStage + warp * kStripBytes;
+            Epi::template tile<BN>(args, shape, t, part, [&] {
                 tc::fence_before_sync();
                 __syncwarp();
                 if (lane == 0) arrive_first<CTAS>(&ctl.acc_empty[buf]);
-                if ((buf ^= 1) == 0) acc_phase ^= 1u;
-            }
+            });
+            if (!empty && (buf ^= 1) == 0) acc_phase ^= 1u;
         }
     }
     tc::fence_before_sync();
@@ -359,27 +439,6 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         if constexpr (CTAS == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(kCols) : "memory");
         else tc::tmem_free(tmem, kCols);
     }
-}
-
-// 32 consecutive 32-bit columns of this thread's lane; tmem_wait32() before they are used
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&v)[32])
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
-                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
-                   "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
-                   "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
-                   "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
-                 : "r"(taddr) : "memory");
-}
-__device__ __forceinline__ void tmem_wait32(uint32_t (&v)[32])
-{
-    asm volatile("tcgen05.wait::ld.sync.aligned;\n"
-                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
-                   "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]),
-                   "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]),
-                   "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])
-                 :: "memory");
 }
 
 // ---- host pieces ---------------------------------------------------------------------------------------------------------

@@ -124,41 +124,59 @@ struct ScaledOut {
         int64_t ldo;
         bool whole;          // rows of out on 16-byte boundaries
     };
-    template <int BN>
-    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit& u, int row0, int rows, uint32_t acc, bool)
+    // 16 or 32 columns of a strip: 64 bytes of a row
+    template <int TYPE>
+    static __device__ __forceinline__ void write(const Args& a, const gemm::Part& p, int columns, int col, const float (&f)[32])
     {
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-        const int row = row0 + (warp & 3) * 32 + lane;
-        const float sx = row < rows ? __ldg(a.s_x + row) : 0.f;
-#pragma unroll 1
-        for (int c = 0; c < BN / 2; c += 32) {
-            const int col = u.col + (warp >> 2) * (BN / 2) + c;
-            if (col >= sh.n) break;
-            uint32_t v[32];
-            __syncwarp();
-            gemm::tmem_ld32(acc + c, v);
-            float sw[32];
+        constexpr int kElts = 16 / type_bytes(TYPE), kStrips = type_bytes(TYPE) / 2;
+        using T = typename Elt<TYPE>::T;
+#pragma unroll
+        for (int h = 0; h < kStrips; ++h) {
+            uint32_t w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                if constexpr (TYPE == BIGCN_F32) w[i] = __float_as_uint(f[16 * h + i]);
+                else w[i] = pack2<TYPE>(f[2 * i], f[2 * i + 1]);
+            }
+            gemm::write_strip(p.strip, w, [&](int r, int piece, const uint4& v) {
+                const int row = p.row + r, c = col + 16 * h + piece * kElts;
+                if (row >= p.rows || c >= columns) return;
+                T* to = static_cast<T*>(a.out) + (int64_t)row * a.ldo + c;
+                if (a.whole && c + kElts <= columns) {
+                    *reinterpret_cast<uint4*>(to) = v;
+                } else {
+                    const T* e = reinterpret_cast<const T*>(&v);
+#pragma unroll
+                    for (int i = 0; i < kElts; ++i)
+                        if (c + i < columns) to[i] = e[i];
+                }
+            });
+        }
+    }
+    template <int BN, class Done>
+    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit&, const gemm::Part& p, const Done& done)
+    {
+        const int row = p.row + (threadIdx.x & 31);
+        const float sx = row < p.rows ? __ldg(a.s_x + row) : 0.f;
+        gemm::each_chunk<BN>(p, sh.n, done, [&](int c, uint32_t (&v)[32]) {
+            const int col = p.col + c;
+            float f[32];
             if (a.s_w_whole && col + 32 <= sh.n) {
 #pragma unroll
                 for (int i = 0; i < 32; i += 4) {
                     const float4 w = __ldg(reinterpret_cast<const float4*>(a.s_w + col + i));
-                    sw[i] = w.x; sw[i + 1] = w.y; sw[i + 2] = w.z; sw[i + 3] = w.w;
+                    f[i] = w.x; f[i + 1] = w.y; f[i + 2] = w.z; f[i + 3] = w.w;
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) sw[i] = col + i < sh.n ? __ldg(a.s_w + col + i) : 0.f;
+                for (int i = 0; i < 32; ++i) f[i] = col + i < sh.n ? __ldg(a.s_w + col + i) : 0.f;
             }
-            gemm::tmem_wait32(v);
-            if (row < rows) {
 #pragma unroll
-                for (int i = 0; i < 32; i += 8) {
-                    float f[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) f[j] = (float)(int)v[i + j] * (sx * sw[i + j]);
-                    store_as<8>(a.out, a.type, (int64_t)row * a.ldo + col + i, sh.n - (col + i), a.whole, f);
-                }
-            }
-        }
+            for (int i = 0; i < 32; ++i) f[i] = (float)(int)v[i] * (sx * f[i]);
+            if (a.type == BIGCN_F32) write<BIGCN_F32>(a, p, sh.n, col, f);
+            else if (a.type == BIGCN_BF16) write<BIGCN_BF16>(a, p, sh.n, col, f);
+            else write<BIGCN_F16>(a, p, sh.n, col, f);
+        });
     }
 };
 

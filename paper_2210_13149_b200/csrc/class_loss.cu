@@ -3,7 +3,7 @@
 //   z_ik = sum_j x_ij w_kj,  lse_i = log sum_k exp z_ik,  loss_i = lse_i - z_i,label(i)
 //   G_ik = (exp(z_ik - lse_i) - [k = label(i)]) g_i,  g_x = G W,  g_w = G^T X            (g_i = the gradient of loss_i)
 //
-// All four products run on the tensor cores (dense_gemm.cuh).  The first leaves, for every row and half a tile of columns, the
+// All four products run on the tensor cores (dense_gemm.cuh).  The first leaves, for every row and tile of columns, the
 // maximum and the sum of exp(z - maximum); a second kernel joins them.  The backward pass computes z once more, a piece of rows and classes at a time
 // (kPieceBytes of G), turns it into G in its epilogue, and multiplies that piece into g_x and g_w; sums over pieces, and over
 // parts of a long depth, are kept in fp32 in the workspace and added in a fixed order.  G is rounded to the operands' type, the one
@@ -185,12 +185,13 @@ __global__ void __launch_bounds__(256) align_rows_kernel(const uint16_t* __restr
 
 // ---- epilogues -----------------------------------------------------------------------------------------------------------
 
-// Maximum and sum of exp(z - maximum) of half a tile's columns, and the label's z.  An argument of exp2 is the difference times
-// log2 e: the difference first, so that the largest term is exactly 1 and a loss near 0 keeps its digits.
+// Maximum and sum of exp(z - maximum) of a tile's columns, and the label's z.  An argument of exp2 is the difference times
+// log2 e: the difference first, so that the largest term is exactly 1 and a loss near 0 keeps its digits.  The four warps of the same rows
+// join theirs in shared memory (128 threads meet twice a tile), which leaves a quarter of the parts to write and to join.
 struct SumExp {
     struct Args {
         const int* label;    // of the rows
-        float2* part;        // [2 * column tiles][rows]
+        float2* part;        // [column tiles][rows]
         int64_t rows;
         float* at;           // [rows]
     };
@@ -224,7 +225,22 @@ struct SumExp {
                 a.at[row] = z;
             }
         });
-        if (row < p.rows) a.part[(int64_t)(u.col / BN * 2 + (threadIdx.x >> 7)) * a.rows + row] = make_float2(m, s);
+        // each warp's strip holds its own 32 pairs; those of the other three lie kStripBytes * 4 apart
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        unsigned char* const first = p.strip - (warp >> 2) * (4 * gemm::kStripBytes);
+        gemm::meet(1 + (warp & 3), 32 * gemm::kColumnParts, true);
+        if (warp >= 4) *reinterpret_cast<float2*>(p.strip + 8 * lane) = make_float2(m, s);
+        gemm::meet(1 + (warp & 3), 32 * gemm::kColumnParts, true);
+        if (warp < 4) {
+#pragma unroll
+            for (int w = 1; w < gemm::kColumnParts; ++w) {
+                const float2 q = *reinterpret_cast<const float2*>(first + w * (4 * gemm::kStripBytes) + 8 * lane);
+                const float top = fmaxf(m, q.x), t = top == -INFINITY ? 0.f : top;
+                s = s * exp2_fast((m - t) * kLog2e) + q.y * exp2_fast((q.x - t) * kLog2e);
+                m = top;
+            }
+            if (row < p.rows) a.part[(int64_t)(u.col / BN) * a.rows + row] = make_float2(m, s);
+        }
     }
 };
 
@@ -461,7 +477,7 @@ Plan make_plan(int64_t n, int d, int classes, bool backward, bool align_w)
     p.x = take((size_t)p.n_pad * p.ldt * 2);
     if (align_w) p.w = take((size_t)classes * p.ldt * 2);
     if (!backward) {
-        p.parts = 2 * (int)ceil_div(classes, p.bn);
+        p.parts = (int)ceil_div(classes, p.bn);
         p.rows = std::min(p.n_pad, std::max<int64_t>(2048, kPieceBytes / (8 * (int64_t)p.parts) / 128 * 128));
         p.row_pieces = (int)ceil_div(p.n_pad, p.rows);
         p.col_pieces = 1;

@@ -1,9 +1,9 @@
 // The dense products on the 5th-generation tensor cores: D = A B^T over operands in device memory, with an epilogue of the
 // including file's choice on the accumulators.
 //
-// One persistent block per multiprocessor, its warps in roles: eight warps of the epilogue, one that fetches tiles of 128 bytes of
-// depth by TMA into a ring of shared-memory stages (128-byte swizzle), one that issues tcgen05.mma.  Accumulators lie in tensor
-// memory twice, so that the epilogue of a tile runs beside the products of the next.  CTAS = 2: two blocks of a cluster share a tile of 256
+// One persistent block per multiprocessor, its warps in roles: 16 warps of the epilogue (four to a scheduler hide what one of
+// them waits for), one that fetches tiles of 128 bytes of depth by TMA into a ring of shared-memory stages (128-byte swizzle), one that
+// issues tcgen05.mma.  Accumulators lie in tensor memory twice, so that the epilogue of a tile runs beside the products of the next.  CTAS = 2: two blocks of a cluster share a tile of 256
 // rows; each fetches its 128 rows of A and half of B's rows, and the first one issues products over both halves, so that B
 // crosses shared memory once for 256 rows.
 //
@@ -23,12 +23,13 @@
 namespace bigcn {
 namespace gemm {
 
-constexpr int kEpiWarps = 8, kProducer = 8, kIssuer = 9, kThreads = 320;
+constexpr int kEpiWarps = 16, kProducer = 16, kIssuer = 17, kThreads = 576;
+constexpr int kColumnParts = kEpiWarps / 4;   // a tile's columns are shared among four warps for each 32 rows
 constexpr int kRows = 128;                    // rows of a block's tile: the lanes of tensor memory
 constexpr int kDepthBytes = 128;              // depth of a stage
 constexpr int kTries = 1 << 22;               // bound of every wait, in tries of up to about a microsecond
 constexpr int kMaxStages = 8;
-constexpr int kStripPitch = 80, kStripBytes = 32 * kStripPitch;      // a warp's strip of 32 rows x 64 bytes on its way out; see write_strip()
+constexpr int kStripBytes = 32 * 64;          // a warp's strip of 32 rows x 64 bytes on its way out; see write_strip()
 
 // Sizes of a product.  `count`, where given, holds at run time how many rows (or, with over_depth, steps of depth) the whole matrix
 // has of at most `of`; this product's begin at `base` of it, so that it has at most m (or k) and at least none.  Where nothing was left
@@ -153,16 +154,26 @@ __device__ __forceinline__ void product(uint32_t acc, uint64_t a, uint64_t b, ui
     else BIGCN_MMA("f16", "2");
 #undef BIGCN_MMA
 }
-// An arrival at the barrier of the cluster's first block.
+// A named barrier of `threads` threads that tells each whether all of them were ok.
+__device__ __forceinline__ bool meet(int id, int threads, bool ok)
+{
+    uint32_t all;
+    __syncwarp();
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %3, 0;\nbarrier.cta.red.and.aligned.pred q, %1, %2, p;\nselp.u32 %0, 1, 0, q;\n}\n"
+                 : "=r"(all) : "r"(id), "r"(threads), "r"(ok ? 1u : 0u) : "memory");
+    return all != 0;
+}
+// An arrival at the barrier of the cluster's first block, after reads of tensor memory (which tcgen05.fence orders); relaxed, since one that
+// released would wait for the epilogue's stores to global memory, too.
 template <int CTAS>
 __device__ __forceinline__ void arrive_first(uint64_t* bar)
 {
     if constexpr (CTAS == 2) {
         uint32_t remote;
         asm volatile("mapa.shared::cluster.u32 %0, %1, 0;\n" : "=r"(remote) : "r"(tc::smem_u32(bar)));
-        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(remote) : "memory");
+        asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(remote) : "memory");
     } else {
-        asm volatile("mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];\n" ::"r"(tc::smem_u32(bar)) : "memory");
+        asm volatile("mbarrier.arrive.relaxed.cta.shared::cta.b64 _, [%0];\n" ::"r"(tc::smem_u32(bar)) : "memory");
     }
 }
 
@@ -178,7 +189,7 @@ template <int BN, int CTAS>
 struct Config {
     static constexpr int kBRows = BN / CTAS;                     // rows of B a block holds
     static constexpr int kABytes = kRows * kDepthBytes, kBBytes = kBRows * kDepthBytes, kStage = kABytes + kBBytes;
-    static constexpr int kFit = 196608 / kStage;
+    static constexpr int kFit = (232448 - 1024 - 512 - kEpiWarps * kStripBytes) / kStage;
     static constexpr int kStages = kFit < kMaxStages ? kFit : kMaxStages;
     static constexpr size_t kSmem = (size_t)kStages * kStage + 1024 + kEpiWarps * kStripBytes;
 };
@@ -211,58 +222,57 @@ __device__ __forceinline__ void tmem_wait32(uint32_t (&v)[32])
 }
 
 // What an epilogue warp works with: warp w has lanes 32 (w & 3) .. + 31 of tensor memory (rows of the tile) and columns
-// (w >> 2) BN / 2 .. + BN / 2 - 1 of it.
+// (w >> 2) BN / 4 .. + BN / 4 - 1 of it (32 at least: in the narrowest tile the upper warps have none).
 struct Part {
     int row;                 // first of the warp's 32 rows
     int rows;                // rows of the whole product
     int col;                 // first column
     uint32_t acc;            // its lanes and first column
     bool empty;              // no depth: the accumulators hold nothing, the sums are 0
+    bool there;              // the warp has columns of the tile
     unsigned char* strip;    // kStripBytes of shared memory
 };
 
-// body(c, v) for every 32 columns c, c + 1, .. of the warp's, as far as there are `columns`: v is the row of this lane.  The next columns are
-// read from tensor memory while body works on these; done() once all are read.
+// Columns of a warp's part.
+__host__ __device__ constexpr int part_cols(int bn) { return bn / kColumnParts < 32 ? 32 : bn / kColumnParts; }
+
+// body(c, v) for every 32 columns c, c + 1, .. of the warp's, as far as there are `columns`: v is the row of this lane.  done() once all
+// are read from tensor memory.
 template <int BN, class Done, class Body>
 __device__ __forceinline__ void each_chunk(const Part& p, int columns, const Done& done, const Body& body)
 {
-    constexpr int kChunks = BN / 2 / 32;
-    const int chunks = min(kChunks, (columns - p.col + 31) >> 5);
-    uint32_t v[2][32];
-    if (p.empty) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[0][i] = 0u;
-        for (int c = 0; c < chunks; ++c) body(32 * c, v[0]);
-        return;
-    }
-    __syncwarp();
-    if (chunks > 0) tmem_ld32(p.acc, v[0]);
-    else done();
-#pragma unroll
-    for (int c = 0; c < kChunks; ++c) {
-        if (c >= chunks) break;
+    const int chunks = p.there ? max(0, min(part_cols(BN) / 32, (columns - p.col + 31) >> 5)) : 0;
+    uint32_t v[32];
+    if (!p.empty && chunks == 0) done();
+    for (int c = 0; c < chunks; ++c) {
         __syncwarp();
-        tmem_wait32(v[c & 1]);
-        if (c + 1 < chunks) tmem_ld32(p.acc + 32 * (c + 1), v[(c + 1) & 1]);
-        else done();
-        body(32 * c, v[c & 1]);
+        if (p.empty) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = 0u;
+        } else {
+            tmem_ld32(p.acc + 32 * c, v);
+            tmem_wait32(v);
+            if (c == chunks - 1) done();
+        }
+        body(32 * c, v);
     }
 }
 
 // 64 bytes of each lane's row, turned through shared memory so that four lanes hold the pieces of one row: put(r, piece, 16 bytes)
-// for eight rows at a time.  A lane's own 64 bytes of 32 rows would be 32 half-written pairs of sectors an instruction.
+// for eight rows at a time.  A lane's own 64 bytes of 32 rows would be 32 half-written pairs of sectors an instruction.  Pieces of a
+// row lie in an order that depends on the row, so that eight lanes meet eight groups of banks both ways.
 template <class Put>
 __device__ __forceinline__ void write_strip(unsigned char* strip, const uint32_t (&w)[16], const Put& put)
 {
     const int lane = threadIdx.x & 31;
     __syncwarp();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(strip + lane * kStripPitch + 16 * i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(strip + lane * 64 + 16 * (i ^ ((lane >> 1) & 3))) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int r = 8 * i + (lane >> 2), piece = lane & 3;
-        put(r, piece, *reinterpret_cast<const uint4*>(strip + r * kStripPitch + 16 * piece));
+        put(r, piece, *reinterpret_cast<const uint4*>(strip + r * 64 + 16 * (piece ^ ((r >> 1) & 3))));
     }
 }
 
@@ -413,15 +423,17 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             const Unit t = walk.at(u);
             const bool empty = t.k0 >= t.k1;
             if (!empty) {
-                if (!__all_sync(0xffffffffu, wait(&ctl.acc_full[buf], acc_phase, abort, flag))) break;
+                // the four warps of the same rows go on or give up together: an epilogue may let them meet
+                if (!meet(1 + (warp & 3), 32 * kColumnParts, wait(&ctl.acc_full[buf], acc_phase, abort, flag))) break;
                 tc::fence_after_sync();
             }
             Part part;
             part.row = t.row + (int)rank * kRows + (warp & 3) * 32;
             part.rows = walk.m;
-            part.col = t.col + (warp >> 2) * (BN / 2);
-            part.acc = tmem + (uint32_t)(buf * BN + (warp >> 2) * (BN / 2)) + ((uint32_t)((warp & 3) * 32) << 16);
+            part.col = t.col + (warp >> 2) * part_cols(BN);
+            part.acc = tmem + (uint32_t)(buf * BN + (warp >> 2) * part_cols(BN)) + ((uint32_t)((warp & 3) * 32) << 16);
             part.empty = empty;
+            part.there = (warp >> 2) * part_cols(BN) < BN;
             part.strip = stages + C::kStages * C::kStage + warp * kStripBytes;
             Epi::template tile<BN>(args, shape, t, part, [&] {
                 tc::fence_before_sync();

@@ -156,8 +156,10 @@ struct ScaledOut {
     template <int BN, class Done>
     static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit&, const gemm::Part& p, const Done& done)
     {
-        const int row = p.row + (threadIdx.x & 31);
+        const int lane = threadIdx.x & 31, row = p.row + lane;
         const float sx = row < p.rows ? __ldg(a.s_x + row) : 0.f;
+        // the warp's class scales are read by all lanes at once below: from L1 by then
+        if (lane < gemm::part_cols(BN) / 32 && p.col + 32 * lane < sh.n) asm volatile("prefetch.global.L1 [%0];\n" ::"l"(a.s_w + p.col + 32 * lane));
         gemm::each_chunk<BN>(p, sh.n, done, [&](int c, uint32_t (&v)[32]) {
             const int col = p.col + c;
             float f[32];

@@ -41,11 +41,15 @@ __device__ __forceinline__ float exp2_fast(float x)
 // Four consecutive labels of a thread: which are classes.
 __device__ __forceinline__ void read_labels(const int64_t* labels, int64_t n, int classes, int64_t at, int64_t (&v)[4], bool (&in)[4])
 {
+    if (at + 4 <= n && (reinterpret_cast<uintptr_t>(labels) & 15) == 0) {
+        const longlong2 a = __ldg(reinterpret_cast<const longlong2*>(labels + at)), b = __ldg(reinterpret_cast<const longlong2*>(labels + at) + 1);
+        v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[i] = at + i < n ? __ldg(labels + at + i) : -1;
-        in[i] = v[i] >= 0 && v[i] < classes;
+        for (int i = 0; i < 4; ++i) v[i] = at + i < n ? __ldg(labels + at + i) : -1;
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) in[i] = v[i] >= 0 && v[i] < classes;
 }
 __device__ __forceinline__ int block_sum(int v, int* slot)
 {
@@ -77,6 +81,7 @@ struct ListArgs {
     int* count;              // how many
     float* loss;             // nullable: 0 (NaN for a label that is no class) for the others
     float* lse;
+    bool words;              // both on 16-byte boundaries
 };
 __global__ void __launch_bounds__(1024) list_labels_kernel(const ListArgs a)
 {
@@ -101,19 +106,29 @@ __global__ void __launch_bounds__(1024) list_labels_kernel(const ListArgs a)
     __syncthreads();
     int base = before;
     for (int w = 0; w < warp; ++w) base += slot[w];
-    int next = base + upto - mine;
+    int next = base + upto - mine, places[4];
+    float none[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (at + i >= a.n) break;
-        a.place[at + i] = in[i] ? next : -1;
+        places[i] = in[i] ? next : -1;
+        none[i] = v[i] < 0 ? 0.f : __uint_as_float(0x7fc00000u);
         if (in[i]) {
             a.kept[next] = (int)(at + i);
             a.label[next] = (int)v[i];
             ++next;
-        } else if (a.loss) {
-            const float none = v[i] < 0 ? 0.f : __uint_as_float(0x7fc00000u);
-            a.loss[at + i] = none;
-            a.lse[at + i] = none;
+        }
+    }
+    if (at + 4 <= a.n) *reinterpret_cast<int4*>(a.place + at) = make_int4(places[0], places[1], places[2], places[3]);
+    else
+        for (int i = 0; i < 4 && at + i < a.n; ++i) a.place[at + i] = places[i];
+    if (a.loss && mine < 4) {
+        if (mine == 0 && at + 4 <= a.n && a.words) {
+            *reinterpret_cast<float4*>(a.loss + at) = make_float4(none[0], none[1], none[2], none[3]);
+            *reinterpret_cast<float4*>(a.lse + at) = make_float4(none[0], none[1], none[2], none[3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (!in[i] && at + i < a.n) a.loss[at + i] = a.lse[at + i] = none[i];
         }
     }
     if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 1023) *a.count = base + upto;
@@ -132,55 +147,61 @@ struct GatherArgs {
     int64_t ldgx;
     bool g_whole;
 };
-// A warp to a row: labelled rows are copied together, the gradient of the others is zero; rows up to the next multiple of 128 are zero.
+// A warp to 32 rows at a time, whose places its lanes read together: labelled rows are copied together, the gradient of the others is
+// zero; rows up to the next multiple of 128 are zero.
 __global__ void __launch_bounds__(256) gather_rows_kernel(const GatherArgs a)
 {
     pdl_enter();
     const int lane = threadIdx.x & 31;
     const int count = __ldg(a.count);
-    const bool copy = !(a.whole && count == a.n);
-    const int64_t step = (int64_t)gridDim.x * 8;
-    const int words = (a.d + 7) / 8;
-    if (count == a.n && !copy) return;
-    for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < a.n; row += step) {
-        const int p = __ldg(a.place + row);
-        if (p >= 0) {
-            const uint16_t* from = a.x + row * a.ldx;
-            uint16_t* to = a.to + (int64_t)p * a.ldt;
+    if (a.whole && count == a.n) return;
+    const int64_t warps = (int64_t)gridDim.x * 8, first = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int words = a.d / 8, rest = a.d - 8 * words;
+    for (int64_t row0 = first * 32; row0 < a.n; row0 += warps * 32) {
+        const int place = row0 + lane < a.n ? __ldg(a.place + row0 + lane) : -1;
+        const int rows = (int)min((int64_t)32, a.n - row0);
+        const uint32_t kept = __ballot_sync(0xffffffffu, place >= 0);
+        for (uint32_t left = kept; left != 0u; left &= left - 1) {
+            const int r = __ffs(left) - 1;
+            const uint16_t* from = a.x + (row0 + r) * a.ldx;
+            uint16_t* to = a.to + (int64_t)__shfl_sync(0xffffffffu, place, r) * a.ldt;
             if (a.whole) {
-                for (int w = lane; w < words; w += 32) {
-                    if (8 * w + 8 <= a.d) *reinterpret_cast<uint4*>(to + 8 * w) = __ldg(reinterpret_cast<const uint4*>(from + 8 * w));
-                    else
-                        for (int i = 8 * w; i < a.d; ++i) to[i] = __ldg(from + i);
-                }
+                for (int w = lane; w < words; w += 32) reinterpret_cast<uint4*>(to)[w] = __ldg(reinterpret_cast<const uint4*>(from) + w);
+                if (lane < rest) to[8 * words + lane] = __ldg(from + 8 * words + lane);
             } else {
                 for (int i = lane; i < a.d; i += 32) to[i] = __ldg(from + i);
             }
-        } else if (a.g_x) {
-            uint16_t* to = a.g_x + row * a.ldgx;
+        }
+        if (!a.g_x) continue;
+        for (uint32_t left = ~kept & (rows < 32 ? (1u << rows) - 1u : 0xffffffffu); left != 0u; left &= left - 1) {
+            uint16_t* to = a.g_x + (row0 + __ffs(left) - 1) * a.ldgx;
             if (a.g_whole) {
-                for (int w = lane; w < words; w += 32) {
-                    if (8 * w + 8 <= a.d) *reinterpret_cast<uint4*>(to + 8 * w) = make_uint4(0u, 0u, 0u, 0u);
-                    else
-                        for (int i = 8 * w; i < a.d; ++i) to[i] = 0;
-                }
+                for (int w = lane; w < words; w += 32) reinterpret_cast<uint4*>(to)[w] = make_uint4(0u, 0u, 0u, 0u);
+                if (lane < rest) to[8 * words + lane] = 0;
             } else {
                 for (int i = lane; i < a.d; i += 32) to[i] = 0;
             }
         }
     }
     const int64_t end = ((int64_t)count + 127) / 128 * 128;
-    for (int64_t row = count + (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < end; row += step)
+    for (int64_t row = count + first; row < end; row += warps)
         for (int i = lane; i < a.d; i += 32) a.to[row * a.ldt + i] = 0;
 }
 
-// Rows copied to 16-byte boundaries (a class matrix that does not start its rows there).
+// Rows copied to 16-byte boundaries (a class matrix that does not start its rows there), in words of T where the rows allow it.
+template <class T>
 __global__ void __launch_bounds__(256) align_rows_kernel(const uint16_t* __restrict__ w, int64_t ldw, int64_t n, int d, uint16_t* __restrict__ to, int64_t ldt)
 {
     pdl_enter();
-    const int lane = threadIdx.x & 31;
-    for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < n; row += (int64_t)gridDim.x * 8)
-        for (int i = lane; i < d; i += 32) to[row * ldt + i] = __ldg(w + row * ldw + i);
+    constexpr int kElts = sizeof(T) / 2;
+    const int lane = threadIdx.x & 31, words = d / kElts;
+    for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < n; row += (int64_t)gridDim.x * 8) {
+        const T* from = reinterpret_cast<const T*>(w + row * ldw);
+        T* out = reinterpret_cast<T*>(to + row * ldt);
+#pragma unroll 4
+        for (int i = lane; i < words; i += 32) out[i] = __ldg(from + i);
+        for (int i = words * kElts + lane; i < d; i += 32) to[row * ldt + i] = __ldg(w + row * ldw + i);
+    }
 }
 
 // ---- epilogues -----------------------------------------------------------------------------------------------------------
@@ -404,44 +425,77 @@ struct FinishArgs {
     int64_t ldo;
     bool whole;
 };
-// The parts of a gradient, added in order and rounded: eight columns to a thread.
+// The parts of a gradient, added in order and rounded: 8 columns to a thread, and where there are many parts of few rows, kSlices threads to
+// those, each with every kSlices-th part.
+template <int kSlices>
 __global__ void __launch_bounds__(256) finish_parts_kernel(const FinishArgs a)
 {
     pdl_enter();
+    constexpr int kItems = 256 / kSlices;
+    __shared__ float sums[kSlices > 1 ? kSlices : 1][kItems][9];
     const int64_t rows = a.count ? min(a.rows, (int64_t)max(0, __ldg(a.count) - a.base)) : a.rows;
-    const int words = (a.d + 7) / 8;
-    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < rows * words; t += (int64_t)gridDim.x * 256) {
-        const int64_t row = t / words;
+    const int words = (a.d + 7) / 8, slice = threadIdx.x / kItems, item = threadIdx.x % kItems;
+    for (int64_t base = (int64_t)blockIdx.x * kItems; base < rows * words; base += (int64_t)gridDim.x * kItems) {
+        const int64_t t = base + item, row = t / words;
         const int c = (int)(t - row * words) * 8;
+        const bool there = t < rows * words;
         float f[8] = {};
-        for (int s = 0; s < a.splits; ++s) {
-            const float4* p = reinterpret_cast<const float4*>(a.part + s * a.split_stride + row * a.pitch + c);
-            const float4 u = __ldg(p), v = __ldg(p + 1);
-            f[0] += u.x; f[1] += u.y; f[2] += u.z; f[3] += u.w;
-            f[4] += v.x; f[5] += v.y; f[6] += v.z; f[7] += v.w;
+        if (there) {
+#pragma unroll 4
+            for (int s = slice; s < a.splits; s += kSlices) {
+                const float4* p = reinterpret_cast<const float4*>(a.part + s * a.split_stride + row * a.pitch + c);
+                const float4 u = __ldg(p), v = __ldg(p + 1);
+                f[0] += u.x; f[1] += u.y; f[2] += u.z; f[3] += u.w;
+                f[4] += v.x; f[5] += v.y; f[6] += v.z; f[7] += v.w;
+            }
         }
-        const int64_t to = a.map ? __ldg(a.map + row) : row;
-        store_elts<BIGCN_BF16, 8>(reinterpret_cast<__nv_bfloat16*>(a.out) + to * a.ldo + c, a.d - c, a.whole, f);
+        if constexpr (kSlices > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sums[slice][item][i] = f[i];
+            __syncthreads();
+            if (slice == 0) {
+#pragma unroll 1
+                for (int s = 1; s < kSlices; ++s)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) f[i] += sums[s][item][i];
+            }
+        }
+        if (there && slice == 0) {
+            const int64_t to = a.map ? __ldg(a.map + row) : row;
+            store_elts<BIGCN_BF16, 8>(reinterpret_cast<__nv_bfloat16*>(a.out) + to * a.ldo + c, a.d - c, a.whole, f);
+        }
     }
+}
+cudaError_t launch_finish(cudaStream_t s, const FinishArgs& a, int* launches)
+{
+    const int64_t items = a.rows * ceil_div(a.d, 8);
+    const bool many = a.splits >= 16;
+    ++*launches;
+    const dim3 grid((unsigned)std::min<int64_t>(8 * sm_count(), ceil_div(items, many ? 16 : 256)));
+    return many ? launch_kernel(finish_parts_kernel<16>, grid, dim3(256), 0, s, a) : launch_kernel(finish_parts_kernel<1>, grid, dim3(256), 0, s, a);
 }
 
 // ---- plan ------------------------------------------------------------------------------------------------------------------
 
-constexpr int64_t kPieceBytes = int64_t(256) << 20;      // of G, and of the forward pass's parts
+constexpr int64_t kPieceBytes = int64_t(512) << 20;      // of G, and of the forward pass's parts
 constexpr size_t kAlign = 256;
 size_t up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 
 int tile_cols(int columns) { return columns <= 64 ? 64 : columns <= 128 ? 128 : 256; }
 
-// How many parts a product's depth is split into, so that its tiles fill the machine: the fewest rounds of the 148 multiprocessors,
-// counted in whole products, of parts of at least 8 stages, where a part more must save a twentieth.
-int pick_splits(int64_t tiles, int64_t stages, int most)
+// How many parts a product's depth is split into, so that its tiles fill the machine: the fewest rounds of its multiprocessors (or pairs
+// of them), counted in whole products, of parts of at least 8 stages, where splitting must save a twentieth.
+int pick_splits(int64_t rows, int64_t columns, int64_t stages, int most)
 {
-    const int sms = 148;
+    const int bn = tile_cols((int)columns);
+    const bool pairs = bn == 256 && rows > gemm::kRows;
+    const int units = pairs ? 74 : 148;
+    const int64_t tiles = ceil_div(rows, pairs ? 256 : 128) * ceil_div(columns, bn);
     int best = 1;
     double cost = 1e30;
     for (int s = 1; s <= most && (s == 1 || stages / s >= 8); ++s) {
-        const double c = (double)ceil_div(tiles * s, sms) / s * (1.0 + 0.02 * s / std::max<int64_t>(1, most));
+        const double c = (double)ceil_div(tiles * s, units) / s * (1.0 + 0.02 * s / most);
         if (c < cost * 0.95) cost = c, best = s;
     }
     return best;
@@ -491,9 +545,8 @@ Plan make_plan(int64_t n, int d, int classes, bool backward, bool align_w)
         p.col_pieces = (int)ceil_div(classes, p.cols);
         p.bn_d = tile_cols(d);
         p.pitch = round_up(d, 8);
-        const int64_t tiles_d = ceil_div(d, p.bn_d);
-        p.splits_x = pick_splits(ceil_div(p.rows, 128) * tiles_d, p.cols / 64, 8);
-        p.splits_w = pick_splits(ceil_div(p.cols, 128) * tiles_d, p.rows / 64, 148);
+        p.splits_x = pick_splits(p.rows, d, p.cols / 64, 8);
+        p.splits_w = pick_splits(p.cols, d, p.rows / 64, 148);
         p.g = take((size_t)p.rows * p.cols * 2);
         if (p.splits_x > 1 || p.col_pieces > 1) p.px = take((size_t)p.splits_x * p.n_pad * p.pitch * 4);
         if (p.splits_w > 1 || p.row_pieces > 1) p.pw = take((size_t)p.splits_w * round_up(p.cols, 128) * p.pitch * 4);
@@ -524,7 +577,8 @@ cudaError_t prepare(cudaStream_t s, const Plan& p, char* ws, const void* x, int6
         if (e != cudaSuccess) return e;
     }
     const ListArgs list = {labels, n, classes, counts, reinterpret_cast<int*>(ws + p.kept), reinterpret_cast<int*>(ws + p.label),
-                           reinterpret_cast<int*>(ws + p.place), reinterpret_cast<int*>(ws + p.count), loss, lse};
+                           reinterpret_cast<int*>(ws + p.place), reinterpret_cast<int*>(ws + p.count), loss, lse,
+                           (reinterpret_cast<uintptr_t>(loss) | reinterpret_cast<uintptr_t>(lse)) % 16 == 0};
     ++*launches;
     e = launch_kernel(list_labels_kernel, dim3(blocks), dim3(1024), 0, s, list);
     if (e != cudaSuccess) return e;
@@ -532,12 +586,16 @@ cudaError_t prepare(cudaStream_t s, const Plan& p, char* ws, const void* x, int6
     const GatherArgs gather = {static_cast<const uint16_t*>(x), ldx, n, d, o->x_whole, list.place, list.count, reinterpret_cast<uint16_t*>(ws + p.x), p.ldt,
                                static_cast<uint16_t*>(g_x), ldgx, rows_whole(g_x, ldgx, BIGCN_BF16, 8)};
     ++*launches;
-    e = launch_kernel(gather_rows_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(n, 8), 8 * sm_count())), dim3(256), 0, s, gather);
+    e = launch_kernel(gather_rows_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(n, 256), 8 * sm_count())), dim3(256), 0, s, gather);
     if (e != cudaSuccess) return e;
     if (!rows_whole(w, ldw, BIGCN_BF16, 8)) {
         ++*launches;
-        e = launch_kernel(align_rows_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(classes, 8), 8 * sm_count())), dim3(256), 0, s, static_cast<const uint16_t*>(w), ldw, (int64_t)classes, d,
-                          reinterpret_cast<uint16_t*>(ws + p.w), p.ldt);
+        const dim3 grid((unsigned)std::min<int64_t>(ceil_div(classes, 8), 8 * sm_count()));
+        const uint16_t* from = static_cast<const uint16_t*>(w);
+        uint16_t* to = reinterpret_cast<uint16_t*>(ws + p.w);
+        if (rows_whole(w, ldw, BIGCN_BF16, 4)) e = launch_kernel(align_rows_kernel<uint2>, grid, dim3(256), 0, s, from, ldw, (int64_t)classes, d, to, p.ldt);
+        else if (rows_whole(w, ldw, BIGCN_BF16, 2)) e = launch_kernel(align_rows_kernel<uint32_t>, grid, dim3(256), 0, s, from, ldw, (int64_t)classes, d, to, p.ldt);
+        else e = launch_kernel(align_rows_kernel<uint16_t>, grid, dim3(256), 0, s, from, ldw, (int64_t)classes, d, to, p.ldt);
         o->w = ws + p.w;
         o->ldw = p.ldt;
     }
@@ -651,7 +709,6 @@ cudaError_t launch_class_loss_backward(cudaStream_t s, const void* x, int64_t ld
     const int* label = reinterpret_cast<const int*>(ws + p.label);
     uint16_t* g = reinterpret_cast<uint16_t*>(ws + p.g);
     const bool parts_x = p.splits_x > 1 || p.col_pieces > 1, parts_w = p.splits_w > 1 || p.row_pieces > 1;
-    const unsigned finish_blocks = 8 * sm_count();
     for (int c = 0; c < p.col_pieces && e == cudaSuccess; ++c) {
         const int64_t first_class = c * p.cols;
         const int here = (int)std::min<int64_t>(p.cols, classes - first_class);
@@ -681,8 +738,7 @@ cudaError_t launch_class_loss_backward(cudaStream_t s, const void* x, int64_t ld
                 e = launch_gradient<false>(s, p.bn_d, mg, mw, mw, sh, args, flag);
                 if (e == cudaSuccess && parts_x && c == p.col_pieces - 1) {
                     const FinishArgs fa = {args.part, p.splits_x, args.split_stride, p.pitch, count, (int)first, rows, d, kept + first, static_cast<uint16_t*>(g_x), ldgx, args.whole};
-                    ++*launches;
-                    e = launch_kernel(finish_parts_kernel, dim3((unsigned)std::min<int64_t>(finish_blocks, ceil_div(rows * ceil_div(d, 8), 256))), dim3(256), 0, s, fa);
+                    e = launch_finish(s, fa, launches);
                 }
                 if (e != cudaSuccess) break;
             }
@@ -703,8 +759,7 @@ cudaError_t launch_class_loss_backward(cudaStream_t s, const void* x, int64_t ld
                 e = launch_gradient<true>(s, p.bn_d, mg, mx, own, sh, args, flag);
                 if (e == cudaSuccess && parts_w && r == p.row_pieces - 1) {
                     const FinishArgs fa = {args.part, p.splits_w, args.split_stride, p.pitch, nullptr, 0, here, d, nullptr, out, ldgw, args.whole};
-                    ++*launches;
-                    e = launch_kernel(finish_parts_kernel, dim3((unsigned)std::min<int64_t>(finish_blocks, ceil_div((int64_t)here * ceil_div(d, 8), 256))), dim3(256), 0, s, fa);
+                    e = launch_finish(s, fa, launches);
                 }
             }
         }

@@ -49,13 +49,21 @@ __device__ __forceinline__ float2 unpack2(uint32_t w)
     else return __half22float2(*reinterpret_cast<const __half2*>(&w));
 }
 
-// V (4 or 8) consecutive elements, of which the first `count` exist; the rest read as 0.  `whole`: the pointer is aligned to V
-// elements, and they can be moved as whole words where all of them exist.
+// V (1, 2, 4 or 8) consecutive elements, of which the first `count` exist; the rest read as 0.  `whole`: the pointer is aligned to V
+// elements (or 16 bytes), and they can be moved as whole words where all of them exist.
 template <int TYPE, int V>
 __device__ __forceinline__ void load_elts(const typename Elt<TYPE>::T* __restrict__ p, int count, bool whole, float (&v)[V])
 {
     if (whole && count >= V) {
-        if constexpr (TYPE == BIGCN_F32) {
+        if constexpr (V == 1) {
+            v[0] = to_float<TYPE>(*p);
+        } else if constexpr (V == 2 && TYPE == BIGCN_F32) {
+            const float2 w = *reinterpret_cast<const float2*>(p);
+            v[0] = w.x; v[1] = w.y;
+        } else if constexpr (V == 2) {
+            const float2 w = unpack2<TYPE>(*reinterpret_cast<const uint32_t*>(p));
+            v[0] = w.x; v[1] = w.y;
+        } else if constexpr (TYPE == BIGCN_F32) {
 #pragma unroll
             for (int i = 0; i < V; i += 4) {
                 const float4 w = *reinterpret_cast<const float4*>(p + i);
@@ -85,7 +93,13 @@ template <int TYPE, int V>
 __device__ __forceinline__ void store_elts(typename Elt<TYPE>::T* __restrict__ p, int count, bool whole, const float (&v)[V])
 {
     if (whole && count >= V) {
-        if constexpr (TYPE == BIGCN_F32) {
+        if constexpr (V == 1) {
+            *p = from_float<TYPE>(v[0]);
+        } else if constexpr (V == 2 && TYPE == BIGCN_F32) {
+            *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
+        } else if constexpr (V == 2) {
+            *reinterpret_cast<uint32_t*>(p) = pack2<TYPE>(v[0], v[1]);
+        } else if constexpr (TYPE == BIGCN_F32) {
 #pragma unroll
             for (int i = 0; i < V; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
         } else if constexpr (V == 4) {
@@ -99,7 +113,16 @@ __device__ __forceinline__ void store_elts(typename Elt<TYPE>::T* __restrict__ p
     for (int i = 0; i < V; ++i)
         if (i < count) p[i] = from_float<TYPE>(v[i]);
 }
-// the same with the type known at run time
+// the same with the type known at run time (TYPE < 0) or not
+constexpr int kAnyType = -1;
+template <int TYPE, int V>
+__device__ __forceinline__ void load_as(const void* base, int type, int64_t at, int count, bool whole, float (&v)[V])
+{
+    if constexpr (TYPE >= 0) load_elts<TYPE, V>(static_cast<const typename Elt<TYPE>::T*>(base) + at, count, whole, v);
+    else if (type == BIGCN_F32) load_elts<BIGCN_F32, V>(static_cast<const float*>(base) + at, count, whole, v);
+    else if (type == BIGCN_BF16) load_elts<BIGCN_BF16, V>(static_cast<const __nv_bfloat16*>(base) + at, count, whole, v);
+    else load_elts<BIGCN_F16, V>(static_cast<const __half*>(base) + at, count, whole, v);
+}
 template <int V>
 __device__ __forceinline__ void store_as(void* base, int type, int64_t at, int count, bool whole, const float (&v)[V])
 {

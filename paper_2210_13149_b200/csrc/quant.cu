@@ -27,14 +27,26 @@ struct QuantArgs {
     float* scale;
 };
 
-// The nearest integer to 127 x / top.  In fp32 the quotient is off by 127 * 3 * 2^-24 at most; where that could decide the rounding, it is
-// taken in 64 bits, where 127 x is exact and a quotient halfway between integers cannot be met or missed by its rounding: with x and
-// top of 24 bits it is halfway, or at least 2^-32 of its size away from it.
-__device__ __forceinline__ int nearest(float x, float factor, float top, bool tiny)
+// Four values as the integers nearest to 127 x / top, in the bytes of a word.  In fp32 the quotient is off by 127 * 3 * 2^-24 at
+// most; where that could decide one of the roundings, they are taken in 64 bits, where 127 x is exact and a quotient halfway between integers
+// cannot be met or missed by its rounding: with x and top of 24 bits it is halfway, or at least 2^-32 of its size away from it.  The sum with
+// 1.5 * 2^23 rounds to the integer and holds it in its low bits.
+__device__ __forceinline__ uint32_t nearest4(const float* x, float factor, float top, bool tiny)
 {
-    const float t = x * factor, r = rintf(t);
-    if (!tiny && fabsf(t - r) < 0.4999f) return (int)r;
-    return (int)rint(127.0 * (double)x / (double)top);
+    constexpr float kRound = 12582912.f;
+    uint32_t n[4];
+    float off = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float t = x[i] * factor, r = t + kRound;
+        n[i] = __float_as_uint(r);
+        off = fmaxf(off, fabsf(t - (r - kRound)));
+    }
+    if (tiny || off > 0.4999f) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n[i] = (uint32_t)(int)rint(127.0 * (double)x[i] / (double)top);
+    }
+    return __byte_perm(__byte_perm(n[0], n[1], 0x0040), __byte_perm(n[2], n[3], 0x0040), 0x5410);
 }
 
 // One row to LANES threads (a warp or a block), V values at a time, NV times.
@@ -75,14 +87,7 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : 256) quantize_kernel(cons
         if (c >= a.d) break;
         uint32_t w[V / 4];
 #pragma unroll
-        for (int j = 0; j < V / 4; ++j) {
-            w[j] = 0u;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int qi = finite && top ? nearest(v[k][4 * j + i], factor, t, tiny) : 0;
-                w[j] |= ((uint32_t)qi & 255u) << (8 * i);
-            }
-        }
+        for (int j = 0; j < V / 4; ++j) w[j] = finite && top ? nearest4(&v[k][4 * j], factor, t, tiny) : 0u;
         if (c + V <= a.d) {                   // rows of q start on 16-byte boundaries
             if constexpr (V == 4) *reinterpret_cast<uint32_t*>(q + c) = w[0];
             else *reinterpret_cast<uint2*>(q + c) = make_uint2(w[0], w[1]);
@@ -107,6 +112,7 @@ cudaError_t pick_quantize(cudaStream_t s, const QuantArgs& a, int* launches)
     constexpr int Q = 16 / V;
     const int64_t words = ceil_div(a.d, V);
     if (words <= 32) return launch_quantize_as<TYPE, V, 32, 1>(s, a, launches);
+    if (words <= 64) return launch_quantize_as<TYPE, V, 32, 2>(s, a, launches);
     if (words <= 32 * Q) return launch_quantize_as<TYPE, V, 32, Q>(s, a, launches);
     if (words <= 128 * Q) return launch_quantize_as<TYPE, V, 128, Q>(s, a, launches);
     if (words <= 512 * Q) return launch_quantize_as<TYPE, V, 512, Q>(s, a, launches);

@@ -1118,7 +1118,7 @@ bigcn_status bigcn_quantize_rows(bigcn_ctx* ctx, const void* x, int32_t type, in
     if ((st = check_rows(ctx, "x", x, type, n, d, ldx)) != BIGCN_OK) return st;
     if ((st = check_quantized(ctx, "q", q, n, d, ldq, scale)) != BIGCN_OK) return st;
     if (n == 0) return BIGCN_OK;
-    cudaError_t e = launch_quantize_rows(ctx->stream, x, type, n, d, ldx, q, ldq, scale, &ctx->launches_i);
+    cudaError_t e = launch_quantize_rows(ctx->stream, x, type, n, d, ldx, q, ldq, scale, false, &ctx->launches_i);
     finish_call(ctx);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "quantize launch");
     return BIGCN_OK;
@@ -1150,18 +1150,19 @@ bigcn_status bigcn_quantized_product(bigcn_ctx* ctx, const void* x, int32_t x_ty
     if (!aligned(out, out_type == BIGCN_F32 ? 4 : 2)) return fail(ctx, BIGCN_ERR_ALIGN, "out is not aligned to its elements");
     const int8_t* q_x = static_cast<const int8_t*>(x);
     cudaError_t e = cudaSuccess;
+    const bool early = !ready && quantized_across(n, m);
     if (!ready) {
         const size_t need = bigcn_quantized_product_workspace_bytes(n, d);
         if (!ctx->ws || ctx->ws_bytes < need) return fail(ctx, BIGCN_ERR_WORKSPACE, "needs %zu bytes of workspace (bigcn_quantized_product_workspace_bytes)", need);
         int8_t* q = static_cast<int8_t*>(ctx->ws);
         const int64_t ldq = round_up(d, 16);
         float* scale = reinterpret_cast<float*>(q + up((size_t)n * (size_t)ldq));
-        e = launch_quantize_rows(ctx->stream, x, x_type, n, d, ldx, q, ldq, scale, &ctx->launches_i);
+        e = launch_quantize_rows(ctx->stream, x, x_type, n, d, ldx, q, ldq, scale, early, &ctx->launches_i);
         q_x = q;
         ldx = ldq;
         s_x = scale;
     }
-    if (e == cudaSuccess) e = launch_quantized_product(ctx->stream, q_x, ldx, s_x, n, d, q_w, ldqw, s_w, m, out, out_type, ldo, &ctx->launches_i);
+    if (e == cudaSuccess) e = launch_quantized_product(ctx->stream, q_x, ldx, s_x, n, d, q_w, ldqw, s_w, m, out, out_type, ldo, early, &ctx->launches_i);
     finish_call(ctx);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "quantized product launch");
     return BIGCN_OK;

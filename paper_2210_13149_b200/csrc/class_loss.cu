@@ -146,8 +146,10 @@ struct GatherArgs {
     uint16_t* g_x;           // nullable: rows without a label become zero
     int64_t ldgx;
     bool g_whole;
+    bool pairs;              // rows of x and of `to` can be moved in words of two elements
+    int span;                // rows of a warp at a time, at most 32
 };
-// A warp to 32 rows at a time, whose places its lanes read together: labelled rows are copied together, the gradient of the others is
+// A warp to `span` rows at a time, whose places its lanes read together: labelled rows are copied together, the gradient of the others is
 // zero; rows up to the next multiple of 128 are zero.
 __global__ void __launch_bounds__(256) gather_rows_kernel(const GatherArgs a)
 {
@@ -157,9 +159,9 @@ __global__ void __launch_bounds__(256) gather_rows_kernel(const GatherArgs a)
     if (a.whole && count == a.n) return;
     const int64_t warps = (int64_t)gridDim.x * 8, first = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     const int words = a.d / 8, rest = a.d - 8 * words;
-    for (int64_t row0 = first * 32; row0 < a.n; row0 += warps * 32) {
-        const int place = row0 + lane < a.n ? __ldg(a.place + row0 + lane) : -1;
-        const int rows = (int)min((int64_t)32, a.n - row0);
+    for (int64_t row0 = first * a.span; row0 < a.n; row0 += warps * a.span) {
+        const int rows = (int)min((int64_t)a.span, a.n - row0);
+        const int place = lane < rows ? __ldg(a.place + row0 + lane) : -1;
         const uint32_t kept = __ballot_sync(0xffffffffu, place >= 0);
         for (uint32_t left = kept; left != 0u; left &= left - 1) {
             const int r = __ffs(left) - 1;
@@ -168,6 +170,9 @@ __global__ void __launch_bounds__(256) gather_rows_kernel(const GatherArgs a)
             if (a.whole) {
                 for (int w = lane; w < words; w += 32) reinterpret_cast<uint4*>(to)[w] = __ldg(reinterpret_cast<const uint4*>(from) + w);
                 if (lane < rest) to[8 * words + lane] = __ldg(from + 8 * words + lane);
+            } else if (a.pairs) {
+                for (int i = lane; i < a.d / 2; i += 32) reinterpret_cast<uint32_t*>(to)[i] = __ldg(reinterpret_cast<const uint32_t*>(from) + i);
+                if (a.d % 2 && lane == 0) to[a.d - 1] = __ldg(from + a.d - 1);
             } else {
                 for (int i = lane; i < a.d; i += 32) to[i] = __ldg(from + i);
             }
@@ -583,10 +588,11 @@ cudaError_t prepare(cudaStream_t s, const Plan& p, char* ws, const void* x, int6
     e = launch_kernel(list_labels_kernel, dim3(blocks), dim3(1024), 0, s, list);
     if (e != cudaSuccess) return e;
     *o = {x, ldx, rows_whole(x, ldx, BIGCN_BF16, 8), reinterpret_cast<const uint16_t*>(ws + p.x), w, ldw};
+    const int span = (int)std::max<int64_t>(1, std::min<int64_t>(32, n / (64 * sm_count())));     // as many warps as the machine holds, first
     const GatherArgs gather = {static_cast<const uint16_t*>(x), ldx, n, d, o->x_whole, list.place, list.count, reinterpret_cast<uint16_t*>(ws + p.x), p.ldt,
-                               static_cast<uint16_t*>(g_x), ldgx, rows_whole(g_x, ldgx, BIGCN_BF16, 8)};
+                               static_cast<uint16_t*>(g_x), ldgx, rows_whole(g_x, ldgx, BIGCN_BF16, 8), rows_whole(x, ldx, BIGCN_BF16, 2), span};
     ++*launches;
-    e = launch_kernel(gather_rows_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(n, 256), 8 * sm_count())), dim3(256), 0, s, gather);
+    e = launch_kernel(gather_rows_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(n, 8 * span), 8 * sm_count())), dim3(256), 0, s, gather);
     if (e != cudaSuccess) return e;
     if (!rows_whole(w, ldw, BIGCN_BF16, 8)) {
         ++*launches;

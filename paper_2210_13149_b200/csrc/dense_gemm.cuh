@@ -41,6 +41,8 @@ struct Shape {
     const int* count = nullptr;
     int of = 0, base = 0;
     bool over_depth = false, alt_a = false, alt_b = false;
+    bool a_ahead = false;    // A does not come from the kernel before this one (which let this one start early): its first stages are
+                             // fetched while that one runs.  No count, one block to a tile.
 };
 
 struct Unit {
@@ -320,6 +322,18 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     const uint32_t tmem = ctl.tmem;
     volatile int* abort = &ctl.abort;
 
+    int early = 0;           // stages whose A is on its way
+    if (CTAS == 1 && !A_MN && shape.a_ahead && threadIdx.x == kProducer * 32) {
+        const Walk walk(shape, kRows, BN, kDepth);
+        if ((int)blockIdx.x < walk.units()) {
+            const Unit t = walk.at(blockIdx.x);
+            early = min(t.k1 - t.k0, C::kStages);
+            for (int i = 0; i < early; ++i) {
+                expect_bytes<CTAS>(&ctl.full[i], C::kStage);
+                copy_box<CTAS>(tc::smem_u32(stages + i * C::kStage), &map_a, (t.k0 + i) * kDepth, t.row, &ctl.full[i]);
+            }
+        }
+    }
     pdl_enter();
     const Walk walk(shape, kRows * CTAS, BN, kDepth);
     const int units = walk.units(), first = blockIdx.x / CTAS, step = gridDim.x / CTAS;
@@ -339,9 +353,11 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 for (int k = t.k0; k < t.k1; ++k) {
                     ok = wait(&ctl.empty[slot], phase ^ 1u, abort, flag);
                     if (!ok) break;
-                    if (rank == 0) expect_bytes<CTAS>(&ctl.full[slot], C::kStage * CTAS);
+                    const bool fetched = issued < early;
+                    if (rank == 0 && !fetched) expect_bytes<CTAS>(&ctl.full[slot], C::kStage * CTAS);
                     const uint32_t sa = tc::smem_u32(stages + slot * C::kStage), sb = sa + C::kABytes;
-                    if constexpr (A_MN) {
+                    if (fetched) {
+                    } else if constexpr (A_MN) {
 #pragma unroll
                         for (int i = 0; i < kRows / 64; ++i) copy_box<CTAS>(sa + i * 8192, ma, arow + 64 * i, k * kDepth, &ctl.full[slot]);
                     } else {

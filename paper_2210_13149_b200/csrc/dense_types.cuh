@@ -131,11 +131,108 @@ __device__ __forceinline__ void store_as(void* base, int type, int64_t at, int c
     else store_elts<BIGCN_F16, V>(static_cast<__half*>(base) + at, count, whole, v);
 }
 
+// The same in words of at most `step` elements, a power of two that the address is aligned to.
+template <int V>
+__device__ __forceinline__ void store_steps(void* base, int type, int64_t at, int count, int step, const float (&v)[V])
+{
+    if constexpr (V == 1) {
+        store_as<1>(base, type, at, count, true, v);
+    } else {
+        if (step >= V) return store_as<V>(base, type, at, count, true, v);
+        float lo[V / 2], hi[V / 2];
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) lo[i] = v[i], hi[i] = v[V / 2 + i];
+        store_steps<V / 2>(base, type, at, count, step, lo);
+        store_steps<V / 2>(base, type, at + V / 2, count - V / 2, step, hi);
+    }
+}
+
+// V elements as they lie in memory: 16 bytes of a type known when compiled, or fp32 values.
+template <int TYPE, int V>
+struct Raw {
+    static constexpr int kWords = TYPE == kAnyType ? V : V * type_bytes(TYPE) / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const void* base, int type, int64_t at, int count)
+    {
+        if constexpr (TYPE == kAnyType) {
+            float f[V];
+            load_as<TYPE, V>(base, type, at, count, true, f);
+#pragma unroll
+            for (int i = 0; i < V; ++i) w[i] = __float_as_uint(f[i]);
+        } else if (count >= V) {
+            const auto* p = static_cast<const typename Elt<TYPE>::T*>(base) + at;
+            if constexpr (kWords == 4) {
+                const uint4 q = *reinterpret_cast<const uint4*>(p);
+                w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+            } else {
+                static_assert(kWords == 2, "");
+                const uint2 q = *reinterpret_cast<const uint2*>(p);
+                w[0] = q.x; w[1] = q.y;
+            }
+        } else {
+            float f[V];
+            load_elts<TYPE, V>(static_cast<const typename Elt<TYPE>::T*>(base) + at, count, false, f);
+            pack(f);
+        }
+    }
+    // the same through shared memory: an asynchronous copy to a place of this thread's own, what does not exist as zeros
+    static __device__ __forceinline__ void copy(void* to, const void* base, int64_t at, int count)
+    {
+        constexpr int kBytes = 4 * kWords;
+        const int bytes = count >= V ? kBytes : count > 0 ? count * type_bytes(TYPE) : 0;
+        const auto* p = static_cast<const typename Elt<TYPE>::T*>(base) + (count > 0 ? at : 0);
+        const uint32_t dst = (uint32_t)__cvta_generic_to_shared(to);
+        if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(p), "r"(bytes) : "memory");
+        else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;\n" ::"r"(dst), "l"(p), "r"(bytes) : "memory");
+    }
+    __device__ __forceinline__ void take(const void* from)
+    {
+        if constexpr (kWords == 4) {
+            const uint4 q = *static_cast<const uint4*>(from);
+            w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+        } else if constexpr (kWords == 2) {
+            const uint2 q = *static_cast<const uint2*>(from);
+            w[0] = q.x; w[1] = q.y;
+        }
+    }
+    __device__ __forceinline__ void pack(const float (&f)[V])
+    {
+        if constexpr (kWords == V) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) w[i] = __float_as_uint(f[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) w[i] = pack2<TYPE>(f[2 * i], f[2 * i + 1]);
+        }
+    }
+    __device__ __forceinline__ void values(float (&f)[V]) const
+    {
+        if constexpr (kWords == V) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) f[i] = __uint_as_float(w[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) {
+                const float2 u = unpack2<TYPE>(w[i]);
+                f[2 * i] = u.x;
+                f[2 * i + 1] = u.y;
+            }
+        }
+    }
+};
+
 // Whether rows of `ld` elements from `base` on can be moved in words of V elements.
 inline bool rows_whole(const void* base, int64_t ld, int type, int V)
 {
     const int64_t bytes = (int64_t)V * type_bytes(type), word = bytes < 16 ? bytes : 16;
     return reinterpret_cast<uintptr_t>(base) % word == 0 && ld * type_bytes(type) % word == 0;
+}
+
+// The widest words of at most V elements that they can be moved in.
+inline int rows_step(const void* base, int64_t ld, int type, int V)
+{
+    while (V > 1 && !rows_whole(base, ld, type, V)) V /= 2;
+    return V;
 }
 
 }  // namespace dense

@@ -25,6 +25,7 @@ struct QuantArgs {
     int8_t* q;
     int64_t ldq;
     float* scale;
+    bool early;              // the next kernel may start: it waits for this one where it reads what this one writes
 };
 
 // Four values as the integers nearest to 127 x / top, in the bytes of a word.  In fp32 the quotient is off by 127 * 3 * 2^-24 at
@@ -54,6 +55,7 @@ template <int TYPE, int V, int LANES, int NV>
 __global__ void __launch_bounds__(LANES > 32 ? LANES : 256) quantize_kernel(const QuantArgs a)
 {
     pdl_enter();
+    if (a.early) asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     constexpr int B = LANES > 32 ? LANES : 256, GROUPS = B / LANES;
     __shared__ uint32_t slot[LANES > 32 ? LANES / 32 : 1];
     const int lane = threadIdx.x % LANES;
@@ -188,6 +190,28 @@ struct ScaledOut {
     }
 };
 
+// The same with classes as rows of the tiles and the few rows of x as columns: a lane has a class, so that 32 neighbours of an output row
+// are stored together, and 128 class rows to a tile leave more tiles than 256 columns would.
+struct ScaledAcross {
+    using Args = ScaledOut::Args;
+    template <int BN, class Done>
+    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit&, const gemm::Part& p, const Done& done)
+    {
+        const int k = p.row + (threadIdx.x & 31);
+        const float sw = k < p.rows ? __ldg(a.s_w + k) : 0.f;
+        gemm::each_chunk<BN>(p, sh.n, done, [&](int c, uint32_t (&v)[32]) {
+            if (k >= p.rows) return;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                const int row = p.col + c + i;
+                if (row >= sh.n) break;
+                const float f[1] = {(float)(int)v[i] * (__ldg(a.s_x + row) * sw)};
+                store_as<1>(a.out, a.type, (int64_t)row * a.ldo + k, 1, true, f);
+            }
+        });
+    }
+};
+
 template <int BN, int CTAS>
 cudaError_t launch_product_as(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const int8_t* q_w, int64_t ldqw, const gemm::Shape& shape, const ScaledOut::Args& args, int* flag)
 {
@@ -196,6 +220,16 @@ cudaError_t launch_product_as(cudaStream_t s, const int8_t* q_x, int64_t ldqx, c
     if (e == cudaSuccess) e = gemm::encode_map(&mb, q_w, 1, true, shape.n, shape.k, ldqw, 128, BN / CTAS);
     if (e != cudaSuccess) return e;
     return gemm::launch<true, BN, CTAS, false, false, ScaledOut>(s, ma, mb, ma, shape, args, flag);
+}
+
+template <int BN>
+cudaError_t launch_across(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const int8_t* q_w, int64_t ldqw, const gemm::Shape& shape, const ScaledOut::Args& args, int* flag)
+{
+    CUtensorMap ma, mb;
+    cudaError_t e = gemm::encode_map(&ma, q_w, 1, true, shape.m, shape.k, ldqw, 128, gemm::kRows);
+    if (e == cudaSuccess) e = gemm::encode_map(&mb, q_x, 1, true, shape.n, shape.k, ldqx, 128, BN);
+    if (e != cudaSuccess) return e;
+    return gemm::launch<true, BN, 1, false, false, ScaledAcross>(s, ma, mb, ma, shape, args, flag);
 }
 
 }  // namespace
@@ -207,16 +241,18 @@ int quant_timeouts()
     return v;
 }
 
-cudaError_t launch_quantize_rows(cudaStream_t s, const void* x, int type, int64_t n, int d, int64_t ldx, int8_t* q, int64_t ldq, float* scale, int* launches)
+bool quantized_across(int64_t n, int m) { return n <= 64 && m > 64; }
+
+cudaError_t launch_quantize_rows(cudaStream_t s, const void* x, int type, int64_t n, int d, int64_t ldx, int8_t* q, int64_t ldq, float* scale, bool early, int* launches)
 {
-    const QuantArgs a = {x, ldx, n, d, rows_whole(x, ldx, type, type == BIGCN_F32 ? 4 : 8), q, ldq, scale};
+    const QuantArgs a = {x, ldx, n, d, rows_whole(x, ldx, type, type == BIGCN_F32 ? 4 : 8), q, ldq, scale, early};
     if (type == BIGCN_F32) return pick_quantize<BIGCN_F32, 4>(s, a, launches);
     if (type == BIGCN_BF16) return pick_quantize<BIGCN_BF16, 8>(s, a, launches);
     return pick_quantize<BIGCN_F16, 8>(s, a, launches);
 }
 
 cudaError_t launch_quantized_product(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const float* s_x, int64_t n, int d, const int8_t* q_w, int64_t ldqw,
-                                     const float* s_w, int m, void* out, int out_type, int64_t ldo, int* launches)
+                                     const float* s_w, int m, void* out, int out_type, int64_t ldo, bool early, int* launches)
 {
     int* flag = nullptr;
     cudaError_t e = cudaGetSymbolAddress(reinterpret_cast<void**>(&flag), g_quant_timeout);
@@ -227,6 +263,12 @@ cudaError_t launch_quantized_product(cudaStream_t s, const int8_t* q_x, int64_t 
     shape.n = m;
     shape.k = d;
     ++*launches;
+    if (quantized_across(n, m)) {
+        shape.m = m;
+        shape.n = (int)n;
+        shape.a_ahead = early;
+        return launch_across<64>(s, q_x, ldqx, q_w, ldqw, shape, args, flag);
+    }
     if (m <= 64) return launch_product_as<64, 1>(s, q_x, ldqx, q_w, ldqw, shape, args, flag);
     if (m <= 128) return launch_product_as<128, 1>(s, q_x, ldqx, q_w, ldqw, shape, args, flag);
     if (n > gemm::kRows) return launch_product_as<256, 2>(s, q_x, ldqx, q_w, ldqw, shape, args, flag);

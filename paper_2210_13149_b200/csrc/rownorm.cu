@@ -9,9 +9,8 @@
 // cancellation.  The columns' sums of the backward pass ride along in registers, one pair per column a thread owns, over the rows that
 // its lanes take; blocks leave theirs in the workspace, and a second kernel adds them in 64 bits in a fixed order.
 //
-// Lanes move words of 16 bytes where the rows of all matrices start on their boundaries (kernels for each type), and otherwise words of
-// 4, 2 or 1 elements, whichever all of them allow (kernels that look the type up): 89,250 bf16 rows of 500 columns, backward, in us: 312
-// with single elements for the matrix that fits no 16 bytes, N1 in words of four.
+// Lanes read words of 16 bytes where the rows they read start on their boundaries (kernels for each type), and otherwise words of
+// 4, 2 or 1 elements, whichever both matrices allow (kernels that look the type up); they store what the output's rows allow.
 #include <algorithm>
 
 #include "dense_types.cuh"
@@ -50,13 +49,33 @@ __device__ __forceinline__ void group_sum(float (&v)[COUNT], float* slot)
     }
 }
 
+// The columns' factors of a kernel whose threads own more than 8 columns each: in shared memory, `none` past d and where there are none.
+__device__ __forceinline__ void stage_columns(float* to, const float* p, float none, int d, int padded)
+{
+    for (int c = threadIdx.x; c < padded; c += blockDim.x) to[c] = c < d && p ? __ldg(p + c) : none;
+}
+template <int V>
+__device__ __forceinline__ void staged(const float* from, float (&v)[V])
+{
+    if constexpr (V % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < V; i += 4) {
+            const float4 q = *reinterpret_cast<const float4*>(from + i);
+            v[i] = q.x; v[i + 1] = q.y; v[i + 2] = q.z; v[i + 3] = q.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = from[i];
+    }
+}
+
 struct NormArgs {
     const void* x;
     int x_type;
     int64_t ldx;
     int64_t n;
     int d;
-    bool x_whole, y_whole;     // rows start on boundaries of the kernel's words
+    int y_step;              // elements of y that can be stored at a time
     const float* gain;       // nullable: 1
     const float* offset;     // nullable: 0
     float eps;
@@ -68,55 +87,50 @@ struct NormArgs {
 };
 
 template <int TYPE, int V, int LANES, int NV>
-__global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads) norm_kernel(const NormArgs a)
+__global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads, LANES > 32 ? 1 : 4) norm_kernel(const NormArgs a)
 {
     pdl_enter();
     constexpr int B = LANES > 32 ? LANES : kThreads, GROUPS = B / LANES;
+    constexpr bool kHold = NV * V <= 8;          // gain and offset stay in registers over the rows
+    extern __shared__ float dyn[];               // else [2][LANES V NV]
     __shared__ float slots[2][LANES > 32 ? LANES / 32 : 1];
     const int lane = threadIdx.x % LANES;
     const float inv_d = 1.f / (float)a.d;
-    constexpr bool kHold = NV * V <= 8;          // gain and offset stay in registers over the rows
     float gain[kHold ? NV * V : 1], offset[kHold ? NV * V : 1];
-    auto column_words = [&](const float* p, float none, int c, float (&v)[V]) {
-        if (p) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = c + i < a.d ? __ldg(p + c + i) : 0.f;
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = none;
-        }
-    };
     if constexpr (kHold) {
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            float v[V];
-            column_words(a.gain, 1.f, (k * LANES + lane) * V, v);
+        for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int i = 0; i < V; ++i) gain[k * V + i] = v[i];
-            column_words(a.offset, 0.f, (k * LANES + lane) * V, v);
-#pragma unroll
-            for (int i = 0; i < V; ++i) offset[k * V + i] = v[i];
-        }
+            for (int i = 0; i < V; ++i) {
+                const int c = (k * LANES + lane) * V + i;
+                gain[k * V + i] = c < a.d && a.gain ? __ldg(a.gain + c) : 1.f;
+                offset[k * V + i] = c < a.d && a.offset ? __ldg(a.offset + c) : 0.f;
+            }
+    } else {
+        stage_columns(dyn, a.gain, 1.f, a.d, LANES * V * NV);
+        stage_columns(dyn + LANES * V * NV, a.offset, 0.f, a.d, LANES * V * NV);
+        __syncthreads();
     }
     const int64_t step = (int64_t)gridDim.x * GROUPS;
     int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES;
-    const int64_t first_of_block = (int64_t)blockIdx.x * GROUPS;
-    float next[NV][V];
+    Raw<TYPE, V> next[NV];                       // the row after this one is on its way while this one is worked on
     auto fetch = [&](int64_t r) {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (k * LANES + lane) * V;
-            load_as<TYPE, V>(a.x, a.x_type, r * a.ldx + c, r < a.n ? a.d - c : 0, a.x_whole, next[k]);
+            next[k].load(a.x, a.x_type, r * a.ldx + c, r < a.n ? a.d - c : 0);
         }
     };
     fetch(row);
-    for (int64_t base = first_of_block; base < a.n; base += step, row += step) {   // the same trips for all threads of a block
+    for (int64_t base = (int64_t)blockIdx.x * GROUPS; base < a.n; base += step, row += step) {   // the same trips for all threads of a block
         float v[NV][V], sum[1] = {0.f};
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
+        for (int k = 0; k < NV; ++k) {
+            next[k].values(v[k]);
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[k][i] = next[k][i], sum[0] += next[k][i];
-        if constexpr (kHold) fetch(row + step);
+            for (int i = 0; i < V; ++i) sum[0] += v[k][i];
+        }
+        fetch(row + step);
         group_sum<LANES, 1>(sum, slots[0]);
         const float mu = sum[0] * inv_d;
         float sq[1] = {0.f};
@@ -143,15 +157,14 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads) norm_kernel(con
 #pragma unroll
                     for (int i = 0; i < V; ++i) g[i] = gain[k * V + i], o[i] = offset[k * V + i];
                 } else {
-                    column_words(a.gain, 1.f, c, g);
-                    column_words(a.offset, 0.f, c, o);
+                    staged<V>(dyn + c, g);
+                    staged<V>(dyn + LANES * V * NV + c, o);
                 }
 #pragma unroll
                 for (int i = 0; i < V; ++i) v[k][i] = fmaf(v[k][i] * r, g[i], o[i]);
-                store_as<V>(a.y, a.y_type, row * a.ldy + c, a.d - c, a.y_whole, v[k]);
+                store_steps<V>(a.y, a.y_type, row * a.ldy + c, a.d - c, a.y_step, v[k]);
             }
         }
-        if constexpr (!kHold) fetch(row + step);
     }
 }
 
@@ -164,7 +177,7 @@ struct NormBackArgs {
     int64_t ldx;
     int64_t n;
     int d;
-    bool g_whole, x_whole, gx_whole;
+    int gx_step;             // elements of g_x that can be stored at a time
     const float* gain;
     const float* mean;
     const float* rstd;
@@ -174,14 +187,33 @@ struct NormBackArgs {
     float* part;             // [blocks][2][d]: the columns' sums of every block (null: not wanted)
 };
 
+// How a block of the backward pass is laid out.  Its rows come through a ring in shared memory, copied kRing - 1 rows ahead into places
+// that only the thread itself reads, so that nothing but its own copies is waited for: registers hold one row of 16 to 64 bytes ahead and
+// no more (89,250 bf16 rows of 500 columns in us: 102 with one row ahead in registers, 66 with two in the ring).
 template <int GTYPE, int TYPE, int V, int LANES, int NV>
-__global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads) norm_backward_kernel(const NormBackArgs a)
+struct BackLayout {
+    static constexpr int B = LANES > 32 ? LANES : kThreads;
+    static constexpr bool kHold = NV * V <= 8;          // the gain stays in registers, else in shared memory
+    static constexpr bool kShared = LANES >= 1024;      // no registers left for the columns' sums: each thread keeps its own in shared memory
+    static constexpr bool kTyped = TYPE >= 0 && GTYPE >= 0;
+    static constexpr int kRowBytes = NV * 4 * (Raw<GTYPE, V>::kWords + Raw<TYPE, V>::kWords);      // of a thread
+    static constexpr int kRing = !kTyped || kShared ? 0 : LANES >= 512 ? 2 : NV * V > 8 ? 3 : 4;
+    static constexpr int kBlocks = LANES >= 512 ? 1 : LANES > 32 ? 512 / LANES : kHold ? 3 : 2;    // a multiprocessor, by their registers
+    static constexpr bool kAhead = !kRing && kRowBytes <= 64;                                      // the next row's words fit registers
+    static constexpr int kRingBytes = kRing * kRowBytes * B;
+    static size_t smem(int d) { return kRingBytes + (size_t)(kHold ? 0 : LANES * V * NV) * 4 + (LANES > 32 && !kShared ? 0 : (size_t)2 * d * 4); }
+};
+
+template <int GTYPE, int TYPE, int V, int LANES, int NV>
+__global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads, BackLayout<GTYPE, TYPE, V, LANES, NV>::kBlocks) norm_backward_kernel(const NormBackArgs a)
 {
     pdl_enter();
-    constexpr int B = LANES > 32 ? LANES : kThreads, GROUPS = B / LANES;
-    constexpr bool kHold = NV * V <= 8;
-    constexpr bool kShared = LANES >= 1024;      // no registers left for the columns' sums: each thread keeps its own in shared memory
-    extern __shared__ float dyn[];               // [2][d] for the block's sums
+    using L = BackLayout<GTYPE, TYPE, V, LANES, NV>;
+    constexpr int B = L::B, GROUPS = B / LANES, kRing = L::kRing;
+    constexpr bool kHold = L::kHold, kAhead = L::kAhead, kShared = L::kShared;
+    extern __shared__ __align__(16) unsigned char raw[];       // the ring, the gain, [2][d] for the block's sums
+    float* const gains = reinterpret_cast<float*>(raw + L::kRingBytes);
+    float* const dyn = gains + (kHold ? 0 : LANES * V * NV);
     __shared__ float slots[2][LANES > 32 ? 2 * (LANES / 32) : 1];
     const int lane = threadIdx.x % LANES;
     const float inv_d = 1.f / (float)a.d;
@@ -194,48 +226,90 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads) norm_backward_k
                 const int c = (k * LANES + lane) * V + i;
                 gain[k * V + i] = c < a.d && a.gain ? __ldg(a.gain + c) : 1.f;
             }
+    } else {
+        stage_columns(gains, a.gain, 1.f, a.d, LANES * V * NV);
     }
     if constexpr (!kShared) {
 #pragma unroll
         for (int k = 0; k < NV * V; ++k) dgain[k] = 0.f, doff[k] = 0.f;
     } else {
         for (int c = threadIdx.x; c < 2 * a.d; c += B) dyn[c] = 0.f;
-        __syncthreads();
     }
+    if constexpr (!kHold || kShared) __syncthreads();
     const int64_t step = (int64_t)gridDim.x * GROUPS;
     int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES;
-    float nx[kHold ? NV : 1][V], ng[kHold ? NV : 1][V], nmean = 0.f, nrstd = 0.f;
+    Raw<TYPE, V> nx[NV];
+    Raw<GTYPE, V> ng[NV];
+    float nmean = 0.f, nrstd = 0.f;
     auto fetch = [&](int64_t r) {
-        if constexpr (kHold) {
 #pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                const int c = (k * LANES + lane) * V;
-                load_as<TYPE, V>(a.x, a.x_type, r * a.ldx + c, r < a.n ? a.d - c : 0, a.x_whole, nx[k]);
-                load_as<GTYPE, V>(a.g, a.g_type, r * a.ldg + c, r < a.n ? a.d - c : 0, a.g_whole, ng[k]);
-            }
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * LANES + lane) * V;
+            nx[k].load(a.x, a.x_type, r * a.ldx + c, r < a.n ? a.d - c : 0);
+            ng[k].load(a.g, a.g_type, r * a.ldg + c, r < a.n ? a.d - c : 0);
         }
         nmean = r < a.n ? __ldg(a.mean + r) : 0.f;
         nrstd = r < a.n ? __ldg(a.rstd + r) : 0.f;
     };
-    fetch(row);
+    // a thread's place in a slot of the ring: its words of x, then of g, 16-byte pieces B threads apart
+    constexpr int kXBytes = Raw<TYPE, V>::kWords * 4, kGBytes = Raw<GTYPE, V>::kWords * 4;
+    auto place = [&](int slot, int k, bool of_g) {
+        return raw + (size_t)slot * L::kRowBytes * B + (of_g ? (size_t)NV * kXBytes * B + ((size_t)k * B + threadIdx.x) * kGBytes : ((size_t)k * B + threadIdx.x) * kXBytes);
+    };
+    auto send = [&](int64_t r, int slot) {
+        if constexpr (kRing > 0) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int c = (k * LANES + lane) * V, count = r < a.n ? a.d - c : 0;
+                Raw<TYPE, V>::copy(place(slot, k, false), a.x, r * a.ldx + c, count);
+                Raw<GTYPE, V>::copy(place(slot, k, true), a.g, r * a.ldg + c, count);
+            }
+            asm volatile("cp.async.commit_group;\n" ::: "memory");
+        }
+    };
+    int slot = 0;
+    if constexpr (kRing > 0) {
+#pragma unroll
+        for (int i = 0; i < kRing - 1; ++i) send(row + i * step, i);
+        nmean = row < a.n ? __ldg(a.mean + row) : 0.f;
+        nrstd = row < a.n ? __ldg(a.rstd + row) : 0.f;
+    }
+    if constexpr (kAhead) fetch(row);
     for (int64_t base = (int64_t)blockIdx.x * GROUPS, trip = 0; base < a.n; base += step, row += step, ++trip) {
         float xh[NV][V], gv[NV][V], sums[2] = {0.f, 0.f};
+        if constexpr (kRing > 0) {
+            send(row + (kRing - 1) * step, slot == 0 ? kRing - 1 : slot - 1);
+            asm volatile("cp.async.wait_group %0;\n" ::"n"(kRing > 0 ? kRing - 1 : 0) : "memory");
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                nx[k].take(place(slot, k, false));
+                ng[k].take(place(slot, k, true));
+            }
+            if (++slot == kRing) slot = 0;
+        } else if constexpr (!kAhead) {
+            fetch(row);
+        }
         const float mu = nmean, r = nrstd;
+        if constexpr (kRing > 0) {
+            nmean = row + step < a.n ? __ldg(a.mean + row + step) : 0.f;
+            nrstd = row + step < a.n ? __ldg(a.rstd + row + step) : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            nx[k].values(xh[k]);
+            ng[k].values(gv[k]);
+        }
+        if constexpr (kAhead) fetch(row + step);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (k * LANES + lane) * V;
+            float w[V];
             if constexpr (kHold) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) xh[k][i] = nx[k][i], gv[k][i] = ng[k][i];
+                for (int i = 0; i < V; ++i) w[i] = gain[k * V + i];
             } else {
-                load_as<TYPE, V>(a.x, a.x_type, row * a.ldx + c, row < a.n ? a.d - c : 0, a.x_whole, xh[k]);
-                load_as<GTYPE, V>(a.g, a.g_type, row * a.ldg + c, row < a.n ? a.d - c : 0, a.g_whole, gv[k]);
+                staged<V>(gains + c, w);
             }
-        }
-        fetch(row + step);
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int c = (k * LANES + lane) * V;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const bool in = row < a.n && c + i < a.d;
@@ -250,10 +324,7 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads) norm_backward_k
                     dgain[k * V + i] = fmaf(gi, xh[k][i], dgain[k * V + i]);
                     doff[k * V + i] += gi;
                 }
-                float w;
-                if constexpr (kHold) w = gain[k * V + i];
-                else w = in && a.gain ? __ldg(a.gain + c + i) : 1.f;
-                gv[k][i] = gi * w;
+                gv[k][i] = gi * w[i];
                 sums[0] += gv[k][i];
                 sums[1] = fmaf(gv[k][i], xh[k][i], sums[1]);
             }
@@ -267,7 +338,7 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads) norm_backward_k
                 if (c >= a.d) break;
 #pragma unroll
                 for (int i = 0; i < V; ++i) gv[k][i] = (gv[k][i] - sa - xh[k][i] * sb) * r;
-                store_as<V>(a.gx, a.gx_type, row * a.ldgx + c, a.d - c, a.gx_whole, gv[k]);
+                store_steps<V>(a.gx, a.gx_type, row * a.ldgx + c, a.d - c, a.gx_step, gv[k]);
             }
         }
     }
@@ -336,12 +407,11 @@ __global__ void __launch_bounds__(1024) column_sums_kernel(const float* __restri
     }
 }
 
-// Blocks of the backward pass: two for every multiprocessor (a block of 256 threads and long rows fills half of it), or as many as
-// there are rows.
+// Blocks of the backward pass: `each` for every multiprocessor, or as many as there are rows.
 constexpr int kMaxParts = 512;
-int backward_blocks(int64_t n, int groups)
+int backward_blocks(int64_t n, int groups, int each)
 {
-    return (int)std::min<int64_t>(ceil_div(n, groups), std::min(kMaxParts, 2 * sm_count()));
+    return (int)std::min<int64_t>(ceil_div(n, groups), std::min(kMaxParts, each * sm_count()));
 }
 
 template <int TYPE, int V, int LANES, int NV>
@@ -349,8 +419,14 @@ cudaError_t launch_norm(cudaStream_t s, const NormArgs& a, int* launches)
 {
     constexpr int B = LANES > 32 ? LANES : kThreads;
     const int64_t blocks = std::min<int64_t>(ceil_div(a.n, B / LANES), (int64_t)sm_count() * (2048 / B));
+    auto* kernel = norm_kernel<TYPE, V, LANES, NV>;
+    constexpr size_t smem = NV * V <= 8 ? 0 : (size_t)2 * LANES * V * NV * sizeof(float);
+    if (smem > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
     ++*launches;
-    return launch_kernel(norm_kernel<TYPE, V, LANES, NV>, dim3((unsigned)blocks), dim3(B), 0, s, a);
+    return launch_kernel(kernel, dim3((unsigned)blocks), dim3(B), smem, s, a);
 }
 
 template <int TYPE, int V>
@@ -385,9 +461,10 @@ cudaError_t pick_norm_any(cudaStream_t s, const NormArgs& a, int* launches)
 template <int GTYPE, int TYPE, int V, int LANES, int NV>
 cudaError_t launch_back(cudaStream_t s, const NormBackArgs& a, float* g_gain, float* g_offset, int* launches)
 {
-    constexpr int B = LANES > 32 ? LANES : kThreads;
-    const int blocks = backward_blocks(a.n, B / LANES);
-    const size_t smem = a.part && (LANES <= 32 || LANES >= 1024) ? (size_t)2 * a.d * 4 : LANES >= 1024 ? (size_t)2 * a.d * 4 : 0;
+    using L = BackLayout<GTYPE, TYPE, V, LANES, NV>;
+    constexpr int B = L::B;
+    const size_t smem = L::smem(a.d);
+    const int blocks = backward_blocks(a.n, B / LANES, std::max(1, std::min(L::kBlocks, (int)(227 * 1024 / (smem + 1024)))));
     auto* kernel = norm_backward_kernel<GTYPE, TYPE, V, LANES, NV>;
     if (smem > 48 * 1024) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
@@ -447,15 +524,15 @@ size_t layer_norm_scratch_bytes(int d) { return (size_t)kMaxParts * 2 * (size_t)
 cudaError_t launch_layer_norm(cudaStream_t s, const void* x, int x_type, int64_t n, int d, int64_t ldx, const float* gain, const float* offset,
                               float eps, void* y, int y_type, int64_t ldy, float* mean, float* rstd, int* launches)
 {
-    NormArgs a = {x, x_type, ldx, n, d, true, true, gain, offset, eps, y, y_type, ldy, mean, rstd};
-    const auto fits = [&](int v) { return rows_whole(x, ldx, x_type, v) && rows_whole(y, ldy, y_type, v); };
-    if (fits(x_type == BIGCN_F32 ? 4 : 8)) {
+    NormArgs a = {x, x_type, ldx, n, d, rows_step(y, ldy, y_type, 8), gain, offset, eps, y, y_type, ldy, mean, rstd};
+    if (rows_whole(x, ldx, x_type, x_type == BIGCN_F32 ? 4 : 8)) {
         if (x_type == BIGCN_F32) return pick_norm<BIGCN_F32, 4>(s, a, launches);
         if (x_type == BIGCN_BF16) return pick_norm<BIGCN_BF16, 8>(s, a, launches);
         return pick_norm<BIGCN_F16, 8>(s, a, launches);
     }
-    if (fits(4)) return pick_norm_any<4>(s, a, launches);
-    if (fits(2)) return pick_norm_any<2>(s, a, launches);
+    const int step = rows_step(x, ldx, x_type, 4);
+    if (step == 4) return pick_norm_any<4>(s, a, launches);
+    if (step == 2) return pick_norm_any<2>(s, a, launches);
     return pick_norm_any<1>(s, a, launches);
 }
 
@@ -463,12 +540,13 @@ cudaError_t launch_layer_norm_backward(cudaStream_t s, const void* g, int g_type
                                        const float* gain, const float* mean, const float* rstd, void* gx, int gx_type, int64_t ldgx,
                                        float* g_gain, float* g_offset, void* scratch, int* launches)
 {
-    const NormBackArgs a = {g, g_type, ldg, x, x_type, ldx, n, d, true, true, true, gain, mean, rstd, gx, gx_type, ldgx,
+    const NormBackArgs a = {g, g_type, ldg, x, x_type, ldx, n, d, rows_step(gx, ldgx, gx_type, 8), gain, mean, rstd, gx, gx_type, ldgx,
                             g_gain || g_offset ? static_cast<float*>(scratch) : nullptr};
-    const auto fits = [&](int v) { return rows_whole(g, ldg, g_type, v) && rows_whole(x, ldx, x_type, v) && rows_whole(gx, ldgx, gx_type, v); };
-    if (!fits(x_type == BIGCN_F32 || g_type == BIGCN_F32 ? 4 : 8)) {
-        if (fits(4)) return pick_back_any<4>(s, a, g_gain, g_offset, launches);
-        if (fits(2)) return pick_back_any<2>(s, a, g_gain, g_offset, launches);
+    const int V = x_type == BIGCN_F32 || g_type == BIGCN_F32 ? 4 : 8;
+    if (!rows_whole(g, ldg, g_type, V) || !rows_whole(x, ldx, x_type, V)) {
+        const int step = std::min(rows_step(g, ldg, g_type, 4), rows_step(x, ldx, x_type, 4));
+        if (step == 4) return pick_back_any<4>(s, a, g_gain, g_offset, launches);
+        if (step == 2) return pick_back_any<2>(s, a, g_gain, g_offset, launches);
         return pick_back_any<1>(s, a, g_gain, g_offset, launches);
     }
     if (g_type == BIGCN_F32) return pick_back_x<BIGCN_F32>(s, x_type, a, g_gain, g_offset, launches);

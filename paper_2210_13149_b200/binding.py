@@ -135,6 +135,12 @@ def packed_stride_words(length: int) -> int:
     return int(load().bigcn_packed_stride_words(int(length)))
 
 
+def _dense(rows: int, cols: int, dtype: torch.dtype, device: torch.device) -> torch.Tensor:
+    if cols == 0:
+        return torch.empty_strided((rows,), (1,), dtype=dtype, device=device)
+    return torch.empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device)
+
+
 def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
@@ -472,11 +478,11 @@ class BiGCN:
             self._captured.append(self.workspace)
 
     def _outs(self, *wanted):
-        """Outputs' memory, in the order of the context's stream: (shape, dtype) each, or None."""
+        """Outputs' memory, in the order of the context's stream: (rows, columns or 0 for a vector, dtype) each, or None."""
         if torch._C._cuda_getCurrentRawStream(self.device.index) == self._raw_stream:
-            return [None if w is None else torch.empty(w[0], dtype=w[1], device=self.device) for w in wanted]
+            return [_dense(*w, self.device) if w else None for w in wanted]
         with torch.cuda.stream(self.stream):
-            return [None if w is None else torch.empty(w[0], dtype=w[1], device=self.device) for w in wanted]
+            return [_dense(*w, self.device) if w else None for w in wanted]
 
     def layer_norm(self, X: torch.Tensor, gain: Optional[torch.Tensor] = None, offset: Optional[torch.Tensor] = None,
                    eps: float = 1e-5, out_dtype: Optional[torch.dtype] = None):
@@ -488,8 +494,7 @@ class BiGCN:
         out_dtype = X.dtype if out_dtype is None else out_dtype
         if out_dtype not in (torch.float32, torch.bfloat16, torch.float16):
             raise ValueError("layer_norm: no output of type %s" % out_dtype)
-        Y, stats = self._outs(((n, d), out_dtype), ((2, n), torch.float32))
-        mean, rstd = stats.unbind(0)
+        Y, mean, rstd = self._outs((n, d, out_dtype), (n, 0, torch.float32), (n, 0, torch.float32))
         self._check(self.lib.bigcn_layer_norm(self.h, _ptr(X), TYPES[X.dtype], n, d, ldx, _ptr(gain), _ptr(offset), eps, _ptr(Y),
                                               TYPES[out_dtype], d, _ptr(mean), _ptr(rstd)))
         return Y, mean, rstd
@@ -507,8 +512,7 @@ class BiGCN:
         if out_dtype not in (torch.float32, torch.bfloat16, torch.float16):
             raise ValueError("layer_norm_backward: no output of type %s" % out_dtype)
         self._scratch(int(self.lib.bigcn_layer_norm_workspace_bytes(d)))
-        g_x, sums = self._outs(((n, d), out_dtype), ((2, d), torch.float32))
-        g_gain, g_offset = sums.unbind(0)
+        g_x, g_gain, g_offset = self._outs((n, d, out_dtype), (d, 0, torch.float32), (d, 0, torch.float32))
         self._check(self.lib.bigcn_layer_norm_backward(
             self.h, _ptr(g_y), TYPES[g_y.dtype], ldg, _ptr(X), TYPES[X.dtype], ldx, n, d, _ptr(gain), _ptr(mean), _ptr(rstd),
             _ptr(g_x), TYPES[out_dtype], d, _ptr(g_gain), _ptr(g_offset)))
@@ -526,7 +530,7 @@ class BiGCN:
         A negative label marks a row that takes no part."""
         ldx, ldw, n, d, classes = self._class_rows(X, W, labels)
         self._scratch(int(self.lib.bigcn_class_loss_workspace_bytes(n, d, classes, 0)))
-        loss, lse = self._outs((n, torch.float32), (n, torch.float32))
+        loss, lse = self._outs((n, 0, torch.float32), (n, 0, torch.float32))
         self._check(self.lib.bigcn_class_loss(self.h, _ptr(X), _ptr(W), TYPES[X.dtype], n, d, classes, ldx, ldw, _ptr(labels), _ptr(loss), _ptr(lse)))
         return loss, lse
 
@@ -537,7 +541,7 @@ class BiGCN:
         self._vector("lse", lse, n)
         self._vector("g_loss", g_loss, n)
         self._scratch(int(self.lib.bigcn_class_loss_workspace_bytes(n, d, classes, 1)))
-        g_x, g_w = self._outs(((n, d), X.dtype) if want_g_x else None, ((classes, d), X.dtype) if want_g_w else None)
+        g_x, g_w = self._outs((n, d, X.dtype) if want_g_x else None, (classes, d, X.dtype) if want_g_w else None)
         self._check(self.lib.bigcn_class_loss_backward(self.h, _ptr(X), _ptr(W), TYPES[X.dtype], n, d, classes, ldx, ldw, _ptr(labels), _ptr(lse),
                                                        _ptr(g_loss), _ptr(g_x), d, _ptr(g_w), d))
         return g_x, g_w
@@ -547,7 +551,7 @@ class BiGCN:
         ldx = self._rows("X", X)
         n, d = X.shape
         ldq = (d + 15) // 16 * 16
-        q, scale = self._outs(((n, ldq), torch.int8), (n, torch.float32))
+        q, scale = self._outs((n, ldq, torch.int8), (n, 0, torch.float32))
         if ldq != d:
             with torch.cuda.stream(self.stream):
                 q[:, d:] = 0
@@ -581,7 +585,7 @@ class BiGCN:
         self._vector("s_w", s_w, m)
         if out_dtype not in (torch.float32, torch.bfloat16, torch.float16):
             raise ValueError("quantized_product: no output of type %s" % out_dtype)
-        out, = self._outs(((n, m), out_dtype))
+        out, = self._outs((n, m, out_dtype))
         self._check(self.lib.bigcn_quantized_product(self.h, _ptr(X), TYPES[X.dtype], _ptr(s_x), n, d, ldx, _ptr(q_w), ldqw, _ptr(s_w), m,
                                                      _ptr(out), TYPES[out_dtype], m))
         return out

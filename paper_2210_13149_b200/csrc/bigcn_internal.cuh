@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "bigcn.h"
 
 namespace bigcn {
@@ -53,6 +55,23 @@ cudaError_t launch_kernel(void (*kernel)(P...), dim3 grid, dim3 block, size_t sm
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
+// Lets a kernel have `bytes` of dynamic shared memory, and all that a block can have beside its own, once per device (`done`: the devices,
+// by number; those past 63 each time).
+template <class K>
+cudaError_t allow_shared(K* kernel, size_t bytes, std::atomic<uint64_t>* done)
+{
+    if (bytes <= 48 * 1024) return cudaSuccess;
+    int device = 64;
+    cudaError_t e = cudaGetDevice(&device);
+    const uint64_t bit = device < 64 ? uint64_t(1) << device : 0;
+    if (e != cudaSuccess || (done->load(std::memory_order_relaxed) & bit)) return e;
+    cudaFuncAttributes own;
+    e = cudaFuncGetAttributes(&own, kernel);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - (int)own.sharedSizeBytes);
+    if (e == cudaSuccess) done->fetch_or(bit, std::memory_order_relaxed);
+    return e;
 }
 
 // ---- launchers (each returns the launch status; all asynchronous on `s`) ------------------------

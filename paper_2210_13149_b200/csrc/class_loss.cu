@@ -14,6 +14,7 @@
 // the others hold (NaN, infinities) reaches nothing and their work is not done.  How many there are is known on the GPU only; the
 // kernels read it there.
 #include <algorithm>
+#include <climits>
 
 #include "dense_gemm.cuh"
 #include "dense_types.cuh"
@@ -82,6 +83,10 @@ struct ListArgs {
     float* loss;             // nullable: 0 (NaN for a label that is no class) for the others
     float* lse;
     bool words;              // both on 16-byte boundaries
+    const float* of_lse;     // nullable: two values of every row,
+    const float* of_g_loss;
+    float* to_lse;           // [n] those of the labelled ones
+    float* to_g_loss;
 };
 __global__ void __launch_bounds__(1024) list_labels_kernel(const ListArgs a)
 {
@@ -115,6 +120,10 @@ __global__ void __launch_bounds__(1024) list_labels_kernel(const ListArgs a)
         if (in[i]) {
             a.kept[next] = (int)(at + i);
             a.label[next] = (int)v[i];
+            if (a.of_lse) {
+                a.to_lse[next] = __ldg(a.of_lse + at + i);
+                a.to_g_loss[next] = __ldg(a.of_g_loss + at + i);
+            }
             ++next;
         }
     }
@@ -163,7 +172,24 @@ __global__ void __launch_bounds__(256) gather_rows_kernel(const GatherArgs a)
         const int rows = (int)min((int64_t)a.span, a.n - row0);
         const int place = lane < rows ? __ldg(a.place + row0 + lane) : -1;
         const uint32_t kept = __ballot_sync(0xffffffffu, place >= 0);
-        for (uint32_t left = kept; left != 0u; left &= left - 1) {
+        uint32_t left = kept;
+        if (a.whole && rest == 0 && words <= 32) {            // rows of one word a lane: four of them on their way at a time
+            while (left != 0u) {
+                uint4 q[4];
+                int64_t to[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = __ffs(left) - 1;
+                    to[i] = left != 0u ? (int64_t)__shfl_sync(0xffffffffu, place, r) * a.ldt : -1;
+                    if (left != 0u && lane < words) q[i] = __ldg(reinterpret_cast<const uint4*>(a.x + (row0 + r) * a.ldx) + lane);
+                    left &= left - 1;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (to[i] >= 0 && lane < words) reinterpret_cast<uint4*>(a.to + to[i])[lane] = q[i];
+            }
+        }
+        for (; left != 0u; left &= left - 1) {
             const int r = __ffs(left) - 1;
             const uint16_t* from = a.x + (row0 + r) * a.ldx;
             uint16_t* to = a.to + (int64_t)__shfl_sync(0xffffffffu, place, r) * a.ldt;
@@ -178,7 +204,7 @@ __global__ void __launch_bounds__(256) gather_rows_kernel(const GatherArgs a)
             }
         }
         if (!a.g_x) continue;
-        for (uint32_t left = ~kept & (rows < 32 ? (1u << rows) - 1u : 0xffffffffu); left != 0u; left &= left - 1) {
+        for (left = ~kept & (rows < 32 ? (1u << rows) - 1u : 0xffffffffu); left != 0u; left &= left - 1) {
             uint16_t* to = a.g_x + (row0 + __ffs(left) - 1) * a.ldgx;
             if (a.g_whole) {
                 for (int w = lane; w < words; w += 32) reinterpret_cast<uint4*>(to)[w] = make_uint4(0u, 0u, 0u, 0u);
@@ -221,11 +247,14 @@ struct SumExp {
         int64_t rows;
         float* at;           // [rows]
     };
+    static __device__ int* flag() { return &g_loss_timeout; }
+    using Row = int;
+    static __device__ __forceinline__ Row row(const Args& a, int row, int rows) { return row < rows ? __ldg(a.label + row) : INT_MIN; }
     template <int BN, class Done>
-    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit& u, const gemm::Part& p, const Done& done)
+    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit& u, const gemm::Part& p, const Row& of_row, const Done& done)
     {
         const int row = p.row + (threadIdx.x & 31);
-        const int label = row < p.rows ? __ldg(a.label + row) - p.col : -1;
+        const int label = of_row >= p.col ? of_row - p.col : INT_MIN;          // far from any column, as the rows that are not there have it
         float m = -INFINITY, s = 0.f;
         gemm::each_chunk<BN>(p, sh.n, done, [&](int c, uint32_t (&v)[32]) {
             const int left = sh.n - (p.col + c);
@@ -243,12 +272,13 @@ struct SumExp {
             for (int i = 0; i < 32; ++i) s4[i & 3] += exp2_fast((__uint_as_float(v[i]) - t) * kLog2e);
             s = (s4[0] + s4[1]) + (s4[2] + s4[3]);
             m = top;
-            if ((unsigned)(label - c) < 32u) {
+            const unsigned in = (unsigned)label - (unsigned)c;
+            if (__any_sync(0xffffffffu, in < 32u)) {
                 float z = 0.f;
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
-                    if (label - c == i) z = __uint_as_float(v[i]);
-                a.at[row] = z;
+                    if (in == (unsigned)i) z = __uint_as_float(v[i]);
+                if (in < 32u) a.at[row] = z;
             }
         });
         // each warp's strip holds its own 32 pairs; those of the other three lie kStripBytes * 4 apart
@@ -273,31 +303,39 @@ struct SumExp {
 // G of a tile, rounded to the operands' type; zero past the last class and the last row, which pads the depth of what reads it.
 struct Gradient {
     struct Args {
-        const int* kept;
         const int* label;
-        const float* lse;    // of all rows
+        const float* lse;    // of the labelled rows
         const float* g_loss;
         int first_class;     // of the piece
         uint16_t* g;
         int64_t ldg;         // a multiple of 64
     };
-    template <int BN, class Done>
-    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit&, const gemm::Part& p, const Done& done)
+    static __device__ int* flag() { return &g_loss_timeout; }
+    struct Row {
+        int label;
+        float lse, weight;
+    };
+    static __device__ __forceinline__ Row row(const Args& a, int row, int rows)
     {
-        const int row = p.row + (threadIdx.x & 31);
-        const bool there = row < p.rows;
-        const int source = there ? __ldg(a.kept + row) : 0;
-        const int label = there ? __ldg(a.label + row) - a.first_class - p.col : -1;
-        const float lse = there ? __ldg(a.lse + source) : 0.f, weight = there ? __ldg(a.g_loss + source) : 0.f;
+        if (row >= rows) return {INT_MIN, 0.f, 0.f};
+        return {__ldg(a.label + row), __ldg(a.lse + row), __ldg(a.g_loss + row)};
+    }
+    template <int BN, class Done>
+    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit&, const gemm::Part& p, const Row& of_row, const Done& done)
+    {
+        const bool there = p.row + (int)(threadIdx.x & 31) < p.rows;
+        const int label = of_row.label >= a.first_class + p.col ? of_row.label - a.first_class - p.col : INT_MIN;
+        const float lse = of_row.lse, weight = of_row.weight;
         gemm::each_chunk<BN>(p, (int)a.ldg, done, [&](int c, uint32_t (&v)[32]) {
             const int left = sh.n - (p.col + c);
             float f[32];
 #pragma unroll
             for (int i = 0; i < 32; ++i) f[i] = exp2_fast((__uint_as_float(v[i]) - lse) * kLog2e);
-            if ((unsigned)(label - c) < 32u) {
+            const unsigned in = (unsigned)label - (unsigned)c;
+            if (__any_sync(0xffffffffu, in < 32u)) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
-                    if (label - c == i) f[i] -= 1.f;
+                    if (in == (unsigned)i) f[i] -= 1.f;
             }
             uint32_t w[16];
 #pragma unroll
@@ -326,12 +364,13 @@ struct Store {
         int64_t pitch, split_stride;
         bool add;            // parts: to what is there
     };
+    static __device__ int* flag() { return &g_loss_timeout; }
+    using Row = int;
+    static __device__ __forceinline__ Row row(const Args& a, int row, int rows) { return row < rows && a.map ? __ldg(a.map + row) : row; }
     template <int BN, class Done>
-    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit& u, const gemm::Part& p, const Done& done)
+    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit& u, const gemm::Part& p, const Row& mapped, const Done& done)
     {
         if (p.empty && a.part && a.add) return;
-        const int row = p.row + (threadIdx.x & 31);
-        const int mapped = row < p.rows && a.map ? __ldg(a.map + row) : row;
         gemm::each_chunk<BN>(p, sh.n, done, [&](int c, uint32_t (&v)[32]) {
             const int col = p.col + c;
             uint32_t w[16];
@@ -517,7 +556,7 @@ struct Plan {
     int64_t pitch;                            // of fp32 parts
     size_t bytes;
     // offsets
-    size_t kept, label, place, count, counts, x, w, at, part, g, px, pw;
+    size_t kept, label, place, count, counts, lse, g_loss, x, w, at, part, g, px, pw;
 };
 
 Plan make_plan(int64_t n, int d, int classes, bool backward, bool align_w)
@@ -533,6 +572,10 @@ Plan make_plan(int64_t n, int d, int classes, bool backward, bool align_w)
     p.kept = take((size_t)p.n_pad * 4);
     p.label = take((size_t)p.n_pad * 4);
     p.place = take((size_t)p.n_pad * 4);
+    if (backward) {
+        p.lse = take((size_t)p.n_pad * 4);
+        p.g_loss = take((size_t)p.n_pad * 4);
+    }
     p.x = take((size_t)p.n_pad * p.ldt * 2);
     if (align_w) p.w = take((size_t)classes * p.ldt * 2);
     if (!backward) {
@@ -571,7 +614,7 @@ struct Operands {
 
 // Lists the labelled rows, copies them together where that is needed, and lays the class matrix on 16-byte boundaries.
 cudaError_t prepare(cudaStream_t s, const Plan& p, char* ws, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n, int d, int classes,
-                    const int64_t* labels, float* loss, float* lse, void* g_x, int64_t ldgx, Operands* o, int* launches)
+                    const int64_t* labels, float* loss, float* lse, const float* of_lse, const float* of_g_loss, void* g_x, int64_t ldgx, Operands* o, int* launches)
 {
     int* counts = reinterpret_cast<int*>(ws + p.counts);
     const int blocks = (int)ceil_div(n, kScan);
@@ -583,7 +626,8 @@ cudaError_t prepare(cudaStream_t s, const Plan& p, char* ws, const void* x, int6
     }
     const ListArgs list = {labels, n, classes, counts, reinterpret_cast<int*>(ws + p.kept), reinterpret_cast<int*>(ws + p.label),
                            reinterpret_cast<int*>(ws + p.place), reinterpret_cast<int*>(ws + p.count), loss, lse,
-                           (reinterpret_cast<uintptr_t>(loss) | reinterpret_cast<uintptr_t>(lse)) % 16 == 0};
+                           (reinterpret_cast<uintptr_t>(loss) | reinterpret_cast<uintptr_t>(lse)) % 16 == 0, of_lse, of_g_loss,
+                           reinterpret_cast<float*>(ws + p.lse), reinterpret_cast<float*>(ws + p.g_loss)};
     ++*launches;
     e = launch_kernel(list_labels_kernel, dim3(blocks), dim3(1024), 0, s, list);
     if (e != cudaSuccess) return e;
@@ -622,7 +666,7 @@ cudaError_t row_maps(CUtensorMap* copied, CUtensorMap* own, const Plan& p, const
 
 template <int BN, int CTAS, class Epi>
 cudaError_t launch_logits(cudaStream_t s, const Plan& p, const Operands& o, int64_t n, int d, int classes, int64_t first_row, int64_t rows, int64_t first_class,
-                          const int* count, const typename Epi::Args& args, int* flag, int* launches)
+                          const int* count, const typename Epi::Args& args, int* launches)
 {
     CUtensorMap a, b, own;
     cudaError_t e = row_maps(&a, &own, p, o, n, d, first_row, 64, gemm::kRows);
@@ -637,26 +681,26 @@ cudaError_t launch_logits(cudaStream_t s, const Plan& p, const Operands& o, int6
     sh.base = (int)first_row;
     sh.alt_a = o.x_whole;
     ++*launches;
-    return gemm::launch<false, BN, CTAS, false, false, Epi>(s, a, b, own, sh, args, flag);
+    return gemm::launch<false, BN, CTAS, false, false, Epi>(s, a, b, own, sh, args);
 }
 template <class Epi>
 cudaError_t pick_logits(cudaStream_t s, int bn, const Plan& p, const Operands& o, int64_t n, int d, int classes, int64_t first_row, int64_t rows, int64_t first_class,
-                        const int* count, const typename Epi::Args& args, int* flag, int* launches)
+                        const int* count, const typename Epi::Args& args, int* launches)
 {
-    if (bn == 64) return launch_logits<64, 1, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, args, flag, launches);
-    if (bn == 128) return launch_logits<128, 1, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, args, flag, launches);
-    if (rows > gemm::kRows) return launch_logits<256, 2, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, args, flag, launches);
-    return launch_logits<256, 1, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, args, flag, launches);
+    if (bn == 64) return launch_logits<64, 1, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, args, launches);
+    if (bn == 128) return launch_logits<128, 1, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, args, launches);
+    if (rows > gemm::kRows) return launch_logits<256, 2, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, args, launches);
+    return launch_logits<256, 1, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, args, launches);
 }
 
 // g_x = G W (columns of W outside, its rows the depth) and g_w = G^T X.
 template <bool A_MN>
-cudaError_t launch_gradient(cudaStream_t s, int bn, const CUtensorMap& g, const CUtensorMap& b, const CUtensorMap& own, const gemm::Shape& sh, const Store::Args& args, int* flag)
+cudaError_t launch_gradient(cudaStream_t s, int bn, const CUtensorMap& g, const CUtensorMap& b, const CUtensorMap& own, const gemm::Shape& sh, const Store::Args& args)
 {
-    if (bn == 64) return gemm::launch<false, 64, 1, A_MN, true, Store>(s, g, b, own, sh, args, flag);
-    if (bn == 128) return gemm::launch<false, 128, 1, A_MN, true, Store>(s, g, b, own, sh, args, flag);
-    if (sh.m > gemm::kRows) return gemm::launch<false, 256, 2, A_MN, true, Store>(s, g, b, own, sh, args, flag);
-    return gemm::launch<false, 256, 1, A_MN, true, Store>(s, g, b, own, sh, args, flag);
+    if (bn == 64) return gemm::launch<false, 64, 1, A_MN, true, Store>(s, g, b, own, sh, args);
+    if (bn == 128) return gemm::launch<false, 128, 1, A_MN, true, Store>(s, g, b, own, sh, args);
+    if (sh.m > gemm::kRows) return gemm::launch<false, 256, 2, A_MN, true, Store>(s, g, b, own, sh, args);
+    return gemm::launch<false, 256, 1, A_MN, true, Store>(s, g, b, own, sh, args);
 }
 
 }  // namespace
@@ -674,12 +718,10 @@ cudaError_t launch_class_loss(cudaStream_t s, const void* x, int64_t ldx, const 
                               float* loss, float* lse, void* scratch, int* launches)
 {
     char* ws = static_cast<char*>(scratch);
-    int* flag = nullptr;
-    cudaError_t e = cudaGetSymbolAddress(reinterpret_cast<void**>(&flag), g_loss_timeout);
-    if (e != cudaSuccess) return e;
+    cudaError_t e;
     const Plan p = make_plan(n, d, classes, false, true);
     Operands o;
-    e = prepare(s, p, ws, x, ldx, w, ldw, n, d, classes, labels, loss, lse, nullptr, 0, &o, launches);
+    e = prepare(s, p, ws, x, ldx, w, ldw, n, d, classes, labels, loss, lse, nullptr, nullptr, nullptr, 0, &o, launches);
     const int* count = reinterpret_cast<const int*>(ws + p.count);
     const int* kept = reinterpret_cast<const int*>(ws + p.kept);
     float* at = reinterpret_cast<float*>(ws + p.at);
@@ -688,7 +730,7 @@ cudaError_t launch_class_loss(cudaStream_t s, const void* x, int64_t ldx, const 
         const int64_t first = r * p.rows, rows = std::min(p.rows, n - first);
         if (rows <= 0) break;
         const SumExp::Args args = {reinterpret_cast<const int*>(ws + p.label) + first, part, p.rows, at};
-        e = pick_logits<SumExp>(s, p.bn, p, o, n, d, classes, first, rows, 0, count, args, flag, launches);
+        e = pick_logits<SumExp>(s, p.bn, p, o, n, d, classes, first, rows, 0, count, args, launches);
         if (e != cudaSuccess) break;
         ++*launches;
         const auto blocks = [&](int rows_per_block) { return dim3((unsigned)std::min<int64_t>(ceil_div(rows, rows_per_block), 16 * sm_count())); };
@@ -704,12 +746,10 @@ cudaError_t launch_class_loss_backward(cudaStream_t s, const void* x, int64_t ld
                                        const float* lse, const float* g_loss, void* g_x, int64_t ldgx, void* g_w, int64_t ldgw, void* scratch, int* launches)
 {
     char* ws = static_cast<char*>(scratch);
-    int* flag = nullptr;
-    cudaError_t e = cudaGetSymbolAddress(reinterpret_cast<void**>(&flag), g_loss_timeout);
-    if (e != cudaSuccess) return e;
+    cudaError_t e;
     const Plan p = make_plan(n, d, classes, true, true);
     Operands o;
-    e = prepare(s, p, ws, x, ldx, w, ldw, n, d, classes, labels, nullptr, nullptr, g_x, ldgx, &o, launches);
+    e = prepare(s, p, ws, x, ldx, w, ldw, n, d, classes, labels, nullptr, nullptr, lse, g_loss, g_x, ldgx, &o, launches);
     const int* count = reinterpret_cast<const int*>(ws + p.count);
     const int* kept = reinterpret_cast<const int*>(ws + p.kept);
     const int* label = reinterpret_cast<const int*>(ws + p.label);
@@ -722,8 +762,8 @@ cudaError_t launch_class_loss_backward(cudaStream_t s, const void* x, int64_t ld
         for (int r = 0; r < p.row_pieces && e == cudaSuccess; ++r) {
             const int64_t first = r * p.rows, rows = std::min(p.rows, n - first);
             if (rows <= 0) break;
-            const Gradient::Args ga = {kept + first, label + first, lse, g_loss, (int)first_class, g, ldg};
-            e = pick_logits<Gradient>(s, tile_cols(here), p, o, n, d, here, first, rows, first_class, count, ga, flag, launches);
+            const Gradient::Args ga = {label + first, reinterpret_cast<const float*>(ws + p.lse) + first, reinterpret_cast<const float*>(ws + p.g_loss) + first, (int)first_class, g, ldg};
+            e = pick_logits<Gradient>(s, tile_cols(here), p, o, n, d, here, first, rows, first_class, count, ga, launches);
             if (e != cudaSuccess) break;
             gemm::Shape sh;
             sh.n = d;
@@ -741,7 +781,7 @@ cudaError_t launch_class_loss_backward(cudaStream_t s, const void* x, int64_t ld
                 const Store::Args args = {kept + first, static_cast<uint16_t*>(g_x), ldgx, rows_whole(g_x, ldgx, BIGCN_BF16, 8),
                                           parts_x ? reinterpret_cast<float*>(ws + p.px) + first * p.pitch : nullptr, p.pitch, p.n_pad * p.pitch, c > 0};
                 ++*launches;
-                e = launch_gradient<false>(s, p.bn_d, mg, mw, mw, sh, args, flag);
+                e = launch_gradient<false>(s, p.bn_d, mg, mw, mw, sh, args);
                 if (e == cudaSuccess && parts_x && c == p.col_pieces - 1) {
                     const FinishArgs fa = {args.part, p.splits_x, args.split_stride, p.pitch, count, (int)first, rows, d, kept + first, static_cast<uint16_t*>(g_x), ldgx, args.whole};
                     e = launch_finish(s, fa, launches);
@@ -762,7 +802,7 @@ cudaError_t launch_class_loss_backward(cudaStream_t s, const void* x, int64_t ld
                 const Store::Args args = {nullptr, out, ldgw, rows_whole(out, ldgw, BIGCN_BF16, 8), parts_w ? reinterpret_cast<float*>(ws + p.pw) : nullptr, p.pitch,
                                           round_up(p.cols, 128) * p.pitch, r > 0};
                 ++*launches;
-                e = launch_gradient<true>(s, p.bn_d, mg, mx, own, sh, args, flag);
+                e = launch_gradient<true>(s, p.bn_d, mg, mx, own, sh, args);
                 if (e == cudaSuccess && parts_w && r == p.row_pieces - 1) {
                     const FinishArgs fa = {args.part, p.splits_w, args.split_stride, p.pitch, nullptr, 0, here, d, nullptr, out, ldgw, args.whole};
                     e = launch_finish(s, fa, launches);

@@ -76,10 +76,10 @@ struct Walk {
     __device__ Unit at(int u) const
     {
         Unit r;
-        const int tiles = tiles_m * tiles_n;
+        const int tiles = max(1, tiles_m * tiles_n);
         r.split = u / tiles;
         const int t = u - r.split * tiles, band = t / (kBand * tiles_n), in = t - band * kBand * tiles_n;
-        const int rows = min(kBand, tiles_m - band * kBand);
+        const int rows = max(1, min(kBand, tiles_m - band * kBand));
         r.col = in / rows * tile_cols;
         r.row = (band * kBand + in % rows) * tile_rows;
         r.k0 = min(stages, r.split * per_split);
@@ -278,12 +278,17 @@ __device__ __forceinline__ void write_strip(unsigned char* strip, const uint32_t
     }
 }
 
-// Epi: struct with Args, and  template <int BN, class Done> static __device__ void tile(const Args&, const Shape&, const Unit&, const Part&,
-// const Done& done)  that the eight epilogue warps run; done() once the accumulators are read, unless they are empty.
+// Epi: struct with
+//   Args
+//   Row                            what it reads of a row (of the tile, a lane's)
+//   static __device__ Row row(const Args&, int row, int rows)                    fetched while the tile before is worked on
+//   template <int BN, class Done> static __device__ void tile(const Args&, const Shape&, const Unit&, const Part&, const Row&, const Done& done)
+//                                  run by the epilogue warps; done() once the accumulators are read, unless they are empty
+//   static __device__ int* flag()  raised when a wait ran out
 template <bool I8, int BN, int CTAS, bool A_MN, bool B_MN, class Epi>
 __global__ void __launch_bounds__(kThreads, 1)
 product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_alt,
-               const __grid_constant__ Shape shape, const __grid_constant__ typename Epi::Args args, int* flag)
+               const __grid_constant__ Shape shape, const __grid_constant__ typename Epi::Args args)
 {
     using C = Config<BN, CTAS>;
     constexpr int kDepth = I8 ? 128 : 64;
@@ -321,6 +326,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     tc::fence_after_sync();
     const uint32_t tmem = ctl.tmem;
     volatile int* abort = &ctl.abort;
+    int* const flag = Epi::flag();
 
     int early = 0;           // stages whose A is on its way
     if (CTAS == 1 && !A_MN && shape.a_ahead && threadIdx.x == kProducer * 32) {
@@ -435,8 +441,16 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     } else {
         int buf = 0;
         uint32_t acc_phase = 0;
+        const int own = (int)rank * kRows + (warp & 3) * 32;
+        Unit coming = walk.at(first < units ? first : 0);
+        typename Epi::Row ahead = Epi::row(args, first < units ? coming.row + own + lane : walk.m, walk.m);
         for (int u = first; u < units; u += step) {
-            const Unit t = walk.at(u);
+            const Unit t = coming;
+            const typename Epi::Row now = ahead;
+            if (u + step < units) {
+                coming = walk.at(u + step);
+                ahead = Epi::row(args, coming.row + own + lane, walk.m);
+            }
             const bool empty = t.k0 >= t.k1;
             if (!empty) {
                 // the four warps of the same rows go on or give up together: an epilogue may let them meet
@@ -444,14 +458,14 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 tc::fence_after_sync();
             }
             Part part;
-            part.row = t.row + (int)rank * kRows + (warp & 3) * 32;
+            part.row = t.row + own;
             part.rows = walk.m;
             part.col = t.col + (warp >> 2) * part_cols(BN);
             part.acc = tmem + (uint32_t)(buf * BN + (warp >> 2) * part_cols(BN)) + ((uint32_t)((warp & 3) * 32) << 16);
             part.empty = empty;
             part.there = (warp >> 2) * part_cols(BN) < BN;
             part.strip = stages + C::kStages * C::kStage + warp * kStripBytes;
-            Epi::template tile<BN>(args, shape, t, part, [&] {
+            Epi::template tile<BN>(args, shape, t, part, now, [&] {
                 tc::fence_before_sync();
                 __syncwarp();
                 if (lane == 0) arrive_first<CTAS>(&ctl.acc_empty[buf]);
@@ -476,11 +490,12 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 cudaError_t encode_map(CUtensorMap* map, const void* base, int elt, bool integers, int64_t rows, int64_t cols, int64_t pitch, int box_cols, int box_rows);
 
 template <bool I8, int BN, int CTAS, bool A_MN, bool B_MN, class Epi>
-cudaError_t launch(cudaStream_t s, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& alt, const Shape& shape, const typename Epi::Args& args, int* flag)
+cudaError_t launch(cudaStream_t s, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& alt, const Shape& shape, const typename Epi::Args& args)
 {
     using C = Config<BN, CTAS>;
     auto* kernel = product_kernel<I8, BN, CTAS, A_MN, B_MN, Epi>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
+    static std::atomic<uint64_t> ready{0};     // by device
+    const cudaError_t e = allow_shared(kernel, C::kSmem, &ready);
     if (e != cudaSuccess) return e;
     const int64_t units = ceil_div(shape.m, kRows * CTAS) * ceil_div(shape.n, BN) * shape.splits;
     const int clusters = (int)std::max<int64_t>(1, std::min<int64_t>(units, sm_count() / CTAS));
@@ -497,7 +512,7 @@ cudaError_t launch(cudaStream_t s, const CUtensorMap& a, const CUtensorMap& b, c
     cfg.stream = s;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kernel, a, b, alt, shape, args, flag);
+    return cudaLaunchKernelEx(&cfg, kernel, a, b, alt, shape, args);
 }
 
 }  // namespace gemm

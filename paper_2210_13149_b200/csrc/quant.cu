@@ -161,11 +161,13 @@ struct ScaledOut {
             });
         }
     }
+    static __device__ int* flag() { return &g_quant_timeout; }
+    using Row = float;
+    static __device__ __forceinline__ Row row(const Args& a, int row, int rows) { return row < rows ? __ldg(a.s_x + row) : 0.f; }
     template <int BN, class Done>
-    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit&, const gemm::Part& p, const Done& done)
+    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit&, const gemm::Part& p, const Row& sx, const Done& done)
     {
-        const int lane = threadIdx.x & 31, row = p.row + lane;
-        const float sx = row < p.rows ? __ldg(a.s_x + row) : 0.f;
+        const int lane = threadIdx.x & 31;
         // the warp's class scales are read by all lanes at once below: from L1 by then
         if (lane < gemm::part_cols(BN) / 32 && p.col + 32 * lane < sh.n) asm volatile("prefetch.global.L1 [%0];\n" ::"l"(a.s_w + p.col + 32 * lane));
         gemm::each_chunk<BN>(p, sh.n, done, [&](int c, uint32_t (&v)[32]) {
@@ -194,11 +196,13 @@ struct ScaledOut {
 // are stored together, and 128 class rows to a tile leave more tiles than 256 columns would.
 struct ScaledAcross {
     using Args = ScaledOut::Args;
+    static __device__ int* flag() { return &g_quant_timeout; }
+    using Row = float;
+    static __device__ __forceinline__ Row row(const Args& a, int row, int rows) { return row < rows ? __ldg(a.s_w + row) : 0.f; }
     template <int BN, class Done>
-    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit&, const gemm::Part& p, const Done& done)
+    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit&, const gemm::Part& p, const Row& sw, const Done& done)
     {
         const int k = p.row + (threadIdx.x & 31);
-        const float sw = k < p.rows ? __ldg(a.s_w + k) : 0.f;
         gemm::each_chunk<BN>(p, sh.n, done, [&](int c, uint32_t (&v)[32]) {
             if (k >= p.rows) return;
 #pragma unroll
@@ -213,23 +217,23 @@ struct ScaledAcross {
 };
 
 template <int BN, int CTAS>
-cudaError_t launch_product_as(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const int8_t* q_w, int64_t ldqw, const gemm::Shape& shape, const ScaledOut::Args& args, int* flag)
+cudaError_t launch_product_as(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const int8_t* q_w, int64_t ldqw, const gemm::Shape& shape, const ScaledOut::Args& args)
 {
     CUtensorMap ma, mb;
     cudaError_t e = gemm::encode_map(&ma, q_x, 1, true, shape.m, shape.k, ldqx, 128, gemm::kRows);
     if (e == cudaSuccess) e = gemm::encode_map(&mb, q_w, 1, true, shape.n, shape.k, ldqw, 128, BN / CTAS);
     if (e != cudaSuccess) return e;
-    return gemm::launch<true, BN, CTAS, false, false, ScaledOut>(s, ma, mb, ma, shape, args, flag);
+    return gemm::launch<true, BN, CTAS, false, false, ScaledOut>(s, ma, mb, ma, shape, args);
 }
 
 template <int BN>
-cudaError_t launch_across(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const int8_t* q_w, int64_t ldqw, const gemm::Shape& shape, const ScaledOut::Args& args, int* flag)
+cudaError_t launch_across(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const int8_t* q_w, int64_t ldqw, const gemm::Shape& shape, const ScaledOut::Args& args)
 {
     CUtensorMap ma, mb;
     cudaError_t e = gemm::encode_map(&ma, q_w, 1, true, shape.m, shape.k, ldqw, 128, gemm::kRows);
     if (e == cudaSuccess) e = gemm::encode_map(&mb, q_x, 1, true, shape.n, shape.k, ldqx, 128, BN);
     if (e != cudaSuccess) return e;
-    return gemm::launch<true, BN, 1, false, false, ScaledAcross>(s, ma, mb, ma, shape, args, flag);
+    return gemm::launch<true, BN, 1, false, false, ScaledAcross>(s, ma, mb, ma, shape, args);
 }
 
 }  // namespace
@@ -254,9 +258,6 @@ cudaError_t launch_quantize_rows(cudaStream_t s, const void* x, int type, int64_
 cudaError_t launch_quantized_product(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const float* s_x, int64_t n, int d, const int8_t* q_w, int64_t ldqw,
                                      const float* s_w, int m, void* out, int out_type, int64_t ldo, bool early, int* launches)
 {
-    int* flag = nullptr;
-    cudaError_t e = cudaGetSymbolAddress(reinterpret_cast<void**>(&flag), g_quant_timeout);
-    if (e != cudaSuccess) return e;
     const ScaledOut::Args args = {s_x, s_w, reinterpret_cast<uintptr_t>(s_w) % 16 == 0, out, out_type, ldo, rows_whole(out, ldo, out_type, 8)};
     gemm::Shape shape;
     shape.m = (int)n;
@@ -267,12 +268,12 @@ cudaError_t launch_quantized_product(cudaStream_t s, const int8_t* q_x, int64_t 
         shape.m = m;
         shape.n = (int)n;
         shape.a_ahead = early;
-        return launch_across<64>(s, q_x, ldqx, q_w, ldqw, shape, args, flag);
+        return launch_across<64>(s, q_x, ldqx, q_w, ldqw, shape, args);
     }
-    if (m <= 64) return launch_product_as<64, 1>(s, q_x, ldqx, q_w, ldqw, shape, args, flag);
-    if (m <= 128) return launch_product_as<128, 1>(s, q_x, ldqx, q_w, ldqw, shape, args, flag);
-    if (n > gemm::kRows) return launch_product_as<256, 2>(s, q_x, ldqx, q_w, ldqw, shape, args, flag);
-    return launch_product_as<256, 1>(s, q_x, ldqx, q_w, ldqw, shape, args, flag);
+    if (m <= 64) return launch_product_as<64, 1>(s, q_x, ldqx, q_w, ldqw, shape, args);
+    if (m <= 128) return launch_product_as<128, 1>(s, q_x, ldqx, q_w, ldqw, shape, args);
+    if (n > gemm::kRows) return launch_product_as<256, 2>(s, q_x, ldqx, q_w, ldqw, shape, args);
+    return launch_product_as<256, 1>(s, q_x, ldqx, q_w, ldqw, shape, args);
 }
 
 }  // namespace bigcn

@@ -421,10 +421,9 @@ cudaError_t launch_norm(cudaStream_t s, const NormArgs& a, int* launches)
     const int64_t blocks = std::min<int64_t>(ceil_div(a.n, B / LANES), (int64_t)sm_count() * (2048 / B));
     auto* kernel = norm_kernel<TYPE, V, LANES, NV>;
     constexpr size_t smem = NV * V <= 8 ? 0 : (size_t)2 * LANES * V * NV * sizeof(float);
-    if (smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return e;
-    }
+    static std::atomic<uint64_t> ready{0};     // by device
+    const cudaError_t e = allow_shared(kernel, smem, &ready);
+    if (e != cudaSuccess) return e;
     ++*launches;
     return launch_kernel(kernel, dim3((unsigned)blocks), dim3(B), smem, s, a);
 }
@@ -466,12 +465,11 @@ cudaError_t launch_back(cudaStream_t s, const NormBackArgs& a, float* g_gain, fl
     const size_t smem = L::smem(a.d);
     const int blocks = backward_blocks(a.n, B / LANES, std::max(1, std::min(L::kBlocks, (int)(227 * 1024 / (smem + 1024)))));
     auto* kernel = norm_backward_kernel<GTYPE, TYPE, V, LANES, NV>;
-    if (smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return e;
-    }
+    static std::atomic<uint64_t> ready{0};     // by device
+    cudaError_t e = allow_shared(kernel, smem, &ready);
+    if (e != cudaSuccess) return e;
     ++*launches;
-    cudaError_t e = launch_kernel(kernel, dim3((unsigned)blocks), dim3(B), smem, s, a);
+    e = launch_kernel(kernel, dim3((unsigned)blocks), dim3(B), smem, s, a);
     if (e == cudaSuccess && a.part) {
         ++*launches;
         e = launch_kernel(column_sums_kernel, dim3((unsigned)ceil_div(2 * a.d, 32)), dim3(1024), 0, s, (const float*)a.part, blocks, a.d, g_gain, g_offset);

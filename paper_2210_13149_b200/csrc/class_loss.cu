@@ -88,14 +88,37 @@ struct ListArgs {
     float* to_lse;           // [n] those of the labelled ones
     float* to_g_loss;
 };
-__global__ void __launch_bounds__(1024) list_labels_kernel(const ListArgs a)
+struct GatherArgs {
+    const uint16_t* x;
+    int64_t ldx, n;
+    int d;
+    bool whole;              // rows of x on 16-byte boundaries: where all are labelled they are read where they are
+    const int* place;
+    const int* count;
+    uint16_t* to;            // [n rounded up to 128] rows of ldt (a multiple of 8)
+    int64_t ldt;
+    uint16_t* g_x;           // nullable: rows without a label become zero
+    int64_t ldgx;
+    bool g_whole;
+    bool pairs;              // rows of x and of `to` can be moved in words of two elements
+    int span;                // rows of a warp at a time, at most 32
+};
+__device__ void gather_rows(const GatherArgs& a, int count, const int* places, int64_t first, int64_t warps);
+
+// kGather: at most kScan rows, whose listing every block does for itself (the first one writes it) before it gathers its share: one launch less.
+template <bool kGather>
+__global__ void __launch_bounds__(1024) list_labels_kernel(const ListArgs a, const GatherArgs gather)
 {
     pdl_enter();
     __shared__ int slot[32];
+    __shared__ int here[kGather ? kScan : 1];
+    __shared__ int total;
+    const int block = kGather ? 0 : blockIdx.x;
+    const bool write = !kGather || blockIdx.x == 0;
     int before = 0;
-    for (int b = threadIdx.x; b < (int)blockIdx.x; b += 1024) before += __ldg(a.counts + b);
-    before = gridDim.x > 1 ? block_sum(before, slot) : 0;
-    const int64_t at = ((int64_t)blockIdx.x * 1024 + threadIdx.x) * 4;
+    for (int b = threadIdx.x; b < block; b += 1024) before += __ldg(a.counts + b);
+    before = !kGather && gridDim.x > 1 ? block_sum(before, slot) : 0;
+    const int64_t at = ((int64_t)block * 1024 + threadIdx.x) * 4;
     int64_t v[4];
     bool in[4];
     read_labels(a.labels, a.n, a.classes, at, v, in);
@@ -118,19 +141,26 @@ __global__ void __launch_bounds__(1024) list_labels_kernel(const ListArgs a)
         places[i] = in[i] ? next : -1;
         none[i] = v[i] < 0 ? 0.f : __uint_as_float(0x7fc00000u);
         if (in[i]) {
-            a.kept[next] = (int)(at + i);
-            a.label[next] = (int)v[i];
-            if (a.of_lse) {
-                a.to_lse[next] = __ldg(a.of_lse + at + i);
-                a.to_g_loss[next] = __ldg(a.of_g_loss + at + i);
+            if (write) {
+                a.kept[next] = (int)(at + i);
+                a.label[next] = (int)v[i];
+                if (a.of_lse) {
+                    a.to_lse[next] = __ldg(a.of_lse + at + i);
+                    a.to_g_loss[next] = __ldg(a.of_g_loss + at + i);
+                }
             }
             ++next;
         }
     }
-    if (at + 4 <= a.n) *reinterpret_cast<int4*>(a.place + at) = make_int4(places[0], places[1], places[2], places[3]);
-    else
+    if constexpr (kGather) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) here[4 * threadIdx.x + i] = places[i];
+    } else if (at + 4 <= a.n) {
+        *reinterpret_cast<int4*>(a.place + at) = make_int4(places[0], places[1], places[2], places[3]);
+    } else {
         for (int i = 0; i < 4 && at + i < a.n; ++i) a.place[at + i] = places[i];
-    if (a.loss && mine < 4) {
+    }
+    if (write && a.loss && mine < 4) {
         if (mine == 0 && at + 4 <= a.n && a.words) {
             *reinterpret_cast<float4*>(a.loss + at) = make_float4(none[0], none[1], none[2], none[3]);
             *reinterpret_cast<float4*>(a.lse + at) = make_float4(none[0], none[1], none[2], none[3]);
@@ -140,37 +170,26 @@ __global__ void __launch_bounds__(1024) list_labels_kernel(const ListArgs a)
                 if (!in[i] && at + i < a.n) a.loss[at + i] = a.lse[at + i] = none[i];
         }
     }
-    if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 1023) *a.count = base + upto;
+    if (threadIdx.x == 1023) {
+        total = base + upto;
+        if (write && block == (kGather ? 0 : (int)gridDim.x - 1)) *a.count = base + upto;
+    }
+    if constexpr (kGather) {
+        __syncthreads();
+        gather_rows(gather, total, here, (int64_t)blockIdx.x * 32 + warp, (int64_t)gridDim.x * 32);
+    }
 }
 
-struct GatherArgs {
-    const uint16_t* x;
-    int64_t ldx, n;
-    int d;
-    bool whole;              // rows of x on 16-byte boundaries: where all are labelled they are read where they are
-    const int* place;
-    const int* count;
-    uint16_t* to;            // [n rounded up to 128] rows of ldt (a multiple of 8)
-    int64_t ldt;
-    uint16_t* g_x;           // nullable: rows without a label become zero
-    int64_t ldgx;
-    bool g_whole;
-    bool pairs;              // rows of x and of `to` can be moved in words of two elements
-    int span;                // rows of a warp at a time, at most 32
-};
 // A warp to `span` rows at a time, whose places its lanes read together: labelled rows are copied together, the gradient of the others is
 // zero; rows up to the next multiple of 128 are zero.
-__global__ void __launch_bounds__(256) gather_rows_kernel(const GatherArgs a)
+__device__ __forceinline__ void gather_rows(const GatherArgs& a, int count, const int* places, int64_t first, int64_t warps)
 {
-    pdl_enter();
     const int lane = threadIdx.x & 31;
-    const int count = __ldg(a.count);
     if (a.whole && count == a.n) return;
-    const int64_t warps = (int64_t)gridDim.x * 8, first = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     const int words = a.d / 8, rest = a.d - 8 * words;
     for (int64_t row0 = first * a.span; row0 < a.n; row0 += warps * a.span) {
         const int rows = (int)min((int64_t)a.span, a.n - row0);
-        const int place = lane < rows ? __ldg(a.place + row0 + lane) : -1;
+        const int place = lane < rows ? places[row0 + lane] : -1;
         const uint32_t kept = __ballot_sync(0xffffffffu, place >= 0);
         uint32_t left = kept;
         if (a.whole && rest == 0 && words <= 32) {            // rows of one word a lane: four of them on their way at a time
@@ -218,6 +237,11 @@ __global__ void __launch_bounds__(256) gather_rows_kernel(const GatherArgs a)
     for (int64_t row = count + first; row < end; row += warps)
         for (int i = lane; i < a.d; i += 32) a.to[row * a.ldt + i] = 0;
 }
+__global__ void __launch_bounds__(256) gather_rows_kernel(const GatherArgs a)
+{
+    pdl_enter();
+    gather_rows(a, __ldg(a.count), a.place, (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), (int64_t)gridDim.x * 8);
+}
 
 // Rows copied to 16-byte boundaries (a class matrix that does not start its rows there), in words of T where the rows allow it.
 template <class T>
@@ -245,7 +269,10 @@ struct SumExp {
         const int* label;    // of the rows
         float2* part;        // [column tiles][rows]
         int64_t rows;
-        float* at;           // [rows]
+        float* at;           // [rows] the label's z
+        const int* kept;     // one tile holds all columns: straight to the results (null otherwise)
+        float* loss;
+        float* lse;
     };
     static __device__ int* flag() { return &g_loss_timeout; }
     using Row = int;
@@ -255,7 +282,8 @@ struct SumExp {
     {
         const int row = p.row + (threadIdx.x & 31);
         const int label = of_row >= p.col ? of_row - p.col : INT_MIN;          // far from any column, as the rows that are not there have it
-        float m = -INFINITY, s = 0.f;
+        float m = -INFINITY, s = 0.f, at = 0.f;
+        bool mine = false;
         gemm::each_chunk<BN>(p, sh.n, done, [&](int c, uint32_t (&v)[32]) {
             const int left = sh.n - (p.col + c);
             if (left < 32) {
@@ -274,11 +302,10 @@ struct SumExp {
             m = top;
             const unsigned in = (unsigned)label - (unsigned)c;
             if (__any_sync(0xffffffffu, in < 32u)) {
-                float z = 0.f;
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
-                    if (in == (unsigned)i) z = __uint_as_float(v[i]);
-                if (in < 32u) a.at[row] = z;
+                    if (in == (unsigned)i) at = __uint_as_float(v[i]);
+                mine |= in < 32u;
             }
         });
         // each warp's strip holds its own 32 pairs; those of the other three lie kStripBytes * 4 apart
@@ -286,6 +313,10 @@ struct SumExp {
         unsigned char* const first = p.strip - (warp >> 2) * (4 * gemm::kStripBytes);
         gemm::meet(1 + (warp & 3), 32 * gemm::kColumnParts, true);
         if (warp >= 4) *reinterpret_cast<float2*>(p.strip + 8 * lane) = make_float2(m, s);
+        if (mine) {
+            if (a.kept) *reinterpret_cast<float*>(first + 256 + 4 * lane) = at;      // in the first warp's
+            else a.at[row] = at;
+        }
         gemm::meet(1 + (warp & 3), 32 * gemm::kColumnParts, true);
         if (warp < 4) {
 #pragma unroll
@@ -295,7 +326,14 @@ struct SumExp {
                 s = s * exp2_fast((m - t) * kLog2e) + q.y * exp2_fast((q.x - t) * kLog2e);
                 m = top;
             }
-            if (row < p.rows) a.part[(int64_t)(u.col / BN) * a.rows + row] = make_float2(m, s);
+            if (row < p.rows && a.kept) {
+                const int to = __ldg(a.kept + row);
+                const float l = logf(s);
+                a.loss[to] = (m - *reinterpret_cast<const float*>(first + 256 + 4 * lane)) + l;
+                a.lse[to] = m + l;
+            } else if (row < p.rows) {
+                a.part[(int64_t)(u.col / BN) * a.rows + row] = make_float2(m, s);
+            }
         }
     }
 };
@@ -528,8 +566,9 @@ size_t up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 
 int tile_cols(int columns) { return columns <= 64 ? 64 : columns <= 128 ? 128 : 256; }
 
-// How many parts a product's depth is split into, so that its tiles fill the machine: the fewest rounds of its multiprocessors (or pairs
-// of them), counted in whole products, of parts of at least 8 stages, where splitting must save a twentieth.
+// How many parts a product's depth is split into, so that its tiles fill the machine: what its rounds take, a stage of a pair's 256 x 256 tile
+// at 0.42 us and of a block's at 0.15 us (measured), and where it is split another 5 us for the kernel that adds the parts and their bytes, written
+// and read, at 5 TB/s.
 int pick_splits(int64_t rows, int64_t columns, int64_t stages, int most)
 {
     const int bn = tile_cols((int)columns);
@@ -537,10 +576,10 @@ int pick_splits(int64_t rows, int64_t columns, int64_t stages, int most)
     const int units = pairs ? 74 : 148;
     const int64_t tiles = ceil_div(rows, pairs ? 256 : 128) * ceil_div(columns, bn);
     int best = 1;
-    double cost = 1e30;
-    for (int s = 1; s <= most && (s == 1 || stages / s >= 8); ++s) {
-        const double c = (double)ceil_div(tiles * s, units) / s * (1.0 + 0.02 * s / most);
-        if (c < cost * 0.95) cost = c, best = s;
+    double least = 1e30;
+    for (int s = 1; s <= most && (s == 1 || stages / s >= 4); ++s) {
+        const double t = (double)ceil_div(tiles * s, units) * (double)ceil_div(stages, s) * (pairs ? 0.42 : 0.15) + (s > 1 ? 5.0 + 8.0 * s * (double)rows * (double)columns / 5e6 : 0.0);
+        if (t < least) least = t, best = s;
     }
     return best;
 }
@@ -580,11 +619,13 @@ Plan make_plan(int64_t n, int d, int classes, bool backward, bool align_w)
     if (align_w) p.w = take((size_t)classes * p.ldt * 2);
     if (!backward) {
         p.parts = (int)ceil_div(classes, p.bn);
-        p.rows = std::min(p.n_pad, std::max<int64_t>(2048, kPieceBytes / (8 * (int64_t)p.parts) / 128 * 128));
+        p.rows = p.parts == 1 ? p.n_pad : std::min(p.n_pad, std::max<int64_t>(2048, kPieceBytes / (8 * (int64_t)p.parts) / 128 * 128));
         p.row_pieces = (int)ceil_div(p.n_pad, p.rows);
         p.col_pieces = 1;
-        p.at = take((size_t)p.rows * 4);
-        p.part = take((size_t)p.rows * p.parts * 8);
+        if (p.parts > 1) {
+            p.at = take((size_t)p.rows * 4);
+            p.part = take((size_t)p.rows * p.parts * 8);
+        }
     } else {
         const int64_t all = round_up(classes, 64);
         p.rows = std::min(p.n_pad, std::max<int64_t>(16384, kPieceBytes / (2 * all) / 128 * 128));
@@ -628,15 +669,19 @@ cudaError_t prepare(cudaStream_t s, const Plan& p, char* ws, const void* x, int6
                            reinterpret_cast<int*>(ws + p.place), reinterpret_cast<int*>(ws + p.count), loss, lse,
                            (reinterpret_cast<uintptr_t>(loss) | reinterpret_cast<uintptr_t>(lse)) % 16 == 0, of_lse, of_g_loss,
                            reinterpret_cast<float*>(ws + p.lse), reinterpret_cast<float*>(ws + p.g_loss)};
-    ++*launches;
-    e = launch_kernel(list_labels_kernel, dim3(blocks), dim3(1024), 0, s, list);
-    if (e != cudaSuccess) return e;
     *o = {x, ldx, rows_whole(x, ldx, BIGCN_BF16, 8), reinterpret_cast<const uint16_t*>(ws + p.x), w, ldw};
     const int span = (int)std::max<int64_t>(1, std::min<int64_t>(32, n / (64 * sm_count())));     // as many warps as the machine holds, first
     const GatherArgs gather = {static_cast<const uint16_t*>(x), ldx, n, d, o->x_whole, list.place, list.count, reinterpret_cast<uint16_t*>(ws + p.x), p.ldt,
                                static_cast<uint16_t*>(g_x), ldgx, rows_whole(g_x, ldgx, BIGCN_BF16, 8), rows_whole(x, ldx, BIGCN_BF16, 2), span};
     ++*launches;
-    e = launch_kernel(gather_rows_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(n, 8 * span), 8 * sm_count())), dim3(256), 0, s, gather);
+    if (n <= kScan) {
+        e = launch_kernel(list_labels_kernel<true>, dim3((unsigned)std::min<int64_t>(ceil_div(n, 32), sm_count())), dim3(1024), 0, s, list, gather);
+    } else {
+        e = launch_kernel(list_labels_kernel<false>, dim3(blocks), dim3(1024), 0, s, list, gather);
+        if (e != cudaSuccess) return e;
+        ++*launches;
+        e = launch_kernel(gather_rows_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(n, 8 * span), 8 * sm_count())), dim3(256), 0, s, gather);
+    }
     if (e != cudaSuccess) return e;
     if (!rows_whole(w, ldw, BIGCN_BF16, 8)) {
         ++*launches;
@@ -729,9 +774,10 @@ cudaError_t launch_class_loss(cudaStream_t s, const void* x, int64_t ldx, const 
     for (int r = 0; r < p.row_pieces && e == cudaSuccess; ++r) {
         const int64_t first = r * p.rows, rows = std::min(p.rows, n - first);
         if (rows <= 0) break;
-        const SumExp::Args args = {reinterpret_cast<const int*>(ws + p.label) + first, part, p.rows, at};
+        const bool direct = p.parts == 1;
+        const SumExp::Args args = {reinterpret_cast<const int*>(ws + p.label) + first, part, p.rows, at, direct ? kept + first : nullptr, loss, lse};
         e = pick_logits<SumExp>(s, p.bn, p, o, n, d, classes, first, rows, 0, count, args, launches);
-        if (e != cudaSuccess) break;
+        if (e != cudaSuccess || direct) continue;
         ++*launches;
         const auto blocks = [&](int rows_per_block) { return dim3((unsigned)std::min<int64_t>(ceil_div(rows, rows_per_block), 16 * sm_count())); };
         // rows side by side where there are enough of them, else threads side by side over a row's parts

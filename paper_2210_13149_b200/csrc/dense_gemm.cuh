@@ -41,6 +41,7 @@ struct Shape {
     const int* count = nullptr;
     int of = 0, base = 0;
     bool over_depth = false, alt_a = false, alt_b = false;
+    int tile_rows = kRows;   // rows of a tile that count (a multiple of 8; the accumulators have 128), one block to a tile, K-major A
     bool a_ahead = false;    // A does not come from the kernel before this one (which let this one start early): its first stages are
                              // fetched while that one runs.  No count, one block to a tile.
 };
@@ -330,18 +331,19 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 
     int early = 0;           // stages whose A is on its way
     if (CTAS == 1 && !A_MN && shape.a_ahead && threadIdx.x == kProducer * 32) {
-        const Walk walk(shape, kRows, BN, kDepth);
+        const Walk walk(shape, shape.tile_rows, BN, kDepth);
         if ((int)blockIdx.x < walk.units()) {
             const Unit t = walk.at(blockIdx.x);
             early = min(t.k1 - t.k0, C::kStages);
             for (int i = 0; i < early; ++i) {
-                expect_bytes<CTAS>(&ctl.full[i], C::kStage);
+                expect_bytes<CTAS>(&ctl.full[i], shape.tile_rows * kDepthBytes + C::kBBytes);
                 copy_box<CTAS>(tc::smem_u32(stages + i * C::kStage), &map_a, (t.k0 + i) * kDepth, t.row, &ctl.full[i]);
             }
         }
     }
     pdl_enter();
-    const Walk walk(shape, kRows * CTAS, BN, kDepth);
+    const Walk walk(shape, CTAS == 1 && !A_MN ? shape.tile_rows : kRows * CTAS, BN, kDepth);
+    const uint32_t stage_bytes = (CTAS == 1 && !A_MN ? shape.tile_rows * kDepthBytes : C::kABytes) + C::kBBytes;
     const int units = walk.units(), first = blockIdx.x / CTAS, step = gridDim.x / CTAS;
 
     if (warp == kProducer) {
@@ -360,7 +362,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     ok = wait(&ctl.empty[slot], phase ^ 1u, abort, flag);
                     if (!ok) break;
                     const bool fetched = issued < early;
-                    if (rank == 0 && !fetched) expect_bytes<CTAS>(&ctl.full[slot], C::kStage * CTAS);
+                    if (rank == 0 && !fetched) expect_bytes<CTAS>(&ctl.full[slot], stage_bytes * CTAS);
                     const uint32_t sa = tc::smem_u32(stages + slot * C::kStage), sb = sa + C::kABytes;
                     if (fetched) {
                     } else if constexpr (A_MN) {
@@ -459,7 +461,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             }
             Part part;
             part.row = t.row + own;
-            part.rows = walk.m;
+            part.rows = CTAS == 1 ? min(walk.m, t.row + walk.tile_rows) : walk.m;
             part.col = t.col + (warp >> 2) * part_cols(BN);
             part.acc = tmem + (uint32_t)(buf * BN + (warp >> 2) * part_cols(BN)) + ((uint32_t)((warp & 3) * 32) << 16);
             part.empty = empty;
@@ -497,7 +499,7 @@ cudaError_t launch(cudaStream_t s, const CUtensorMap& a, const CUtensorMap& b, c
     static std::atomic<uint64_t> ready{0};     // by device
     const cudaError_t e = allow_shared(kernel, C::kSmem, &ready);
     if (e != cudaSuccess) return e;
-    const int64_t units = ceil_div(shape.m, kRows * CTAS) * ceil_div(shape.n, BN) * shape.splits;
+    const int64_t units = ceil_div(shape.m, CTAS == 1 && !A_MN ? shape.tile_rows : kRows * CTAS) * ceil_div(shape.n, BN) * shape.splits;
     const int clusters = (int)std::max<int64_t>(1, std::min<int64_t>(units, sm_count() / CTAS));
     cudaLaunchAttribute attr[2] = {};
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -152,11 +152,12 @@ template <int TYPE, int V>
 struct Raw {
     static constexpr int kWords = TYPE == kAnyType ? V : V * type_bytes(TYPE) / 4;
     uint32_t w[kWords];
-    __device__ __forceinline__ void load(const void* base, int type, int64_t at, int count)
+    // of a type looked up: `whole` as in load_elts(); of a known type the address is aligned to the 16 (or 8) bytes
+    __device__ __forceinline__ void load(const void* base, int type, int64_t at, int count, bool whole = true)
     {
         if constexpr (TYPE == kAnyType) {
             float f[V];
-            load_as<TYPE, V>(base, type, at, count, true, f);
+            load_as<TYPE, V>(base, type, at, count, whole, f);
 #pragma unroll
             for (int i = 0; i < V; ++i) w[i] = __float_as_uint(f[i]);
         } else if (count >= V) {

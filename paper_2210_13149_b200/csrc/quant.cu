@@ -6,6 +6,8 @@
 // The integers are exact: the sum of 16,384 products of 127 stays below 2^31.  The three roundings of an output (the sum to fp32, and
 // two products) are fp32's, then one to the output's type.  The scales are multiplied first: a row with fp32's lowest value in it has a
 // scale of 2^121, which times the sum would overflow where the output does not.
+#include <climits>
+
 #include "dense_gemm.cuh"
 #include "dense_types.cuh"
 
@@ -19,9 +21,10 @@ __device__ int g_quant_timeout;               // set when a wait ran out
 
 struct QuantArgs {
     const void* x;
+    int type;
     int64_t ldx, n;
     int d;
-    bool whole;
+    bool whole;              // kAnyType: rows start on boundaries of four elements
     int8_t* q;
     int64_t ldq;
     float* scale;
@@ -50,75 +53,97 @@ __device__ __forceinline__ uint32_t nearest4(const float* x, float factor, float
     return __byte_perm(__byte_perm(n[0], n[1], 0x0040), __byte_perm(n[2], n[3], 0x0040), 0x5410);
 }
 
-// One row to LANES threads (a warp or a block), V values at a time, NV times.
-template <int TYPE, int V, int LANES, int NV>
+// ROWS rows to LANES threads (a warp or a block), V values at a time, NV times: all of them are on their way before the first is looked at.
+template <int TYPE, int V, int LANES, int NV, int ROWS>
 __global__ void __launch_bounds__(LANES > 32 ? LANES : 256) quantize_kernel(const QuantArgs a)
 {
     pdl_enter();
     if (a.early) asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     constexpr int B = LANES > 32 ? LANES : 256, GROUPS = B / LANES;
-    __shared__ uint32_t slot[LANES > 32 ? LANES / 32 : 1];
+    __shared__ uint32_t slot[ROWS][LANES > 32 ? LANES / 32 : 1];
     const int lane = threadIdx.x % LANES;
-    const int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES;
-    const auto* x = static_cast<const typename Elt<TYPE>::T*>(a.x) + row * a.ldx;
-    float v[NV][V];
-    uint32_t top = 0u;                        // as bits, which order magnitudes, infinity and NaN
+    const int64_t row0 = ((int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES) * ROWS;
+    Raw<TYPE, V> w[ROWS][NV];
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const int c = (k * LANES + lane) * V;
-        load_elts<TYPE, V>(x + c, row < a.n ? a.d - c : 0, a.whole, v[k]);
+    for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-        for (int i = 0; i < V; ++i) top = max(top, __float_as_uint(v[k][i]) & 0x7fffffffu);
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * LANES + lane) * V;
+            w[r][k].load(a.x, a.type, (row0 + r) * a.ldx + c, row0 + r < a.n ? a.d - c : 0, a.whole);
+        }
+    uint32_t tops[ROWS];                      // as bits, which order magnitudes, infinity and NaN
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        uint32_t top = 0u;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            float v[V];
+            w[r][k].values(v);
+#pragma unroll
+            for (int i = 0; i < V; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+        }
+        tops[r] = __reduce_max_sync(0xffffffffu, top);
+        if (LANES > 32 && (threadIdx.x & 31) == 0) slot[r][threadIdx.x >> 5] = tops[r];
     }
-    top = __reduce_max_sync(0xffffffffu, top);
     if constexpr (LANES > 32) {
-        if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = top;
         __syncthreads();
-        top = (threadIdx.x & 31) < LANES / 32 ? slot[threadIdx.x & 31] : 0u;
-        top = __reduce_max_sync(0xffffffffu, top);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) tops[r] = __reduce_max_sync(0xffffffffu, (threadIdx.x & 31) < LANES / 32 ? slot[r][threadIdx.x & 31] : 0u);
     }
-    if (row >= a.n) return;
-    const bool finite = top < 0x7f800000u;
-    const float t = __uint_as_float(top), factor = 127.f / t;
-    const bool tiny = t < 1e-30f;             // 127 / t would overflow
-    if (lane == 0) a.scale[row] = finite ? t / 127.f : __uint_as_float(0x7fc00000u);
-    int8_t* q = a.q + row * a.ldq;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const int c = (k * LANES + lane) * V;
-        if (c >= a.d) break;
-        uint32_t w[V / 4];
+    for (int r = 0; r < ROWS; ++r) {
+        const int64_t row = row0 + r;
+        if (row >= a.n) return;
+        const uint32_t top = tops[r];
+        const bool finite = top < 0x7f800000u;
+        const float t = __uint_as_float(top), factor = 127.f / t;
+        const bool tiny = t < 1e-30f;         // 127 / t would overflow
+        if (lane == 0) a.scale[row] = finite ? t / 127.f : __uint_as_float(0x7fc00000u);
+        int8_t* q = a.q + row * a.ldq;
 #pragma unroll
-        for (int j = 0; j < V / 4; ++j) w[j] = finite && top ? nearest4(&v[k][4 * j], factor, t, tiny) : 0u;
-        if (c + V <= a.d) {                   // rows of q start on 16-byte boundaries
-            if constexpr (V == 4) *reinterpret_cast<uint32_t*>(q + c) = w[0];
-            else *reinterpret_cast<uint2*>(q + c) = make_uint2(w[0], w[1]);
-        } else {
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * LANES + lane) * V;
+            if (c >= a.d) break;
+            float v[V];
+            w[r][k].values(v);
+            uint32_t o[V / 4];
 #pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (c + i < a.d) q[c + i] = (int8_t)(w[i >> 2] >> (8 * (i & 3)));
+            for (int j = 0; j < V / 4; ++j) o[j] = finite && top ? nearest4(v + 4 * j, factor, t, tiny) : 0u;
+            if (c + V <= a.d) {               // rows of q start on 16-byte boundaries
+                if constexpr (V == 4) *reinterpret_cast<uint32_t*>(q + c) = o[0];
+                else *reinterpret_cast<uint2*>(q + c) = make_uint2(o[0], o[1]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (c + i < a.d) q[c + i] = (int8_t)(o[i >> 2] >> (8 * (i & 3)));
+            }
         }
     }
 }
 
-template <int TYPE, int V, int LANES, int NV>
+template <int TYPE, int V, int LANES, int NV, int ROWS>
 cudaError_t launch_quantize_as(cudaStream_t s, const QuantArgs& a, int* launches)
 {
     constexpr int B = LANES > 32 ? LANES : 256;
     ++*launches;
-    return launch_kernel(quantize_kernel<TYPE, V, LANES, NV>, dim3((unsigned)ceil_div(a.n, B / LANES)), dim3(B), 0, s, a);
+    return launch_kernel(quantize_kernel<TYPE, V, LANES, NV, ROWS>, dim3((unsigned)ceil_div(a.n, B / LANES * ROWS)), dim3(B), 0, s, a);
 }
+// A warp to a row, or to several short ones, as long as that leaves the machine enough warps; else a block.  16,384 bf16 rows of 2,048
+// in us: 40 with blocks of 128 threads, N2 with warps; 169,343 fp32 rows of 256: 53 with a row to a warp, N3 with four.
 template <int TYPE, int V>
 cudaError_t pick_quantize(cudaStream_t s, const QuantArgs& a, int* launches)
 {
     constexpr int Q = 16 / V;
     const int64_t words = ceil_div(a.d, V);
-    if (words <= 32) return launch_quantize_as<TYPE, V, 32, 1>(s, a, launches);
-    if (words <= 64) return launch_quantize_as<TYPE, V, 32, 2>(s, a, launches);
-    if (words <= 32 * Q) return launch_quantize_as<TYPE, V, 32, Q>(s, a, launches);
-    if (words <= 128 * Q) return launch_quantize_as<TYPE, V, 128, Q>(s, a, launches);
-    if (words <= 512 * Q) return launch_quantize_as<TYPE, V, 512, Q>(s, a, launches);
-    return launch_quantize_as<TYPE, V, 1024, Q>(s, a, launches);
+    const bool many = a.n >= 8192;
+    if (words <= 32) return many ? launch_quantize_as<TYPE, V, 32, 1, 4>(s, a, launches) : launch_quantize_as<TYPE, V, 32, 1, 1>(s, a, launches);
+    if (words <= 64) return many ? launch_quantize_as<TYPE, V, 32, 2, 4>(s, a, launches) : launch_quantize_as<TYPE, V, 32, 2, 1>(s, a, launches);
+    if (many && words <= 128) return launch_quantize_as<TYPE, V, 32, 4, 2>(s, a, launches);
+    if (many && words <= 256) return launch_quantize_as<TYPE, V, 32, 8, 1>(s, a, launches);
+    if (words <= 32 * Q) return launch_quantize_as<TYPE, V, 32, Q, 1>(s, a, launches);
+    if (words <= 128 * Q) return launch_quantize_as<TYPE, V, 128, Q, 1>(s, a, launches);
+    if (words <= 512 * Q) return launch_quantize_as<TYPE, V, 512, Q, 1>(s, a, launches);
+    return launch_quantize_as<TYPE, V, 1024, Q, 1>(s, a, launches);
 }
 
 // Epilogue: the sums times both scales, in the output's type.
@@ -216,6 +241,111 @@ struct ScaledAcross {
     }
 };
 
+// One to four rows, not yet quantised, in one launch.  Every block quantises them for itself into shared memory (their bytes times the number of
+// blocks come from L2 and are few) while its first class rows are on their way; then a warp takes kGemvRows class rows at a time, 16 bytes of each a
+// lane, and sums by four-byte dot products.  Bound by the class rows, which are read once: 65,536 classes x 1,024 for one row in us: 19.5 by two
+// kernels with tensor memory to set up, N4 so; the dot products of more than four rows would cost more than that saves.
+constexpr int kGemvThreads = 512, kGemvRows = 4, kGemvMax = 4, kGemvBytes = 64 * 1024;
+struct GemvArgs {
+    const void* x;
+    int type;
+    int64_t ldx;
+    int n, d;
+    bool whole;
+    const int8_t* q_w;
+    int64_t ldqw;
+    const float* s_w;
+    int m;
+    void* out;
+    int out_type;
+    int64_t ldo;
+};
+template <int N>
+__global__ void __launch_bounds__(kGemvThreads, 2) few_rows_kernel(const GemvArgs a)
+{
+    pdl_enter();
+    extern __shared__ uint4 qs[];             // [N][words] the quantised rows
+    __shared__ uint32_t slot[kGemvThreads / 32];
+    __shared__ float scales[N];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, words = (a.d + 15) / 16;
+    const int warps = gridDim.x * (kGemvThreads / 32);
+    int k = (blockIdx.x * (kGemvThreads / 32) + warp) * kGemvRows;
+    uint4 w[kGemvRows];
+    auto fetch = [&](int at, int word) {
+#pragma unroll
+        for (int j = 0; j < kGemvRows; ++j)
+            w[j] = word < words && at + j < a.m ? __ldg(reinterpret_cast<const uint4*>(a.q_w + (int64_t)(at + j) * a.ldqw) + word) : make_uint4(0u, 0u, 0u, 0u);
+    };
+    fetch(k, lane);
+    for (int r = 0; r < N; ++r) {
+        const int64_t row = (int64_t)r * a.ldx;
+        uint32_t top = 0u;
+        for (int c = threadIdx.x * 4; c < a.d; c += kGemvThreads * 4) {
+            float v[4];
+            load_as<kAnyType, 4>(a.x, a.type, row + c, r < a.n ? a.d - c : 0, a.whole, v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+        }
+        top = __reduce_max_sync(0xffffffffu, top);
+        __syncthreads();
+        if (lane == 0) slot[warp] = top;
+        __syncthreads();
+        top = __reduce_max_sync(0xffffffffu, lane < kGemvThreads / 32 ? slot[lane] : 0u);
+        const bool finite = top < 0x7f800000u;
+        const float t = __uint_as_float(top), factor = 127.f / t;
+        if (threadIdx.x == 0) scales[r] = finite ? t / 127.f : __uint_as_float(0x7fc00000u);
+        uint32_t* q = reinterpret_cast<uint32_t*>(qs + r * words);
+        for (int c = threadIdx.x * 4; c < words * 16; c += kGemvThreads * 4) {
+            float v[4];
+            load_as<kAnyType, 4>(a.x, a.type, row + c, r < a.n ? a.d - c : 0, a.whole, v);
+            q[c / 4] = finite && top ? nearest4(v, factor, t, t < 1e-30f) : 0u;
+        }
+    }
+    __syncthreads();
+    for (; k < a.m; k += warps * kGemvRows) {
+        int sum[kGemvRows][N] = {};
+        for (int word = lane; word < words; word += 32) {
+            uint4 now[kGemvRows];
+#pragma unroll
+            for (int j = 0; j < kGemvRows; ++j) now[j] = w[j];
+            // the lane's next word of these rows, or its first of the next ones
+            if (word + 32 < words) fetch(k, word + 32);
+            else fetch(k + warps * kGemvRows, lane);
+#pragma unroll
+            for (int r = 0; r < N; ++r) {
+                const uint4 x = qs[r * words + word];
+#pragma unroll
+                for (int j = 0; j < kGemvRows; ++j) {
+                    sum[j][r] = __dp4a((int)now[j].x, (int)x.x, sum[j][r]);
+                    sum[j][r] = __dp4a((int)now[j].y, (int)x.y, sum[j][r]);
+                    sum[j][r] = __dp4a((int)now[j].z, (int)x.z, sum[j][r]);
+                    sum[j][r] = __dp4a((int)now[j].w, (int)x.w, sum[j][r]);
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kGemvRows; ++j)
+#pragma unroll
+            for (int r = 0; r < N; ++r) {
+                const int total = __reduce_add_sync(0xffffffffu, sum[j][r]);
+                if (lane == j * N + r && k + j < a.m && r < a.n) {
+                    const float f[1] = {(float)total * (scales[r] * __ldg(a.s_w + k + j))};
+                    store_as<1>(a.out, a.out_type, (int64_t)r * a.ldo + k + j, 1, true, f);
+                }
+            }
+    }
+}
+template <int N>
+cudaError_t launch_few_rows(cudaStream_t s, const GemvArgs& a)
+{
+    const size_t smem = (size_t)N * ((a.d + 15) / 16) * 16;
+    static std::atomic<uint64_t> ready{0};    // by device
+    const cudaError_t e = allow_shared(few_rows_kernel<N>, smem, &ready);
+    if (e != cudaSuccess) return e;
+    const int64_t blocks = std::min<int64_t>(2 * sm_count(), ceil_div(a.m, kGemvThreads / 32 * kGemvRows));
+    return launch_kernel(few_rows_kernel<N>, dim3((unsigned)blocks), dim3(kGemvThreads), smem, s, a);
+}
+
 template <int BN, int CTAS>
 cudaError_t launch_product_as(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const int8_t* q_w, int64_t ldqw, const gemm::Shape& shape, const ScaledOut::Args& args)
 {
@@ -230,7 +360,7 @@ template <int BN>
 cudaError_t launch_across(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const int8_t* q_w, int64_t ldqw, const gemm::Shape& shape, const ScaledOut::Args& args)
 {
     CUtensorMap ma, mb;
-    cudaError_t e = gemm::encode_map(&ma, q_w, 1, true, shape.m, shape.k, ldqw, 128, gemm::kRows);
+    cudaError_t e = gemm::encode_map(&ma, q_w, 1, true, shape.m, shape.k, ldqw, 128, shape.tile_rows);
     if (e == cudaSuccess) e = gemm::encode_map(&mb, q_x, 1, true, shape.n, shape.k, ldqx, 128, BN);
     if (e != cudaSuccess) return e;
     return gemm::launch<true, BN, 1, false, false, ScaledAcross>(s, ma, mb, ma, shape, args);
@@ -245,11 +375,21 @@ int quant_timeouts()
     return v;
 }
 
+bool few_rows_covers(int64_t n, int d) { return n <= kGemvMax && n * round_up(d, 16) <= kGemvBytes; }
+cudaError_t launch_few_rows_product(cudaStream_t s, const void* x, int type, int64_t ldx, int64_t n, int d, const int8_t* q_w, int64_t ldqw, const float* s_w, int m,
+                                    void* out, int out_type, int64_t ldo, int* launches)
+{
+    const GemvArgs a = {x, type, ldx, (int)n, d, rows_whole(x, ldx, type, 4), q_w, ldqw, s_w, m, out, out_type, ldo};
+    ++*launches;
+    return n == 1 ? launch_few_rows<1>(s, a) : n == 2 ? launch_few_rows<2>(s, a) : launch_few_rows<4>(s, a);
+}
+
 bool quantized_across(int64_t n, int m) { return n <= 64 && m > 64; }
 
 cudaError_t launch_quantize_rows(cudaStream_t s, const void* x, int type, int64_t n, int d, int64_t ldx, int8_t* q, int64_t ldq, float* scale, bool early, int* launches)
 {
-    const QuantArgs a = {x, ldx, n, d, rows_whole(x, ldx, type, type == BIGCN_F32 ? 4 : 8), q, ldq, scale, early};
+    const QuantArgs a = {x, type, ldx, n, d, rows_whole(x, ldx, type, 4), q, ldq, scale, early};
+    if (!rows_whole(x, ldx, type, type == BIGCN_F32 ? 4 : 8)) return pick_quantize<kAnyType, 4>(s, a, launches);
     if (type == BIGCN_F32) return pick_quantize<BIGCN_F32, 4>(s, a, launches);
     if (type == BIGCN_BF16) return pick_quantize<BIGCN_BF16, 8>(s, a, launches);
     return pick_quantize<BIGCN_F16, 8>(s, a, launches);
@@ -268,6 +408,12 @@ cudaError_t launch_quantized_product(cudaStream_t s, const int8_t* q_x, int64_t 
         shape.m = m;
         shape.n = (int)n;
         shape.a_ahead = early;
+        // a height of the tiles with which the last round of the multiprocessors is full, or nearly so: a round costs its rows, and some 16 more
+        int64_t least = INT64_MAX;
+        for (int r = 128; r >= 64; r -= 8) {
+            const int64_t cost = ceil_div(ceil_div(m, r), sm_count()) * (r + 16);
+            if (cost < least) least = cost, shape.tile_rows = r;
+        }
         return launch_across<64>(s, q_x, ldqx, q_w, ldqw, shape, args);
     }
     if (m <= 64) return launch_product_as<64, 1>(s, q_x, ldqx, q_w, ldqw, shape, args);

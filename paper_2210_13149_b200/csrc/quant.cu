@@ -31,10 +31,23 @@ struct QuantArgs {
     bool early;              // the next kernel may start: it waits for this one where it reads what this one writes
 };
 
-// Four values as the integers nearest to 127 x / top, in the bytes of a word.  In fp32 the quotient is off by 127 * 3 * 2^-24 at
-// most; where that could decide one of the roundings, they are taken in 64 bits, where 127 x is exact and a quotient halfway between integers
-// cannot be met or missed by its rounding: with x and top of 24 bits it is halfway, or at least 2^-32 of its size away from it.  The sum with
-// 1.5 * 2^23 rounds to the integer and holds it in its low bits.
+// Four values as the integers nearest to 127 x / top, in the bytes of a word.  The sum with 1.5 * 2^23 rounds x (127 / top) to an integer and holds it
+// in its low bits; the quotient in it is off by 127 * 2^-23 at most (the factor's rounding, and the sum's own at the border).  Where that
+// could decide one of the roundings, they are taken exactly: of 16-bit types in fp32, where 127 x is exact and a quotient is halfway between
+// integers or at least 2^-20 of its size away, so that its one rounding neither meets nor misses that; of fp32 in 64 bits, where the
+// same holds with 2^-32.
+template <bool HALF>
+__device__ __noinline__ uint32_t nearest4_exactly(float4 x, float top)
+{
+    const float v[4] = {x.x, x.y, x.z, x.w};
+    uint32_t n[4];
+    const float down = HALF && top > 1e30f ? 0x1p-10f : 1.f;                 // 127 x would overflow
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        n[i] = HALF ? (uint32_t)(int)rintf(__fdiv_rn(127.f * (v[i] * down), top * down)) : (uint32_t)(int)rint(127.0 * (double)v[i] / (double)top);
+    return __byte_perm(__byte_perm(n[0], n[1], 0x0040), __byte_perm(n[2], n[3], 0x0040), 0x5410);
+}
+template <bool HALF>
 __device__ __forceinline__ uint32_t nearest4(const float* x, float factor, float top, bool tiny)
 {
     constexpr float kRound = 12582912.f;
@@ -42,59 +55,55 @@ __device__ __forceinline__ uint32_t nearest4(const float* x, float factor, float
     float off = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float t = x[i] * factor, r = t + kRound;
+        const float r = fmaf(x[i], factor, kRound);
         n[i] = __float_as_uint(r);
-        off = fmaxf(off, fabsf(t - (r - kRound)));
+        off = fmaxf(off, fabsf(fmaf(x[i], factor, kRound - r)));
     }
-    if (tiny || off > 0.4999f) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) n[i] = (uint32_t)(int)rint(127.0 * (double)x[i] / (double)top);
-    }
+    if (tiny || off > 0.49998f) return nearest4_exactly<HALF>(make_float4(x[0], x[1], x[2], x[3]), top);
     return __byte_perm(__byte_perm(n[0], n[1], 0x0040), __byte_perm(n[2], n[3], 0x0040), 0x5410);
 }
 
-// ROWS rows to LANES threads (a warp or a block), V values at a time, NV times: all of them are on their way before the first is looked at.
-template <int TYPE, int V, int LANES, int NV, int ROWS>
-__global__ void __launch_bounds__(LANES > 32 ? LANES : 256) quantize_kernel(const QuantArgs a)
+// Rows to LANES threads (a warp or a block) one after the other, V values at a time, NV times; the next row is on its way while one is worked on.
+template <int TYPE, int V, int LANES, int NV>
+__global__ void __launch_bounds__(LANES > 32 ? LANES : 256, LANES > 32 ? 1 : NV * V > 16 ? 2 : 4) quantize_kernel(const QuantArgs a)
 {
     pdl_enter();
     if (a.early) asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     constexpr int B = LANES > 32 ? LANES : 256, GROUPS = B / LANES;
-    __shared__ uint32_t slot[ROWS][LANES > 32 ? LANES / 32 : 1];
+    __shared__ uint32_t slots[2][LANES > 32 ? LANES / 32 : 1];
     const int lane = threadIdx.x % LANES;
-    const int64_t row0 = ((int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES) * ROWS;
-    Raw<TYPE, V> w[ROWS][NV];
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r)
+    const int64_t step = (int64_t)gridDim.x * GROUPS;
+    int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES;
+    Raw<TYPE, V> next[NV];
+    auto fetch = [&](int64_t r) {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (k * LANES + lane) * V;
-            w[r][k].load(a.x, a.type, (row0 + r) * a.ldx + c, row0 + r < a.n ? a.d - c : 0, a.whole);
+            next[k].load(a.x, a.type, r * a.ldx + c, r < a.n ? a.d - c : 0, a.whole);
         }
-    uint32_t tops[ROWS];                      // as bits, which order magnitudes, infinity and NaN
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        uint32_t top = 0u;
+    };
+    fetch(row);
+    int trip = 0;
+    for (int64_t base = (int64_t)blockIdx.x * GROUPS; base < a.n; base += step, row += step, trip ^= 1) {      // the same trips for all threads of a block
+        Raw<TYPE, V> w[NV];
+        uint32_t top = 0u;                    // as bits, which order magnitudes, infinity and NaN
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
+            w[k] = next[k];
             float v[V];
-            w[r][k].values(v);
+            w[k].values(v);
 #pragma unroll
             for (int i = 0; i < V; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
         }
-        tops[r] = __reduce_max_sync(0xffffffffu, top);
-        if (LANES > 32 && (threadIdx.x & 31) == 0) slot[r][threadIdx.x >> 5] = tops[r];
-    }
-    if constexpr (LANES > 32) {
-        __syncthreads();
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) tops[r] = __reduce_max_sync(0xffffffffu, (threadIdx.x & 31) < LANES / 32 ? slot[r][threadIdx.x & 31] : 0u);
-    }
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        const int64_t row = row0 + r;
-        if (row >= a.n) return;
-        const uint32_t top = tops[r];
+        fetch(row + step);
+        top = __reduce_max_sync(0xffffffffu, top);
+        if constexpr (LANES > 32) {
+            uint32_t* slot = slots[trip];
+            if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = top;
+            __syncthreads();
+            top = __reduce_max_sync(0xffffffffu, (threadIdx.x & 31) < LANES / 32 ? slot[threadIdx.x & 31] : 0u);
+        }
+        if (row >= a.n) continue;
         const bool finite = top < 0x7f800000u;
         const float t = __uint_as_float(top), factor = 127.f / t;
         const bool tiny = t < 1e-30f;         // 127 / t would overflow
@@ -105,10 +114,10 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : 256) quantize_kernel(cons
             const int c = (k * LANES + lane) * V;
             if (c >= a.d) break;
             float v[V];
-            w[r][k].values(v);
+            w[k].values(v);
             uint32_t o[V / 4];
 #pragma unroll
-            for (int j = 0; j < V / 4; ++j) o[j] = finite && top ? nearest4(v + 4 * j, factor, t, tiny) : 0u;
+            for (int j = 0; j < V / 4; ++j) o[j] = finite && top ? nearest4<TYPE == BIGCN_BF16 || TYPE == BIGCN_F16>(v + 4 * j, factor, t, tiny) : 0u;
             if (c + V <= a.d) {               // rows of q start on 16-byte boundaries
                 if constexpr (V == 4) *reinterpret_cast<uint32_t*>(q + c) = o[0];
                 else *reinterpret_cast<uint2*>(q + c) = make_uint2(o[0], o[1]);
@@ -121,29 +130,29 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : 256) quantize_kernel(cons
     }
 }
 
-template <int TYPE, int V, int LANES, int NV, int ROWS>
+template <int TYPE, int V, int LANES, int NV>
 cudaError_t launch_quantize_as(cudaStream_t s, const QuantArgs& a, int* launches)
 {
     constexpr int B = LANES > 32 ? LANES : 256;
     ++*launches;
-    return launch_kernel(quantize_kernel<TYPE, V, LANES, NV, ROWS>, dim3((unsigned)ceil_div(a.n, B / LANES * ROWS)), dim3(B), 0, s, a);
+    const int64_t blocks = std::min<int64_t>(ceil_div(a.n, B / LANES), (int64_t)sm_count() * (LANES > 32 ? 2048 / B : NV * V > 16 ? 2 : 4));
+    return launch_kernel(quantize_kernel<TYPE, V, LANES, NV>, dim3((unsigned)blocks), dim3(B), 0, s, a);
 }
-// A warp to a row, or to several short ones, as long as that leaves the machine enough warps; else a block.  16,384 bf16 rows of 2,048
-// in us: 40 with blocks of 128 threads, N2 with warps; 169,343 fp32 rows of 256: 53 with a row to a warp, N3 with four.
+// A warp to a row as long as that leaves the machine enough warps, else a block.  In us: 16,384 bf16 rows of 2,048 45 with a row of 128 threads,
+// 32 with a warp; 169,343 fp32 rows of 256 53 with a warp that ends with its row, 39 with one that goes on.
 template <int TYPE, int V>
 cudaError_t pick_quantize(cudaStream_t s, const QuantArgs& a, int* launches)
 {
     constexpr int Q = 16 / V;
     const int64_t words = ceil_div(a.d, V);
-    const bool many = a.n >= 8192;
-    if (words <= 32) return many ? launch_quantize_as<TYPE, V, 32, 1, 4>(s, a, launches) : launch_quantize_as<TYPE, V, 32, 1, 1>(s, a, launches);
-    if (words <= 64) return many ? launch_quantize_as<TYPE, V, 32, 2, 4>(s, a, launches) : launch_quantize_as<TYPE, V, 32, 2, 1>(s, a, launches);
-    if (many && words <= 128) return launch_quantize_as<TYPE, V, 32, 4, 2>(s, a, launches);
-    if (many && words <= 256) return launch_quantize_as<TYPE, V, 32, 8, 1>(s, a, launches);
-    if (words <= 32 * Q) return launch_quantize_as<TYPE, V, 32, Q, 1>(s, a, launches);
-    if (words <= 128 * Q) return launch_quantize_as<TYPE, V, 128, Q, 1>(s, a, launches);
-    if (words <= 512 * Q) return launch_quantize_as<TYPE, V, 512, Q, 1>(s, a, launches);
-    return launch_quantize_as<TYPE, V, 1024, Q, 1>(s, a, launches);
+    const bool many = a.n >= 4096;
+    if (words <= 32) return launch_quantize_as<TYPE, V, 32, 1>(s, a, launches);
+    if (words <= 64) return launch_quantize_as<TYPE, V, 32, 2>(s, a, launches);
+    if (words <= 32 * Q || (many && words <= 128)) return launch_quantize_as<TYPE, V, 32, 4>(s, a, launches);
+    if (many && words <= 256) return launch_quantize_as<TYPE, V, 32, 8>(s, a, launches);
+    if (words <= 128 * Q) return launch_quantize_as<TYPE, V, 128, Q>(s, a, launches);
+    if (words <= 512 * Q) return launch_quantize_as<TYPE, V, 512, Q>(s, a, launches);
+    return launch_quantize_as<TYPE, V, 1024, Q>(s, a, launches);
 }
 
 // Epilogue: the sums times both scales, in the output's type.
@@ -243,8 +252,8 @@ struct ScaledAcross {
 
 // One to four rows, not yet quantised, in one launch.  Every block quantises them for itself into shared memory (their bytes times the number of
 // blocks come from L2 and are few) while its first class rows are on their way; then a warp takes kGemvRows class rows at a time, 16 bytes of each a
-// lane, and sums by four-byte dot products.  Bound by the class rows, which are read once: 65,536 classes x 1,024 for one row in us: 19.5 by two
-// kernels with tensor memory to set up, N4 so; the dot products of more than four rows would cost more than that saves.
+// lane, and sums by four-byte dot products.  Bound by the class rows, which are read once: 65,536 classes x 1,024 for one row in us: 19.8 by two
+// kernels with tensor memory to set up, 10.8 so; the dot products of more than four rows would cost more than that saves.
 constexpr int kGemvThreads = 512, kGemvRows = 4, kGemvMax = 4, kGemvBytes = 64 * 1024;
 struct GemvArgs {
     const void* x;
@@ -298,7 +307,7 @@ __global__ void __launch_bounds__(kGemvThreads, 2) few_rows_kernel(const GemvArg
         for (int c = threadIdx.x * 4; c < words * 16; c += kGemvThreads * 4) {
             float v[4];
             load_as<kAnyType, 4>(a.x, a.type, row + c, r < a.n ? a.d - c : 0, a.whole, v);
-            q[c / 4] = finite && top ? nearest4(v, factor, t, t < 1e-30f) : 0u;
+            q[c / 4] = finite && top ? nearest4<false>(v, factor, t, t < 1e-30f) : 0u;
         }
     }
     __syncthreads();

@@ -8,6 +8,7 @@ creating a :class:`BiGCN` raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
@@ -139,6 +140,16 @@ def _dense(rows: int, cols: int, dtype: torch.dtype, device: torch.device) -> to
     if cols == 0:
         return torch.empty_strided((rows,), (1,), dtype=dtype, device=device)
     return torch.empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device)
+
+
+def _addr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+@functools.lru_cache(maxsize=1024)
+def _sizes(function: str, *args) -> int:
+    """What one of the library's functions of sizes alone says."""
+    return int(getattr(load(), function)(*args))
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -456,17 +467,19 @@ class BiGCN:
         """Checks a matrix argument and returns its leading dimension."""
         if t.dim() != 2 or t.dtype not in types or t.device != self.device:
             raise ValueError("%s: a matrix on %s of one of the types %s is wanted" % (name, self.device, [str(x) for x in types]))
-        n, d = t.shape
+        (n, d), (ld, step) = t.shape, t.stride()
         if (rows is not None and n != rows) or (cols is not None and d != cols):
             raise ValueError("%s: %d x %d elements where %s x %s are wanted" % (name, n, d, "any" if rows is None else rows, "any" if cols is None else cols))
-        if d > 1 and t.stride(1) != 1:
+        if step != 1 and d > 1:
             raise ValueError("%s: the elements of a row must lie next to each other" % name)
-        if n > 1 and t.stride(0) < d:
+        if n <= 1:
+            return d
+        if ld < d:
             raise ValueError("%s: rows overlap" % name)
-        return t.stride(0) if n > 1 else d
+        return ld
 
     def _vector(self, name: str, t: Optional[torch.Tensor], length: int, dtype=torch.float32):
-        if t is not None and (t.dim() != 1 or t.numel() != length or t.dtype != dtype or t.device != self.device or (length > 1 and t.stride(0) != 1)):
+        if t is not None and (t.shape != (length,) or t.dtype != dtype or t.device != self.device or (length > 1 and t.stride(0) != 1)):
             raise ValueError("%s: %d contiguous elements of %s on %s are wanted" % (name, length, dtype, self.device))
 
     def _scratch(self, nbytes: int):
@@ -474,7 +487,7 @@ class BiGCN:
         if self.workspace is None or self.workspace.numel() < nbytes:
             with torch.cuda.stream(self.stream):
                 self.ensure_workspace(nbytes)
-        if torch.cuda.is_current_stream_capturing() and not any(w is self.workspace for w in self._captured):
+        if torch._C._cuda_isCurrentStreamCapturing() and not any(w is self.workspace for w in self._captured):
             self._captured.append(self.workspace)
 
     def _outs(self, *wanted):
@@ -495,8 +508,8 @@ class BiGCN:
         if out_dtype not in (torch.float32, torch.bfloat16, torch.float16):
             raise ValueError("layer_norm: no output of type %s" % out_dtype)
         Y, mean, rstd = self._outs((n, d, out_dtype), (n, 0, torch.float32), (n, 0, torch.float32))
-        self._check(self.lib.bigcn_layer_norm(self.h, _ptr(X), TYPES[X.dtype], n, d, ldx, _ptr(gain), _ptr(offset), eps, _ptr(Y),
-                                              TYPES[out_dtype], d, _ptr(mean), _ptr(rstd)))
+        self._check(self.lib.bigcn_layer_norm(self.h, _addr(X), TYPES[X.dtype], n, d, ldx, _addr(gain), _addr(offset), eps, _addr(Y),
+                                              TYPES[out_dtype], d, _addr(mean), _addr(rstd)))
         return Y, mean, rstd
 
     def layer_norm_backward(self, g_y: torch.Tensor, X: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
@@ -511,11 +524,11 @@ class BiGCN:
         out_dtype = X.dtype if out_dtype is None else out_dtype
         if out_dtype not in (torch.float32, torch.bfloat16, torch.float16):
             raise ValueError("layer_norm_backward: no output of type %s" % out_dtype)
-        self._scratch(int(self.lib.bigcn_layer_norm_workspace_bytes(d)))
+        self._scratch(_sizes("bigcn_layer_norm_workspace_bytes", d))
         g_x, g_gain, g_offset = self._outs((n, d, out_dtype), (d, 0, torch.float32), (d, 0, torch.float32))
         self._check(self.lib.bigcn_layer_norm_backward(
-            self.h, _ptr(g_y), TYPES[g_y.dtype], ldg, _ptr(X), TYPES[X.dtype], ldx, n, d, _ptr(gain), _ptr(mean), _ptr(rstd),
-            _ptr(g_x), TYPES[out_dtype], d, _ptr(g_gain), _ptr(g_offset)))
+            self.h, _addr(g_y), TYPES[g_y.dtype], ldg, _addr(X), TYPES[X.dtype], ldx, n, d, _addr(gain), _addr(mean), _addr(rstd),
+            _addr(g_x), TYPES[out_dtype], d, _addr(g_gain), _addr(g_offset)))
         return g_x, g_gain, g_offset
 
     def _class_rows(self, X: torch.Tensor, W: torch.Tensor, labels: torch.Tensor):
@@ -529,9 +542,9 @@ class BiGCN:
         """Softmax cross entropy of the rows of X against the class rows of W, the logits never stored: (loss, lse) per row.
         A negative label marks a row that takes no part."""
         ldx, ldw, n, d, classes = self._class_rows(X, W, labels)
-        self._scratch(int(self.lib.bigcn_class_loss_workspace_bytes(n, d, classes, 0)))
+        self._scratch(_sizes("bigcn_class_loss_workspace_bytes", n, d, classes, 0))
         loss, lse = self._outs((n, 0, torch.float32), (n, 0, torch.float32))
-        self._check(self.lib.bigcn_class_loss(self.h, _ptr(X), _ptr(W), TYPES[X.dtype], n, d, classes, ldx, ldw, _ptr(labels), _ptr(loss), _ptr(lse)))
+        self._check(self.lib.bigcn_class_loss(self.h, _addr(X), _addr(W), TYPES[X.dtype], n, d, classes, ldx, ldw, _addr(labels), _addr(loss), _addr(lse)))
         return loss, lse
 
     def class_loss_backward(self, X: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, lse: torch.Tensor, g_loss: torch.Tensor,
@@ -540,10 +553,10 @@ class BiGCN:
         ldx, ldw, n, d, classes = self._class_rows(X, W, labels)
         self._vector("lse", lse, n)
         self._vector("g_loss", g_loss, n)
-        self._scratch(int(self.lib.bigcn_class_loss_workspace_bytes(n, d, classes, 1)))
+        self._scratch(_sizes("bigcn_class_loss_workspace_bytes", n, d, classes, 1))
         g_x, g_w = self._outs((n, d, X.dtype) if want_g_x else None, (classes, d, X.dtype) if want_g_w else None)
-        self._check(self.lib.bigcn_class_loss_backward(self.h, _ptr(X), _ptr(W), TYPES[X.dtype], n, d, classes, ldx, ldw, _ptr(labels), _ptr(lse),
-                                                       _ptr(g_loss), _ptr(g_x), d, _ptr(g_w), d))
+        self._check(self.lib.bigcn_class_loss_backward(self.h, _addr(X), _addr(W), TYPES[X.dtype], n, d, classes, ldx, ldw, _addr(labels), _addr(lse),
+                                                       _addr(g_loss), _addr(g_x), d, _addr(g_w), d))
         return g_x, g_w
 
     def quantize_rows(self, X: torch.Tensor):
@@ -555,7 +568,7 @@ class BiGCN:
         if ldq != d:
             with torch.cuda.stream(self.stream):
                 q[:, d:] = 0
-        self._check(self.lib.bigcn_quantize_rows(self.h, _ptr(X), TYPES[X.dtype], n, d, ldx, _ptr(q), ldq, _ptr(scale)))
+        self._check(self.lib.bigcn_quantize_rows(self.h, _addr(X), TYPES[X.dtype], n, d, ldx, _addr(q), ldq, _addr(scale)))
         return q, scale
 
     def quantized_product(self, X: torch.Tensor, q_w: torch.Tensor, s_w: torch.Tensor, s_x: Optional[torch.Tensor] = None,
@@ -581,13 +594,13 @@ class BiGCN:
             d = X.shape[1]
             if (d + 15) // 16 * 16 != (q_w.shape[1] + 15) // 16 * 16 or q_w.shape[1] < d:
                 raise ValueError("X: rows of %d for class rows of %d" % (d, q_w.shape[1]))
-            self._scratch(int(self.lib.bigcn_quantized_product_workspace_bytes(n, d)))
+            self._scratch(_sizes("bigcn_quantized_product_workspace_bytes", n, d))
         self._vector("s_w", s_w, m)
         if out_dtype not in (torch.float32, torch.bfloat16, torch.float16):
             raise ValueError("quantized_product: no output of type %s" % out_dtype)
         out, = self._outs((n, m, out_dtype))
-        self._check(self.lib.bigcn_quantized_product(self.h, _ptr(X), TYPES[X.dtype], _ptr(s_x), n, d, ldx, _ptr(q_w), ldqw, _ptr(s_w), m,
-                                                     _ptr(out), TYPES[out_dtype], m))
+        self._check(self.lib.bigcn_quantized_product(self.h, _addr(X), TYPES[X.dtype], _addr(s_x), n, d, ldx, _addr(q_w), ldqw, _addr(s_w), m,
+                                                     _addr(out), TYPES[out_dtype], m))
         return out
 
     def measure_popc_peak(self) -> float:

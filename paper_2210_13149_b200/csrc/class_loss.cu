@@ -432,20 +432,27 @@ struct Store {
             } else {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) w[i] = pack2<BIGCN_BF16>(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
-                gemm::write_strip(p.strip, w, [&](int r, int piece, const uint4& q) {
-                    const int64_t to_row = __shfl_sync(0xffffffffu, mapped, r);
-                    const int at = col + 8 * piece;
-                    if (p.row + r >= p.rows || at >= sh.n) return;
-                    uint16_t* to = a.out + to_row * a.ldo + at;
-                    if (a.whole && at + 8 <= sh.n) {
-                        *reinterpret_cast<uint4*>(to) = q;
-                    } else {
-                        const uint16_t* e = reinterpret_cast<const uint16_t*>(&q);
+                if (a.whole) {
+                    gemm::write_strip(p.strip, w, [&](int r, int piece, const uint4& q) {
+                        const int64_t to_row = __shfl_sync(0xffffffffu, mapped, r);
+                        const int at = col + 8 * piece;
+                        if (p.row + r >= p.rows || at >= sh.n) return;
+                        uint16_t* to = a.out + to_row * a.ldo + at;
+                        if (at + 8 <= sh.n) {
+                            *reinterpret_cast<uint4*>(to) = q;
+                        } else {
+                            const uint16_t* e = reinterpret_cast<const uint16_t*>(&q);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            if (at + i < sh.n) to[i] = e[i];
-                    }
-                });
+                            for (int i = 0; i < 8; ++i)
+                                if (at + i < sh.n) to[i] = e[i];
+                        }
+                    });
+                } else {
+                    gemm::write_strip_elements<uint16_t>(p.strip, w, [&](int r, int e, uint16_t bits) {
+                        const int64_t to_row = __shfl_sync(0xffffffffu, mapped, r);
+                        if (p.row + r < p.rows && col + e < sh.n) a.out[to_row * a.ldo + col + e] = bits;
+                    });
+                }
             }
         });
     }

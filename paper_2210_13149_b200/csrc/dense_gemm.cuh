@@ -279,6 +279,23 @@ __device__ __forceinline__ void write_strip(unsigned char* strip, const uint32_t
     }
 }
 
+// The same for rows that start anywhere: put(r, e, bits) for the element e = 0 .. 64 / sizeof(T) - 1 of row r, neighbours to neighbouring lanes.
+template <class T, class Put>
+__device__ __forceinline__ void write_strip_elements(unsigned char* strip, const uint32_t (&w)[16], const Put& put)
+{
+    constexpr int kElts = 64 / sizeof(T), kRowsAtOnce = 32 / kElts < 1 ? 1 : 32 / kElts;
+    const int lane = threadIdx.x & 31;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(strip + lane * 64 + 16 * (i ^ ((lane >> 1) & 3))) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    __syncwarp();
+#pragma unroll 8
+    for (int i = 0; i < 32; i += kRowsAtOnce) {
+        const int r = i + lane / kElts, e = lane % kElts, at = e * (int)sizeof(T);
+        put(r, e, *reinterpret_cast<const T*>(strip + r * 64 + 16 * ((at >> 4) ^ ((r >> 1) & 3)) + (at & 15)));
+    }
+}
+
 // Epi: struct with
 //   Args
 //   Row                            what it reads of a row (of the tile, a lane's)

@@ -131,31 +131,48 @@ __device__ __forceinline__ void store_as(void* base, int type, int64_t at, int c
     else store_elts<BIGCN_F16, V>(static_cast<__half*>(base) + at, count, whole, v);
 }
 
-// The same in words of at most `step` elements, a power of two that the address is aligned to.
-template <int V>
-__device__ __forceinline__ void store_steps(void* base, int type, int64_t at, int count, int step, const float (&v)[V])
+// Words of at most `step` elements, a power of two that the address is aligned to.  A row's store looks its type up once: NV words of a
+// lane, `stride` elements apart from column `c` on.
+template <int TYPE, int V>
+__device__ __forceinline__ void store_steps(typename Elt<TYPE>::T* p, int count, int step, const float (&v)[V])
 {
     if constexpr (V == 1) {
-        store_as<1>(base, type, at, count, true, v);
+        store_elts<TYPE, 1>(p, count, true, v);
     } else {
-        if (step >= V) return store_as<V>(base, type, at, count, true, v);
+        if (step >= V) return store_elts<TYPE, V>(p, count, true, v);
         float lo[V / 2], hi[V / 2];
 #pragma unroll
         for (int i = 0; i < V / 2; ++i) lo[i] = v[i], hi[i] = v[V / 2 + i];
-        store_steps<V / 2>(base, type, at, count, step, lo);
-        store_steps<V / 2>(base, type, at + V / 2, count - V / 2, step, hi);
+        store_steps<TYPE, V / 2>(p, count, step, lo);
+        store_steps<TYPE, V / 2>(p + V / 2, count - V / 2, step, hi);
     }
 }
+template <int TYPE, int NV, int V>
+__device__ __forceinline__ void store_row_of(void* base, int64_t row_at, int c, int stride, int d, int step, const float (&v)[NV][V])
+{
+    auto* p = static_cast<typename Elt<TYPE>::T*>(base) + row_at;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+        if (c + k * stride < d) store_steps<TYPE, V>(p + c + k * stride, d - c - k * stride, step, v[k]);
+}
+template <int NV, int V>
+__device__ __forceinline__ void store_row(void* base, int type, int64_t row_at, int c, int stride, int d, int step, const float (&v)[NV][V])
+{
+    if (type == BIGCN_F32) store_row_of<BIGCN_F32, NV, V>(base, row_at, c, stride, d, step, v);
+    else if (type == BIGCN_BF16) store_row_of<BIGCN_BF16, NV, V>(base, row_at, c, stride, d, step, v);
+    else store_row_of<BIGCN_F16, NV, V>(base, row_at, c, stride, d, step, v);
+}
 
-// V elements as they lie in memory: 16 bytes of a type known when compiled, or fp32 values.
+// V elements as they lie in memory: 8 or 16 bytes of a type known when compiled, or else fp32 values.
 template <int TYPE, int V>
 struct Raw {
-    static constexpr int kWords = TYPE == kAnyType ? V : V * type_bytes(TYPE) / 4;
+    static constexpr bool kPacked = TYPE != kAnyType && V * type_bytes(TYPE) >= 8;
+    static constexpr int kWords = kPacked ? V * type_bytes(TYPE) / 4 : V;
     uint32_t w[kWords];
     // of a type looked up: `whole` as in load_elts(); of a known type the address is aligned to the 16 (or 8) bytes
     __device__ __forceinline__ void load(const void* base, int type, int64_t at, int count, bool whole = true)
     {
-        if constexpr (TYPE == kAnyType) {
+        if constexpr (!kPacked) {
             float f[V];
             load_as<TYPE, V>(base, type, at, count, whole, f);
 #pragma unroll

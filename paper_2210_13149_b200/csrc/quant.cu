@@ -7,6 +7,7 @@
 // two products) are fp32's, then one to the output's type.  The scales are multiplied first: a row with fp32's lowest value in it has a
 // scale of 2^121, which times the sum would overflow where the output does not.
 #include <climits>
+#include <type_traits>
 
 #include "dense_gemm.cuh"
 #include "dense_types.cuh"
@@ -180,19 +181,27 @@ struct ScaledOut {
                 if constexpr (TYPE == BIGCN_F32) w[i] = __float_as_uint(f[16 * h + i]);
                 else w[i] = pack2<TYPE>(f[2 * i], f[2 * i + 1]);
             }
-            gemm::write_strip(p.strip, w, [&](int r, int piece, const uint4& v) {
-                const int row = p.row + r, c = col + 16 * h + piece * kElts;
-                if (row >= p.rows || c >= columns) return;
-                T* to = static_cast<T*>(a.out) + (int64_t)row * a.ldo + c;
-                if (a.whole && c + kElts <= columns) {
-                    *reinterpret_cast<uint4*>(to) = v;
-                } else {
-                    const T* e = reinterpret_cast<const T*>(&v);
+            T* const out = static_cast<T*>(a.out) + col + 16 * h;
+            if (a.whole) {
+                gemm::write_strip(p.strip, w, [&](int r, int piece, const uint4& v) {
+                    const int row = p.row + r, c = piece * kElts, left = columns - (col + 16 * h + c);
+                    if (row >= p.rows || left <= 0) return;
+                    T* to = out + (int64_t)row * a.ldo + c;
+                    if (left >= kElts) {
+                        *reinterpret_cast<uint4*>(to) = v;
+                    } else {
+                        const T* e = reinterpret_cast<const T*>(&v);
 #pragma unroll
-                    for (int i = 0; i < kElts; ++i)
-                        if (c + i < columns) to[i] = e[i];
-                }
-            });
+                        for (int i = 0; i < kElts; ++i)
+                            if (i < left) to[i] = e[i];
+                    }
+                });
+            } else {
+                using Bits = typename std::conditional<sizeof(T) == 4, uint32_t, uint16_t>::type;
+                gemm::write_strip_elements<Bits>(p.strip, w, [&](int r, int e, Bits v) {
+                    if (p.row + r < p.rows && col + 16 * h + e < columns) reinterpret_cast<Bits*>(out)[(int64_t)(p.row + r) * a.ldo + e] = v;
+                });
+            }
         }
     }
     static __device__ int* flag() { return &g_quant_timeout; }

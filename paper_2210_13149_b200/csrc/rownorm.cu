@@ -9,8 +9,8 @@
 // cancellation.  The columns' sums of the backward pass ride along in registers, one pair per column a thread owns, over the rows that
 // its lanes take; blocks leave theirs in the workspace, and a second kernel adds them in 64 bits in a fixed order.
 //
-// Lanes read words of 16 bytes where the rows they read start on their boundaries (kernels for each type), and otherwise words of
-// 4, 2 or 1 elements, whichever both matrices allow (kernels that look the type up); they store what the output's rows allow.
+// Lanes read words of 16 bytes where the rows they read start on their boundaries, and otherwise words of 4, 2 or 1 elements, whichever the rows
+// allow (the backward pass, with two types to read, then looks them up); they store what the output's rows allow.
 #include <algorithm>
 
 #include "dense_types.cuh"
@@ -86,8 +86,11 @@ struct NormArgs {
     float* rstd;
 };
 
+// Blocks of the forward pass on a multiprocessor: 1,024 threads with 64 registers each, rows going round in all of them.
+constexpr int norm_blocks(int lanes) { return lanes > 32 ? 1024 / lanes : 1024 / kThreads; }
+
 template <int TYPE, int V, int LANES, int NV>
-__global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads, LANES > 32 ? 1 : 4) norm_kernel(const NormArgs a)
+__global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads, norm_blocks(LANES)) norm_kernel(const NormArgs a)
 {
     pdl_enter();
     constexpr int B = LANES > 32 ? LANES : kThreads, GROUPS = B / LANES;
@@ -151,7 +154,6 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads, LANES > 32 ? 1 
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 const int c = (k * LANES + lane) * V;
-                if (c >= a.d) break;
                 float g[V], o[V];
                 if constexpr (kHold) {
 #pragma unroll
@@ -162,8 +164,8 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads, LANES > 32 ? 1 
                 }
 #pragma unroll
                 for (int i = 0; i < V; ++i) v[k][i] = fmaf(v[k][i] * r, g[i], o[i]);
-                store_steps<V>(a.y, a.y_type, row * a.ldy + c, a.d - c, a.y_step, v[k]);
             }
+            store_row<NV, V>(a.y, a.y_type, row * a.ldy, lane * V, LANES * V, a.d, a.y_step, v);
         }
     }
 }
@@ -333,13 +335,10 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads, BackLayout<GTYP
         if (row < a.n) {
             const float sa = sums[0] * inv_d, sb = sums[1] * inv_d;
 #pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                const int c = (k * LANES + lane) * V;
-                if (c >= a.d) break;
+            for (int k = 0; k < NV; ++k)
 #pragma unroll
                 for (int i = 0; i < V; ++i) gv[k][i] = (gv[k][i] - sa - xh[k][i] * sb) * r;
-                store_steps<V>(a.gx, a.gx_type, row * a.ldgx + c, a.d - c, a.gx_step, gv[k]);
-            }
+            store_row<NV, V>(a.gx, a.gx_type, row * a.ldgx, lane * V, LANES * V, a.d, a.gx_step, gv);
         }
     }
     if (!a.part) return;
@@ -418,7 +417,7 @@ template <int TYPE, int V, int LANES, int NV>
 cudaError_t launch_norm(cudaStream_t s, const NormArgs& a, int* launches)
 {
     constexpr int B = LANES > 32 ? LANES : kThreads;
-    const int64_t blocks = std::min<int64_t>(ceil_div(a.n, B / LANES), (int64_t)sm_count() * (2048 / B));
+    const int64_t blocks = std::min<int64_t>(ceil_div(a.n, B / LANES), (int64_t)sm_count() * norm_blocks(LANES));
     auto* kernel = norm_kernel<TYPE, V, LANES, NV>;
     constexpr size_t smem = NV * V <= 8 ? 0 : (size_t)2 * LANES * V * NV * sizeof(float);
     static std::atomic<uint64_t> ready{0};     // by device
@@ -439,22 +438,37 @@ cudaError_t pick_norm(cudaStream_t s, const NormArgs& a, int* launches)
     if (words <= 32) return launch_norm<TYPE, V, 32, 1>(s, a, launches);
     if (words <= 64) return launch_norm<TYPE, V, 32, 2>(s, a, launches);
     if (words <= 32 * Q) return launch_norm<TYPE, V, 32, Q>(s, a, launches);
+    if (words <= 128 * Q / 2) return launch_norm<TYPE, V, 128, Q / 2>(s, a, launches);
     if (words <= 128 * Q) return launch_norm<TYPE, V, 128, Q>(s, a, launches);
     if (words <= 256 * Q) return launch_norm<TYPE, V, 256, Q>(s, a, launches);
     if (words <= 512 * Q) return launch_norm<TYPE, V, 512, Q>(s, a, launches);
     return launch_norm<TYPE, V, 1024, Q>(s, a, launches);
 }
 
-template <int V>
-cudaError_t pick_norm_any(cudaStream_t s, const NormArgs& a, int* launches)
+// Rows off 16-byte boundaries, in words of V elements.
+template <int TYPE, int V>
+cudaError_t pick_norm_off(cudaStream_t s, const NormArgs& a, int* launches)
 {
     constexpr int Q = 16 / V;
-    if (a.d <= 64) return launch_norm<kAnyType, V, 32, V == 1 ? 2 : 1>(s, a, launches);
-    if (a.d <= 128) return launch_norm<kAnyType, V, 32, 4 / V>(s, a, launches);
-    if (a.d <= 512) return launch_norm<kAnyType, V, 32, Q>(s, a, launches);
-    if (a.d <= 2048) return launch_norm<kAnyType, V, 128, Q>(s, a, launches);
-    if (a.d <= 8192) return launch_norm<kAnyType, V, 512, Q>(s, a, launches);
-    return launch_norm<kAnyType, V, 1024, Q>(s, a, launches);
+    if (a.d <= 16) return launch_norm<TYPE, V, 8, 2 / (V < 2 ? V : 2)>(s, a, launches);
+    if (a.d <= 32) return launch_norm<TYPE, V, 16, 2 / (V < 2 ? V : 2)>(s, a, launches);
+    if (a.d <= 64) return launch_norm<TYPE, V, 32, 2 / (V < 2 ? V : 2)>(s, a, launches);
+    if (a.d <= 128) return launch_norm<TYPE, V, 32, 4 / V>(s, a, launches);
+    if (a.d <= 256) return launch_norm<TYPE, V, 32, 8 / V>(s, a, launches);
+    if (a.d <= 512) return launch_norm<TYPE, V, 32, Q>(s, a, launches);
+    if (a.d <= 1024) return launch_norm<TYPE, V, 128, Q / 2>(s, a, launches);
+    if (a.d <= 2048) return launch_norm<TYPE, V, 128, Q>(s, a, launches);
+    if (a.d <= 4096) return launch_norm<TYPE, V, 512, Q / 2>(s, a, launches);
+    if (a.d <= 8192) return launch_norm<TYPE, V, 512, Q>(s, a, launches);
+    return launch_norm<TYPE, V, 1024, Q>(s, a, launches);
+}
+template <int TYPE>
+cudaError_t pick_norm_step(cudaStream_t s, int step, const NormArgs& a, int* launches)
+{
+    if constexpr (TYPE != BIGCN_F32)
+        if (step >= 4) return pick_norm_off<TYPE, 4>(s, a, launches);
+    if (step >= 2) return pick_norm_off<TYPE, 2>(s, a, launches);
+    return pick_norm_off<TYPE, 1>(s, a, launches);
 }
 
 template <int GTYPE, int TYPE, int V, int LANES, int NV>
@@ -489,6 +503,7 @@ cudaError_t pick_back(cudaStream_t s, const NormBackArgs& a, float* g_gain, floa
     if (words <= 32) return launch_back<GTYPE, TYPE, V, 32, 1>(s, a, g_gain, g_offset, launches);
     if (words <= 64) return launch_back<GTYPE, TYPE, V, 32, 2>(s, a, g_gain, g_offset, launches);
     if (words <= 32 * Q) return launch_back<GTYPE, TYPE, V, 32, Q>(s, a, g_gain, g_offset, launches);
+    if (words <= 128 * Q / 2) return launch_back<GTYPE, TYPE, V, 128, Q / 2>(s, a, g_gain, g_offset, launches);
     if (words <= 128 * Q) return launch_back<GTYPE, TYPE, V, 128, Q>(s, a, g_gain, g_offset, launches);
     if (words <= 256 * Q) return launch_back<GTYPE, TYPE, V, 256, Q>(s, a, g_gain, g_offset, launches);
     if (words <= 512 * Q) return launch_back<GTYPE, TYPE, V, 512, Q>(s, a, g_gain, g_offset, launches);
@@ -496,15 +511,20 @@ cudaError_t pick_back(cudaStream_t s, const NormBackArgs& a, float* g_gain, floa
 }
 
 template <int V>
-cudaError_t pick_back_any(cudaStream_t s, const NormBackArgs& a, float* g_gain, float* g_offset, int* launches)
+cudaError_t pick_back_off(cudaStream_t s, const NormBackArgs& a, float* g_gain, float* g_offset, int* launches)
 {
-    constexpr int Q = 16 / V;
-    if (a.d <= 64) return launch_back<kAnyType, kAnyType, V, 32, V == 1 ? 2 : 1>(s, a, g_gain, g_offset, launches);
-    if (a.d <= 128) return launch_back<kAnyType, kAnyType, V, 32, 4 / V>(s, a, g_gain, g_offset, launches);
-    if (a.d <= 512) return launch_back<kAnyType, kAnyType, V, 32, Q>(s, a, g_gain, g_offset, launches);
-    if (a.d <= 2048) return launch_back<kAnyType, kAnyType, V, 128, Q>(s, a, g_gain, g_offset, launches);
-    if (a.d <= 8192) return launch_back<kAnyType, kAnyType, V, 512, Q>(s, a, g_gain, g_offset, launches);
-    return launch_back<kAnyType, kAnyType, V, 1024, Q>(s, a, g_gain, g_offset, launches);
+    constexpr int Q = 16 / V, T = kAnyType;
+    if (a.d <= 16) return launch_back<T, T, V, 8, 2 / (V < 2 ? V : 2)>(s, a, g_gain, g_offset, launches);
+    if (a.d <= 32) return launch_back<T, T, V, 16, 2 / (V < 2 ? V : 2)>(s, a, g_gain, g_offset, launches);
+    if (a.d <= 64) return launch_back<T, T, V, 32, 2 / (V < 2 ? V : 2)>(s, a, g_gain, g_offset, launches);
+    if (a.d <= 128) return launch_back<T, T, V, 32, 4 / V>(s, a, g_gain, g_offset, launches);
+    if (a.d <= 256) return launch_back<T, T, V, 32, 8 / V>(s, a, g_gain, g_offset, launches);
+    if (a.d <= 512) return launch_back<T, T, V, 32, Q>(s, a, g_gain, g_offset, launches);
+    if (a.d <= 1024) return launch_back<T, T, V, 128, Q / 2>(s, a, g_gain, g_offset, launches);
+    if (a.d <= 2048) return launch_back<T, T, V, 128, Q>(s, a, g_gain, g_offset, launches);
+    if (a.d <= 4096) return launch_back<T, T, V, 512, Q / 2>(s, a, g_gain, g_offset, launches);
+    if (a.d <= 8192) return launch_back<T, T, V, 512, Q>(s, a, g_gain, g_offset, launches);
+    return launch_back<T, T, V, 1024, Q>(s, a, g_gain, g_offset, launches);
 }
 
 template <int GTYPE>
@@ -529,9 +549,9 @@ cudaError_t launch_layer_norm(cudaStream_t s, const void* x, int x_type, int64_t
         return pick_norm<BIGCN_F16, 8>(s, a, launches);
     }
     const int step = rows_step(x, ldx, x_type, 4);
-    if (step == 4) return pick_norm_any<4>(s, a, launches);
-    if (step == 2) return pick_norm_any<2>(s, a, launches);
-    return pick_norm_any<1>(s, a, launches);
+    if (x_type == BIGCN_F32) return pick_norm_step<BIGCN_F32>(s, step, a, launches);
+    if (x_type == BIGCN_BF16) return pick_norm_step<BIGCN_BF16>(s, step, a, launches);
+    return pick_norm_step<BIGCN_F16>(s, step, a, launches);
 }
 
 cudaError_t launch_layer_norm_backward(cudaStream_t s, const void* g, int g_type, int64_t ldg, const void* x, int x_type, int64_t ldx, int64_t n, int d,
@@ -543,9 +563,9 @@ cudaError_t launch_layer_norm_backward(cudaStream_t s, const void* g, int g_type
     const int V = x_type == BIGCN_F32 || g_type == BIGCN_F32 ? 4 : 8;
     if (!rows_whole(g, ldg, g_type, V) || !rows_whole(x, ldx, x_type, V)) {
         const int step = std::min(rows_step(g, ldg, g_type, 4), rows_step(x, ldx, x_type, 4));
-        if (step == 4) return pick_back_any<4>(s, a, g_gain, g_offset, launches);
-        if (step == 2) return pick_back_any<2>(s, a, g_gain, g_offset, launches);
-        return pick_back_any<1>(s, a, g_gain, g_offset, launches);
+        if (step == 4) return pick_back_off<4>(s, a, g_gain, g_offset, launches);
+        if (step == 2) return pick_back_off<2>(s, a, g_gain, g_offset, launches);
+        return pick_back_off<1>(s, a, g_gain, g_offset, launches);
     }
     if (g_type == BIGCN_F32) return pick_back_x<BIGCN_F32>(s, x_type, a, g_gain, g_offset, launches);
     if (g_type == BIGCN_BF16) return pick_back_x<BIGCN_BF16>(s, x_type, a, g_gain, g_offset, launches);

@@ -1154,7 +1154,7 @@ bigcn_status bigcn_quantized_product(bigcn_ctx* ctx, const void* x, int32_t x_ty
     if (!ready) {
         const size_t need = bigcn_quantized_product_workspace_bytes(n, d);
         if (!ctx->ws || ctx->ws_bytes < need) return fail(ctx, BIGCN_ERR_WORKSPACE, "needs %zu bytes of workspace (bigcn_quantized_product_workspace_bytes)", need);
-        if (few_rows_covers(n, d)) {
+        if (few_rows_pays(n, d, m)) {
             e = launch_few_rows_product(ctx->stream, x, x_type, ldx, n, d, q_w, ldqw, s_w, m, out, out_type, ldo, &ctx->launches_i);
             finish_call(ctx);
             if (e != cudaSuccess) return cuda_fail(ctx, e, "quantized product launch");

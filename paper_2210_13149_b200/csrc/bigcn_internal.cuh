@@ -217,8 +217,8 @@ cudaError_t launch_layer_norm_backward(cudaStream_t s, const void* g, int g_type
 cudaError_t launch_quantize_rows(cudaStream_t s, const void* x, int type, int64_t n, int d, int64_t ldx, int8_t* q, int64_t ldq, float* scale, bool early, int* launches);
 cudaError_t launch_quantized_product(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const float* s_x, int64_t n, int d, const int8_t* q_w, int64_t ldqw,
                                      const float* s_w, int m, void* out, int out_type, int64_t ldo, bool early, int* launches);
-// One to four rows that are not quantised yet, in one launch, where they fit its shared memory.
-bool few_rows_covers(int64_t n, int d);
+// One to four rows that are not quantised yet, in one launch, where that is expected to be faster.
+bool few_rows_pays(int64_t n, int d, int m);
 cudaError_t launch_few_rows_product(cudaStream_t s, const void* x, int type, int64_t ldx, int64_t n, int d, const int8_t* q_w, int64_t ldqw, const float* s_w, int m,
                                     void* out, int out_type, int64_t ldo, int* launches);
 // Whether the product takes classes as rows of its tiles.  Then, with `early` in both launches one after the other, it fetches classes while the rows

@@ -262,7 +262,7 @@ struct ScaledAcross {
 // One to four rows, not yet quantised, in one launch.  Every block quantises them for itself into shared memory (their bytes times the number of
 // blocks come from L2 and are few) while its first class rows are on their way; then a warp takes kGemvRows class rows at a time, 16 bytes of each a
 // lane, and sums by four-byte dot products.  Bound by the class rows, which are read once: 65,536 classes x 1,024 for one row in us: 19.8 by two
-// kernels with tensor memory to set up, 10.8 so; the dot products of more than four rows would cost more than that saves.
+// kernels with tensor memory to set up, 10.8 so.  More rows cost more dot products: few_rows_pays().
 constexpr int kGemvThreads = 512, kGemvRows = 4, kGemvMax = 4, kGemvBytes = 64 * 1024;
 struct GemvArgs {
     const void* x;
@@ -393,7 +393,16 @@ int quant_timeouts()
     return v;
 }
 
-bool few_rows_covers(int64_t n, int d) { return n <= kGemvMax && n * round_up(d, 16) <= kGemvBytes; }
+// Whether that is expected to be the faster one, of what each takes in us: a launch from Python, 11 and 14.5; the class rows' bytes; and the
+// steps of a class row in one of 2,368 warps (16 bytes a lane are a load and four dot products a row, and every row's sum a reduction and a store).
+// Measured for 1, 2, 3, 4 rows against what two kernels take: 65,536 classes x 1,024 15.7, 18.6, 23.7, 24.8 against 18.5; 32,768 x 4,096 24, 28,
+// 34, 35 against 32; 200,000 x 256 22, 29, 41, 45 against 20; 30,011 x 602 11.3, 11.3, 14.2, 14.7 against 14.7; 4,096 x 256 11 against 14.6.
+bool few_rows_pays(int64_t n, int d, int m)
+{
+    if (n > kGemvMax || n * round_up(d, 16) > kGemvBytes) return false;
+    const double bytes = (double)m * d, steps = (double)m * ((double)ceil_div(d, 512) * (4 * n + 4) + 12 * n);
+    return std::max(11.0, 7.0 + std::max(3.7e-6 * steps, bytes / 6e6)) <= std::max(14.5, 8.0 + bytes / 6.4e6);
+}
 cudaError_t launch_few_rows_product(cudaStream_t s, const void* x, int type, int64_t ldx, int64_t n, int d, const int8_t* q_w, int64_t ldqw, const float* s_w, int m,
                                     void* out, int out_type, int64_t ldo, int* launches)
 {

@@ -389,8 +389,8 @@ bigcn_status bigcn_layer_norm_backward(bigcn_ctx* ctx, const void* g_y, int32_t 
                                        float* g_offset);
 
 /* Softmax cross entropy of rows against a class matrix: z_ik = sum_j x_ij w_kj over k < classes, lse_i = log sum_k exp z_ik,
- * loss_i = lse_i - z_i,label(i).  The logits z are never stored.  x [n x d], w [classes x d] (a row to a class) of type
- * BIGCN_BF16, products and sums in fp32; 1 <= d <= BIGCN_MAX_D_IN; n, classes < 2^31 - 512.  labels int64 [n]: a negative
+ * loss_i = lse_i - z_i,label(i).  The logits z are never stored.  x [n x d], w [classes x d] (a row to a class), both of type
+ * BIGCN_BF16 or both BIGCN_F16 (round fp32 rows to one of them: bigcn_layer_norm() writes them), products and sums in fp32; 1 <= d <= BIGCN_MAX_D_IN; n, classes < 2^31 - 512.  labels int64 [n]: a negative
  * one marks a row without a label, whose loss and lse are 0 and which takes no part in anything, whatever it holds; one
  * >= classes is an error that shows as NaN in loss_i and lse_i and is otherwise a row without a label.  loss, lse fp32 [n].
  * Needs bigcn_class_loss_workspace_bytes(n, d, classes, 0) of workspace.
@@ -398,7 +398,8 @@ bigcn_status bigcn_layer_norm_backward(bigcn_ctx* ctx, const void* g_y, int32_t 
  * bigcn_class_loss_backward(): the gradients for g_loss = dL/dloss (fp32 [n]) and the lse of the forward pass,
  *   G_ik = (exp(z_ik - lse_i) - [k = label(i)]) g_loss_i,  g_x = G w,  g_w = G^T x,
  * g_x [n x ldgx] and g_w [classes x ldgw] in the operands' type, nullable each.  z is computed again and G held a piece of
- * rows and classes at a time, in the operands' type; sums in fp32.  Rows without a label get zero.  The same call gives the
+ * rows and classes at a time, in the operands' type (in fp16 without g_loss, which comes in in fp32 for g_x and by way of
+ * rows of x times g_loss_i / max |g_loss| for g_w); sums in fp32.  Rows without a label get zero.  The same call gives the
  * same bits.  Needs bigcn_class_loss_workspace_bytes(n, d, classes, 1) of workspace. */
 size_t bigcn_class_loss_workspace_bytes(int64_t n, int32_t d, int32_t classes, int32_t backward);
 bigcn_status bigcn_class_loss(bigcn_ctx* ctx, const void* x, const void* w, int32_t type, int64_t n, int32_t d, int32_t classes,

@@ -532,9 +532,9 @@ class BiGCN:
         return g_x, g_gain, g_offset
 
     def _class_rows(self, X: torch.Tensor, W: torch.Tensor, labels: torch.Tensor):
-        types = (torch.bfloat16,)
+        types = (torch.bfloat16, torch.float16)
         ldx = self._rows("X", X, types)
-        ldw = self._rows("W", W, types, cols=X.shape[1])
+        ldw = self._rows("W", W, (X.dtype,), cols=X.shape[1])
         self._vector("labels", labels, X.shape[0], torch.int64)
         return ldx, ldw, X.shape[0], X.shape[1], W.shape[0]
 

@@ -214,7 +214,7 @@ bigcn_status check_quantized(bigcn_ctx* ctx, const char* name, const void* q, in
 bigcn_status check_class_loss(bigcn_ctx* ctx, const void* x, const void* w, int32_t type, int64_t n, int32_t d, int32_t classes, int64_t ldx, int64_t ldw,
                               const int64_t* labels)
 {
-    if (type != BIGCN_BF16) return fail(ctx, BIGCN_ERR_UNSUPPORTED, "type %d: the class loss takes BIGCN_BF16", type);
+    if (type != BIGCN_BF16 && type != BIGCN_F16) return fail(ctx, BIGCN_ERR_UNSUPPORTED, "type %d: the class loss takes BIGCN_BF16 and BIGCN_F16", type);
     if (classes < 1) return fail(ctx, BIGCN_ERR_SHAPE, "classes=%d must be >= 1", classes);
     bigcn_status st = check_rows(ctx, "x", x, type, n, d, ldx);
     if (st == BIGCN_OK) st = check_rows(ctx, "w", w, type, classes, d, ldw);
@@ -1081,7 +1081,7 @@ bigcn_status bigcn_class_loss(bigcn_ctx* ctx, const void* x, const void* w, int3
     if (!loss || !lse) return fail(ctx, BIGCN_ERR_NULL, "loss or lse is null");
     const size_t need = class_loss_scratch_bytes(n, d, classes, false);
     if (!ctx->ws || ctx->ws_bytes < need) return fail(ctx, BIGCN_ERR_WORKSPACE, "needs %zu bytes of workspace (bigcn_class_loss_workspace_bytes)", need);
-    cudaError_t e = launch_class_loss(ctx->stream, x, ldx, w, ldw, n, d, classes, labels, loss, lse, ctx->ws, &ctx->launches_i);
+    cudaError_t e = launch_class_loss(ctx->stream, type, x, ldx, w, ldw, n, d, classes, labels, loss, lse, ctx->ws, &ctx->launches_i);
     finish_call(ctx);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "class loss launch");
     return BIGCN_OK;
@@ -1104,7 +1104,7 @@ bigcn_status bigcn_class_loss_backward(bigcn_ctx* ctx, const void* x, const void
     if (!lse || !g_loss) return fail(ctx, BIGCN_ERR_NULL, "lse or g_loss is null");
     const size_t need = class_loss_scratch_bytes(n, d, classes, true);
     if (!ctx->ws || ctx->ws_bytes < need) return fail(ctx, BIGCN_ERR_WORKSPACE, "needs %zu bytes of workspace (bigcn_class_loss_workspace_bytes)", need);
-    cudaError_t e = launch_class_loss_backward(ctx->stream, x, ldx, w, ldw, n, d, classes, labels, lse, g_loss, g_x, ldgx, g_w, ldgw, ctx->ws, &ctx->launches_i);
+    cudaError_t e = launch_class_loss_backward(ctx->stream, type, x, ldx, w, ldw, n, d, classes, labels, lse, g_loss, g_x, ldgx, g_w, ldgw, ctx->ws, &ctx->launches_i);
     finish_call(ctx);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "class loss backward launch");
     return BIGCN_OK;

@@ -226,11 +226,11 @@ cudaError_t launch_few_rows_product(cudaStream_t s, const void* x, int type, int
 bool quantized_across(int64_t n, int m);
 int quant_timeouts();
 
-// Softmax cross entropy of bf16 rows against a class matrix, and its gradients (class_loss.cu).
+// Softmax cross entropy of bf16 or fp16 rows against a class matrix, and its gradients (class_loss.cu).
 size_t class_loss_scratch_bytes(int64_t n, int d, int classes, bool backward);
-cudaError_t launch_class_loss(cudaStream_t s, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n, int d, int classes, const int64_t* labels,
+cudaError_t launch_class_loss(cudaStream_t s, int type, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n, int d, int classes, const int64_t* labels,
                               float* loss, float* lse, void* scratch, int* launches);
-cudaError_t launch_class_loss_backward(cudaStream_t s, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n, int d, int classes, const int64_t* labels,
+cudaError_t launch_class_loss_backward(cudaStream_t s, int type, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n, int d, int classes, const int64_t* labels,
                                        const float* lse, const float* g_loss, void* g_x, int64_t ldgx, void* g_w, int64_t ldgw, void* scratch, int* launches);
 int class_loss_timeouts();
 

@@ -8,7 +8,9 @@
 // (kPieceBytes of G), turns it into G in its epilogue, and multiplies that piece into g_x and g_w; sums over pieces, and over
 // parts of a long depth, are kept in fp32 in the workspace and added in a fixed order.  G is rounded to the operands' type, the one
 // rounding besides the outputs' own: a relative error of half a step for each term of sums whose terms' errors are independent,
-// which is the size of the output's rounding.
+// which is the size of the output's rounding.  In bf16 g_i is part of G.  fp16 has no exponents for a g_i of, say, 1 / n times a small
+// probability, so there G holds (exp(z - lse) - [..]) 2^14 (down to 2^-28 in normal numbers), rows of g_x are multiplied by g_i 2^-14 in fp32, and X enters
+// g_w as rows times g_i / max |g| (one more rounding, none where all g_i are the same), the rest in fp32.
 //
 // Rows without a label take no part: the labelled ones are listed first and, unless that is all of them, copied together, so that what
 // the others hold (NaN, infinities) reaches nothing and their work is not done.  How many there are is known on the GPU only; the
@@ -87,6 +89,7 @@ struct ListArgs {
     const float* of_g_loss;
     float* to_lse;           // [n] those of the labelled ones
     float* to_g_loss;
+    unsigned* top;           // nullable: the largest magnitude of g_loss among them, as bits (0 before)
 };
 struct GatherArgs {
     const uint16_t* x;
@@ -102,8 +105,11 @@ struct GatherArgs {
     bool g_whole;
     bool pairs;              // rows of x and of `to` can be moved in words of two elements
     int span;                // rows of a warp at a time, at most 32
+    const float* g_loss;     // fp16's gradients: of every row,
+    const float* top;        // and the largest magnitude among the labelled ones;
+    uint16_t* scaled;        // rows times g / top, as `to` lies (nullable)
 };
-__device__ void gather_rows(const GatherArgs& a, int count, const int* places, int64_t first, int64_t warps);
+__device__ void gather_rows(const GatherArgs& a, int count, const int* places, int64_t first, int64_t warps, float top);
 
 // kGather: at most kScan rows, whose listing every block does for itself (the first one writes it) before it gathers its share: one launch less.
 template <bool kGather>
@@ -136,8 +142,10 @@ __global__ void __launch_bounds__(1024) list_labels_kernel(const ListArgs a, con
     for (int w = 0; w < warp; ++w) base += slot[w];
     int next = base + upto - mine, places[4];
     float none[4];
+    unsigned top = 0u;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+        if (a.top && in[i]) top = max(top, __float_as_uint(__ldg(a.of_g_loss + at + i)) & 0x7fffffffu);
         places[i] = in[i] ? next : -1;
         none[i] = v[i] < 0 ? 0.f : __uint_as_float(0x7fc00000u);
         if (in[i]) {
@@ -174,17 +182,37 @@ __global__ void __launch_bounds__(1024) list_labels_kernel(const ListArgs a, con
         total = base + upto;
         if (write && block == (kGather ? 0 : (int)gridDim.x - 1)) *a.count = base + upto;
     }
+    if (a.top) {                              // (magnitudes and NaN order as bits; the largest does not depend on the order of the blocks)
+        top = __reduce_max_sync(0xffffffffu, top);
+        __syncthreads();
+        if (lane == 0) slot[warp] = (int)top;
+        __syncthreads();
+        top = __reduce_max_sync(0xffffffffu, (unsigned)slot[lane]);
+        if (threadIdx.x == 0 && write) atomicMax(a.top, top);
+    }
     if constexpr (kGather) {
         __syncthreads();
-        gather_rows(gather, total, here, (int64_t)blockIdx.x * 32 + warp, (int64_t)gridDim.x * 32);
+        gather_rows(gather, total, here, (int64_t)blockIdx.x * 32 + warp, (int64_t)gridDim.x * 32, __uint_as_float(top));
     }
 }
 
 // A warp to `span` rows at a time, whose places its lanes read together: labelled rows are copied together, the gradient of the others is
 // zero; rows up to the next multiple of 128 are zero.
-__device__ __forceinline__ void gather_rows(const GatherArgs& a, int count, const int* places, int64_t first, int64_t warps)
+__device__ __forceinline__ void gather_rows(const GatherArgs& a, int count, const int* places, int64_t first, int64_t warps, float top)
 {
     const int lane = threadIdx.x & 31;
+    const int64_t end = ((int64_t)count + 127) / 128 * 128;
+    if (a.scaled) {
+        for (int64_t row = first; row < a.n; row += warps) {
+            const int p = places[row];
+            if (p < 0) continue;
+            const float ratio = top > 0.f ? __ldg(a.g_loss + row) / top : 0.f;
+            for (int i = lane; i < a.d; i += 32)
+                a.scaled[(int64_t)p * a.ldt + i] = __half_as_ushort(__float2half_rn(__half2float(__ushort_as_half(__ldg(a.x + row * a.ldx + i))) * ratio));
+        }
+        for (int64_t row = count + first; row < end; row += warps)
+            for (int i = lane; i < a.d; i += 32) a.scaled[row * a.ldt + i] = 0;
+    }
     if (a.whole && count == a.n) return;
     const int words = a.d / 8, rest = a.d - 8 * words;
     for (int64_t row0 = first * a.span; row0 < a.n; row0 += warps * a.span) {
@@ -233,14 +261,13 @@ __device__ __forceinline__ void gather_rows(const GatherArgs& a, int count, cons
             }
         }
     }
-    const int64_t end = ((int64_t)count + 127) / 128 * 128;
     for (int64_t row = count + first; row < end; row += warps)
         for (int i = lane; i < a.d; i += 32) a.to[row * a.ldt + i] = 0;
 }
 __global__ void __launch_bounds__(256) gather_rows_kernel(const GatherArgs a)
 {
     pdl_enter();
-    gather_rows(a, __ldg(a.count), a.place, (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), (int64_t)gridDim.x * 8);
+    gather_rows(a, __ldg(a.count), a.place, (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), (int64_t)gridDim.x * 8, a.scaled ? __ldg(a.top) : 0.f);
 }
 
 // Rows copied to 16-byte boundaries (a class matrix that does not start its rows there), in words of T where the rows allow it.
@@ -338,7 +365,10 @@ struct SumExp {
     }
 };
 
+constexpr float kHalfScale = 16384.f;         // fp16's G is this much larger
+
 // G of a tile, rounded to the operands' type; zero past the last class and the last row, which pads the depth of what reads it.
+template <int TYPE>
 struct Gradient {
     struct Args {
         const int* label;
@@ -363,7 +393,7 @@ struct Gradient {
     {
         const bool there = p.row + (int)(threadIdx.x & 31) < p.rows;
         const int label = of_row.label >= a.first_class + p.col ? of_row.label - a.first_class - p.col : INT_MIN;
-        const float lse = of_row.lse, weight = of_row.weight;
+        const float lse = of_row.lse, weight = TYPE == BIGCN_F16 ? kHalfScale : of_row.weight;
         gemm::each_chunk<BN>(p, (int)a.ldg, done, [&](int c, uint32_t (&v)[32]) {
             const int left = sh.n - (p.col + c);
             float f[32];
@@ -377,7 +407,7 @@ struct Gradient {
             }
             uint32_t w[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) w[i] = pack2<BIGCN_BF16>(f[2 * i] * weight, f[2 * i + 1] * weight);
+            for (int i = 0; i < 16; ++i) w[i] = pack2<TYPE>(f[2 * i] * weight, f[2 * i + 1] * weight);
             if (!there || left < 32) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -391,7 +421,8 @@ struct Gradient {
     }
 };
 
-// The accumulators as they are: rounded to the output, or into fp32 parts.
+// The accumulators: times a row's factor and a common one where there are such, rounded to the output, or as they are into fp32 parts.
+template <int TYPE>
 struct Store {
     struct Args {
         const int* map;      // nullable: the output row of every row
@@ -401,14 +432,25 @@ struct Store {
         float* part;         // [splits][rows][pitch], pitch a multiple of 8
         int64_t pitch, split_stride;
         bool add;            // parts: to what is there
+        const float* row_factor;     // nullable
+        const float* factor;         // nullable
+        float constant;
     };
     static __device__ int* flag() { return &g_loss_timeout; }
-    using Row = int;
-    static __device__ __forceinline__ Row row(const Args& a, int row, int rows) { return row < rows && a.map ? __ldg(a.map + row) : row; }
+    struct Row {
+        int to;
+        float factor;
+    };
+    static __device__ __forceinline__ Row row(const Args& a, int row, int rows)
+    {
+        return {row < rows && a.map ? __ldg(a.map + row) : row, (row < rows && a.row_factor ? __ldg(a.row_factor + row) : 1.f) * a.constant};
+    }
     template <int BN, class Done>
-    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit& u, const gemm::Part& p, const Row& mapped, const Done& done)
+    static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit& u, const gemm::Part& p, const Row& of_row, const Done& done)
     {
         if (p.empty && a.part && a.add) return;
+        const int mapped = of_row.to;
+        const float factor = TYPE == BIGCN_F16 ? of_row.factor * (a.factor ? __ldg(a.factor) : 1.f) : 1.f;
         gemm::each_chunk<BN>(p, sh.n, done, [&](int c, uint32_t (&v)[32]) {
             const int col = p.col + c;
             uint32_t w[16];
@@ -431,7 +473,7 @@ struct Store {
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) w[i] = pack2<BIGCN_BF16>(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+                for (int i = 0; i < 16; ++i) w[i] = pack2<TYPE>(__uint_as_float(v[2 * i]) * factor, __uint_as_float(v[2 * i + 1]) * factor);
                 if (a.whole) {
                     gemm::write_strip(p.strip, w, [&](int r, int piece, const uint4& q) {
                         const int64_t to_row = __shfl_sync(0xffffffffu, mapped, r);
@@ -513,10 +555,13 @@ struct FinishArgs {
     uint16_t* out;
     int64_t ldo;
     bool whole;
+    const float* row_factor; // as Store's
+    const float* factor;
+    float constant;
 };
 // The parts of a gradient, added in order and rounded: 8 columns to a thread, and where there are many parts of few rows, kSlices threads to
 // those, each with every kSlices-th part.
-template <int kSlices>
+template <int TYPE, int kSlices>
 __global__ void __launch_bounds__(256) finish_parts_kernel(const FinishArgs a)
 {
     pdl_enter();
@@ -552,17 +597,23 @@ __global__ void __launch_bounds__(256) finish_parts_kernel(const FinishArgs a)
         }
         if (there && slice == 0) {
             const int64_t to = a.map ? __ldg(a.map + row) : row;
-            store_elts<BIGCN_BF16, 8>(reinterpret_cast<__nv_bfloat16*>(a.out) + to * a.ldo + c, a.d - c, a.whole, f);
+            if constexpr (TYPE == BIGCN_F16) {
+                const float factor = (a.row_factor ? __ldg(a.row_factor + row) : 1.f) * a.constant * (a.factor ? __ldg(a.factor) : 1.f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] *= factor;
+            }
+            store_elts<TYPE, 8>(reinterpret_cast<typename Elt<TYPE>::T*>(a.out) + to * a.ldo + c, a.d - c, a.whole, f);
         }
     }
 }
+template <int TYPE>
 cudaError_t launch_finish(cudaStream_t s, const FinishArgs& a, int* launches)
 {
     const int64_t items = a.rows * ceil_div(a.d, 8);
     const bool many = a.splits >= 16;
     ++*launches;
     const dim3 grid((unsigned)std::min<int64_t>(8 * sm_count(), ceil_div(items, many ? 16 : 256)));
-    return many ? launch_kernel(finish_parts_kernel<16>, grid, dim3(256), 0, s, a) : launch_kernel(finish_parts_kernel<1>, grid, dim3(256), 0, s, a);
+    return many ? launch_kernel(finish_parts_kernel<TYPE, 16>, grid, dim3(256), 0, s, a) : launch_kernel(finish_parts_kernel<TYPE, 1>, grid, dim3(256), 0, s, a);
 }
 
 // ---- plan ------------------------------------------------------------------------------------------------------------------
@@ -602,10 +653,10 @@ struct Plan {
     int64_t pitch;                            // of fp32 parts
     size_t bytes;
     // offsets
-    size_t kept, label, place, count, counts, lse, g_loss, x, w, at, part, g, px, pw;
+    size_t kept, label, place, count, counts, lse, g_loss, x, w, scaled, top, at, part, g, px, pw;
 };
 
-Plan make_plan(int64_t n, int d, int classes, bool backward, bool align_w)
+Plan make_plan(int64_t n, int d, int classes, bool backward, bool half)
 {
     Plan p = {};
     p.n_pad = round_up(std::max<int64_t>(n, 1), 128);
@@ -623,7 +674,11 @@ Plan make_plan(int64_t n, int d, int classes, bool backward, bool align_w)
         p.g_loss = take((size_t)p.n_pad * 4);
     }
     p.x = take((size_t)p.n_pad * p.ldt * 2);
-    if (align_w) p.w = take((size_t)classes * p.ldt * 2);
+    p.w = take((size_t)classes * p.ldt * 2);                    // (the class matrix laid on boundaries, where it is not)
+    if (backward && half) {
+        p.scaled = take((size_t)p.n_pad * p.ldt * 2);
+        p.top = take(sizeof(unsigned));
+    }
     if (!backward) {
         p.parts = (int)ceil_div(classes, p.bn);
         p.rows = p.parts == 1 ? p.n_pad : std::min(p.n_pad, std::max<int64_t>(2048, kPieceBytes / (8 * (int64_t)p.parts) / 128 * 128));
@@ -661,12 +716,14 @@ struct Operands {
 };
 
 // Lists the labelled rows, copies them together where that is needed, and lays the class matrix on 16-byte boundaries.
-cudaError_t prepare(cudaStream_t s, const Plan& p, char* ws, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n, int d, int classes,
+cudaError_t prepare(cudaStream_t s, const Plan& p, char* ws, int type, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n, int d, int classes,
                     const int64_t* labels, float* loss, float* lse, const float* of_lse, const float* of_g_loss, void* g_x, int64_t ldgx, Operands* o, int* launches)
 {
     int* counts = reinterpret_cast<int*>(ws + p.counts);
+    unsigned* top = type == BIGCN_F16 && of_g_loss ? reinterpret_cast<unsigned*>(ws + p.top) : nullptr;
     const int blocks = (int)ceil_div(n, kScan);
-    cudaError_t e = cudaSuccess;
+    cudaError_t e = top ? cudaMemsetAsync(top, 0, sizeof(unsigned), s) : cudaSuccess;
+    if (e != cudaSuccess) return e;
     if (blocks > 1) {
         ++*launches;
         e = launch_kernel(count_labels_kernel, dim3(blocks), dim3(1024), 0, s, labels, n, classes, counts);
@@ -675,11 +732,12 @@ cudaError_t prepare(cudaStream_t s, const Plan& p, char* ws, const void* x, int6
     const ListArgs list = {labels, n, classes, counts, reinterpret_cast<int*>(ws + p.kept), reinterpret_cast<int*>(ws + p.label),
                            reinterpret_cast<int*>(ws + p.place), reinterpret_cast<int*>(ws + p.count), loss, lse,
                            (reinterpret_cast<uintptr_t>(loss) | reinterpret_cast<uintptr_t>(lse)) % 16 == 0, of_lse, of_g_loss,
-                           reinterpret_cast<float*>(ws + p.lse), reinterpret_cast<float*>(ws + p.g_loss)};
+                           reinterpret_cast<float*>(ws + p.lse), reinterpret_cast<float*>(ws + p.g_loss), top};
     *o = {x, ldx, rows_whole(x, ldx, BIGCN_BF16, 8), reinterpret_cast<const uint16_t*>(ws + p.x), w, ldw};
     const int span = (int)std::max<int64_t>(1, std::min<int64_t>(32, n / (64 * sm_count())));     // as many warps as the machine holds, first
     const GatherArgs gather = {static_cast<const uint16_t*>(x), ldx, n, d, o->x_whole, list.place, list.count, reinterpret_cast<uint16_t*>(ws + p.x), p.ldt,
-                               static_cast<uint16_t*>(g_x), ldgx, rows_whole(g_x, ldgx, BIGCN_BF16, 8), rows_whole(x, ldx, BIGCN_BF16, 2), span};
+                               static_cast<uint16_t*>(g_x), ldgx, rows_whole(g_x, ldgx, BIGCN_BF16, 8), rows_whole(x, ldx, BIGCN_BF16, 2), span, of_g_loss,
+                               reinterpret_cast<const float*>(top), top ? reinterpret_cast<uint16_t*>(ws + p.scaled) : nullptr};
     ++*launches;
     if (n <= kScan) {
         e = launch_kernel(list_labels_kernel<true>, dim3((unsigned)std::min<int64_t>(ceil_div(n, 32), sm_count())), dim3(1024), 0, s, list, gather);
@@ -718,7 +776,7 @@ cudaError_t row_maps(CUtensorMap* copied, CUtensorMap* own, const Plan& p, const
 
 template <int BN, int CTAS, class Epi>
 cudaError_t launch_logits(cudaStream_t s, const Plan& p, const Operands& o, int64_t n, int d, int classes, int64_t first_row, int64_t rows, int64_t first_class,
-                          const int* count, const typename Epi::Args& args, int* launches)
+                          const int* count, int type, const typename Epi::Args& args, int* launches)
 {
     CUtensorMap a, b, own;
     cudaError_t e = row_maps(&a, &own, p, o, n, d, first_row, 64, gemm::kRows);
@@ -732,27 +790,109 @@ cudaError_t launch_logits(cudaStream_t s, const Plan& p, const Operands& o, int6
     sh.of = (int)n;
     sh.base = (int)first_row;
     sh.alt_a = o.x_whole;
+    sh.half = type == BIGCN_F16;
     ++*launches;
     return gemm::launch<false, BN, CTAS, false, false, Epi>(s, a, b, own, sh, args);
 }
 template <class Epi>
 cudaError_t pick_logits(cudaStream_t s, int bn, const Plan& p, const Operands& o, int64_t n, int d, int classes, int64_t first_row, int64_t rows, int64_t first_class,
-                        const int* count, const typename Epi::Args& args, int* launches)
+                        const int* count, int type, const typename Epi::Args& args, int* launches)
 {
-    if (bn == 64) return launch_logits<64, 1, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, args, launches);
-    if (bn == 128) return launch_logits<128, 1, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, args, launches);
-    if (rows > gemm::kRows) return launch_logits<256, 2, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, args, launches);
-    return launch_logits<256, 1, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, args, launches);
+    if (bn == 64) return launch_logits<64, 1, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, type, args, launches);
+    if (bn == 128) return launch_logits<128, 1, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, type, args, launches);
+    if (rows > gemm::kRows) return launch_logits<256, 2, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, type, args, launches);
+    return launch_logits<256, 1, Epi>(s, p, o, n, d, classes, first_row, rows, first_class, count, type, args, launches);
 }
 
 // g_x = G W (columns of W outside, its rows the depth) and g_w = G^T X.
-template <bool A_MN>
-cudaError_t launch_gradient(cudaStream_t s, int bn, const CUtensorMap& g, const CUtensorMap& b, const CUtensorMap& own, const gemm::Shape& sh, const Store::Args& args)
+template <int TYPE, bool A_MN>
+cudaError_t launch_gradient(cudaStream_t s, int bn, const CUtensorMap& g, const CUtensorMap& b, const CUtensorMap& own, const gemm::Shape& sh, const typename Store<TYPE>::Args& args)
 {
-    if (bn == 64) return gemm::launch<false, 64, 1, A_MN, true, Store>(s, g, b, own, sh, args);
-    if (bn == 128) return gemm::launch<false, 128, 1, A_MN, true, Store>(s, g, b, own, sh, args);
-    if (sh.m > gemm::kRows) return gemm::launch<false, 256, 2, A_MN, true, Store>(s, g, b, own, sh, args);
-    return gemm::launch<false, 256, 1, A_MN, true, Store>(s, g, b, own, sh, args);
+    if (bn == 64) return gemm::launch<false, 64, 1, A_MN, true, Store<TYPE>>(s, g, b, own, sh, args);
+    if (bn == 128) return gemm::launch<false, 128, 1, A_MN, true, Store<TYPE>>(s, g, b, own, sh, args);
+    if (sh.m > gemm::kRows) return gemm::launch<false, 256, 2, A_MN, true, Store<TYPE>>(s, g, b, own, sh, args);
+    return gemm::launch<false, 256, 1, A_MN, true, Store<TYPE>>(s, g, b, own, sh, args);
+}
+
+template <int TYPE>
+cudaError_t backward_as(cudaStream_t s, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n, int d, int classes, const int64_t* labels,
+                                       const float* lse, const float* g_loss, void* g_x, int64_t ldgx, void* g_w, int64_t ldgw, void* scratch, int* launches)
+{
+    char* ws = static_cast<char*>(scratch);
+    cudaError_t e;
+    constexpr int type = TYPE;
+    constexpr bool half = TYPE == BIGCN_F16;
+    const Plan p = make_plan(n, d, classes, true, half);
+    Operands o;
+    e = prepare(s, p, ws, type, x, ldx, w, ldw, n, d, classes, labels, nullptr, nullptr, lse, g_loss, g_x, ldgx, &o, launches);
+    const int* count = reinterpret_cast<const int*>(ws + p.count);
+    const int* kept = reinterpret_cast<const int*>(ws + p.kept);
+    const int* label = reinterpret_cast<const int*>(ws + p.label);
+    uint16_t* g = reinterpret_cast<uint16_t*>(ws + p.g);
+    const bool parts_x = p.splits_x > 1 || p.col_pieces > 1, parts_w = p.splits_w > 1 || p.row_pieces > 1;
+    for (int c = 0; c < p.col_pieces && e == cudaSuccess; ++c) {
+        const int64_t first_class = c * p.cols;
+        const int here = (int)std::min<int64_t>(p.cols, classes - first_class);
+        const int64_t ldg = round_up(here, 64);
+        for (int r = 0; r < p.row_pieces && e == cudaSuccess; ++r) {
+            const int64_t first = r * p.rows, rows = std::min(p.rows, n - first);
+            if (rows <= 0) break;
+            const typename Gradient<TYPE>::Args ga = {label + first, reinterpret_cast<const float*>(ws + p.lse) + first, reinterpret_cast<const float*>(ws + p.g_loss) + first, (int)first_class, g, ldg};
+            e = pick_logits<Gradient<TYPE>>(s, tile_cols(here), p, o, n, d, here, first, rows, first_class, count, type, ga, launches);
+            if (e != cudaSuccess) break;
+            gemm::Shape sh;
+            sh.n = d;
+            sh.count = count;
+            sh.of = (int)n;
+            sh.base = (int)first;
+            sh.half = half;
+            if (g_x) {
+                CUtensorMap mg, mw;
+                e = gemm::encode_map(&mg, g, 2, false, round_up(rows, 128), ldg, ldg * 2, 64, gemm::kRows);
+                if (e == cudaSuccess) e = gemm::encode_map(&mw, static_cast<const uint16_t*>(o.w) + first_class * o.ldw, 2, false, here, d, o.ldw * 2, 64, 64);
+                if (e != cudaSuccess) break;
+                sh.m = (int)rows;
+                sh.k = here;
+                sh.splits = p.splits_x;
+                const typename Store<TYPE>::Args args = {kept + first, static_cast<uint16_t*>(g_x), ldgx, rows_whole(g_x, ldgx, BIGCN_BF16, 8),
+                                          parts_x ? reinterpret_cast<float*>(ws + p.px) + first * p.pitch : nullptr, p.pitch, p.n_pad * p.pitch, c > 0,
+                                          half ? reinterpret_cast<const float*>(ws + p.g_loss) + first : nullptr, nullptr, half ? 1.f / kHalfScale : 1.f};
+                ++*launches;
+                e = launch_gradient<TYPE, false>(s, p.bn_d, mg, mw, mw, sh, args);
+                if (e == cudaSuccess && parts_x && c == p.col_pieces - 1) {
+                    const FinishArgs fa = {args.part, p.splits_x, args.split_stride, p.pitch, count, (int)first, rows, d, kept + first, static_cast<uint16_t*>(g_x), ldgx, args.whole, args.row_factor, args.factor, args.constant};
+                    e = launch_finish<TYPE>(s, fa, launches);
+                }
+                if (e != cudaSuccess) break;
+            }
+            if (g_w) {
+                CUtensorMap mg, mx, own;
+                e = gemm::encode_map(&mg, g, 2, false, round_up(rows, 128), ldg, ldg * 2, 64, 64);
+                if (e == cudaSuccess && half) {
+                    e = gemm::encode_map(&mx, reinterpret_cast<const uint16_t*>(ws + p.scaled) + first * p.ldt, 2, false, p.n_pad - first, d, p.ldt * 2, 64, 64);
+                    own = mx;
+                } else if (e == cudaSuccess) {
+                    e = row_maps(&mx, &own, p, o, n, d, first, 64, 64);
+                }
+                if (e != cudaSuccess) break;
+                sh.m = here;
+                sh.k = (int)rows;
+                sh.splits = p.splits_w;
+                sh.over_depth = true;
+                sh.alt_b = o.x_whole && !half;
+                uint16_t* out = static_cast<uint16_t*>(g_w) + first_class * ldgw;
+                const typename Store<TYPE>::Args args = {nullptr, out, ldgw, rows_whole(out, ldgw, BIGCN_BF16, 8), parts_w ? reinterpret_cast<float*>(ws + p.pw) : nullptr, p.pitch,
+                                          round_up(p.cols, 128) * p.pitch, r > 0, nullptr, half ? reinterpret_cast<const float*>(ws + p.top) : nullptr, half ? 1.f / kHalfScale : 1.f};
+                ++*launches;
+                e = launch_gradient<TYPE, true>(s, p.bn_d, mg, mx, own, sh, args);
+                if (e == cudaSuccess && parts_w && r == p.row_pieces - 1) {
+                    const FinishArgs fa = {args.part, p.splits_w, args.split_stride, p.pitch, nullptr, 0, here, d, nullptr, out, ldgw, args.whole, args.row_factor, args.factor, args.constant};
+                    e = launch_finish<TYPE>(s, fa, launches);
+                }
+            }
+        }
+    }
+    return e;
 }
 
 }  // namespace
@@ -766,14 +906,14 @@ int class_loss_timeouts()
 
 size_t class_loss_scratch_bytes(int64_t n, int d, int classes, bool backward) { return make_plan(n, d, classes, backward, true).bytes; }
 
-cudaError_t launch_class_loss(cudaStream_t s, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n, int d, int classes, const int64_t* labels,
+cudaError_t launch_class_loss(cudaStream_t s, int type, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n, int d, int classes, const int64_t* labels,
                               float* loss, float* lse, void* scratch, int* launches)
 {
     char* ws = static_cast<char*>(scratch);
     cudaError_t e;
-    const Plan p = make_plan(n, d, classes, false, true);
+    const Plan p = make_plan(n, d, classes, false, false);
     Operands o;
-    e = prepare(s, p, ws, x, ldx, w, ldw, n, d, classes, labels, loss, lse, nullptr, nullptr, nullptr, 0, &o, launches);
+    e = prepare(s, p, ws, type, x, ldx, w, ldw, n, d, classes, labels, loss, lse, nullptr, nullptr, nullptr, 0, &o, launches);
     const int* count = reinterpret_cast<const int*>(ws + p.count);
     const int* kept = reinterpret_cast<const int*>(ws + p.kept);
     float* at = reinterpret_cast<float*>(ws + p.at);
@@ -783,7 +923,7 @@ cudaError_t launch_class_loss(cudaStream_t s, const void* x, int64_t ldx, const 
         if (rows <= 0) break;
         const bool direct = p.parts == 1;
         const SumExp::Args args = {reinterpret_cast<const int*>(ws + p.label) + first, part, p.rows, at, direct ? kept + first : nullptr, loss, lse};
-        e = pick_logits<SumExp>(s, p.bn, p, o, n, d, classes, first, rows, 0, count, args, launches);
+        e = pick_logits<SumExp>(s, p.bn, p, o, n, d, classes, first, rows, 0, count, type, args, launches);
         if (e != cudaSuccess || direct) continue;
         ++*launches;
         const auto blocks = [&](int rows_per_block) { return dim3((unsigned)std::min<int64_t>(ceil_div(rows, rows_per_block), 16 * sm_count())); };
@@ -795,75 +935,12 @@ cudaError_t launch_class_loss(cudaStream_t s, const void* x, int64_t ldx, const 
     return e;
 }
 
-cudaError_t launch_class_loss_backward(cudaStream_t s, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n, int d, int classes, const int64_t* labels,
-                                       const float* lse, const float* g_loss, void* g_x, int64_t ldgx, void* g_w, int64_t ldgw, void* scratch, int* launches)
+cudaError_t launch_class_loss_backward(cudaStream_t s, int type, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n, int d, int classes,
+                                       const int64_t* labels, const float* lse, const float* g_loss, void* g_x, int64_t ldgx, void* g_w, int64_t ldgw,
+                                       void* scratch, int* launches)
 {
-    char* ws = static_cast<char*>(scratch);
-    cudaError_t e;
-    const Plan p = make_plan(n, d, classes, true, true);
-    Operands o;
-    e = prepare(s, p, ws, x, ldx, w, ldw, n, d, classes, labels, nullptr, nullptr, lse, g_loss, g_x, ldgx, &o, launches);
-    const int* count = reinterpret_cast<const int*>(ws + p.count);
-    const int* kept = reinterpret_cast<const int*>(ws + p.kept);
-    const int* label = reinterpret_cast<const int*>(ws + p.label);
-    uint16_t* g = reinterpret_cast<uint16_t*>(ws + p.g);
-    const bool parts_x = p.splits_x > 1 || p.col_pieces > 1, parts_w = p.splits_w > 1 || p.row_pieces > 1;
-    for (int c = 0; c < p.col_pieces && e == cudaSuccess; ++c) {
-        const int64_t first_class = c * p.cols;
-        const int here = (int)std::min<int64_t>(p.cols, classes - first_class);
-        const int64_t ldg = round_up(here, 64);
-        for (int r = 0; r < p.row_pieces && e == cudaSuccess; ++r) {
-            const int64_t first = r * p.rows, rows = std::min(p.rows, n - first);
-            if (rows <= 0) break;
-            const Gradient::Args ga = {label + first, reinterpret_cast<const float*>(ws + p.lse) + first, reinterpret_cast<const float*>(ws + p.g_loss) + first, (int)first_class, g, ldg};
-            e = pick_logits<Gradient>(s, tile_cols(here), p, o, n, d, here, first, rows, first_class, count, ga, launches);
-            if (e != cudaSuccess) break;
-            gemm::Shape sh;
-            sh.n = d;
-            sh.count = count;
-            sh.of = (int)n;
-            sh.base = (int)first;
-            if (g_x) {
-                CUtensorMap mg, mw;
-                e = gemm::encode_map(&mg, g, 2, false, round_up(rows, 128), ldg, ldg * 2, 64, gemm::kRows);
-                if (e == cudaSuccess) e = gemm::encode_map(&mw, static_cast<const uint16_t*>(o.w) + first_class * o.ldw, 2, false, here, d, o.ldw * 2, 64, 64);
-                if (e != cudaSuccess) break;
-                sh.m = (int)rows;
-                sh.k = here;
-                sh.splits = p.splits_x;
-                const Store::Args args = {kept + first, static_cast<uint16_t*>(g_x), ldgx, rows_whole(g_x, ldgx, BIGCN_BF16, 8),
-                                          parts_x ? reinterpret_cast<float*>(ws + p.px) + first * p.pitch : nullptr, p.pitch, p.n_pad * p.pitch, c > 0};
-                ++*launches;
-                e = launch_gradient<false>(s, p.bn_d, mg, mw, mw, sh, args);
-                if (e == cudaSuccess && parts_x && c == p.col_pieces - 1) {
-                    const FinishArgs fa = {args.part, p.splits_x, args.split_stride, p.pitch, count, (int)first, rows, d, kept + first, static_cast<uint16_t*>(g_x), ldgx, args.whole};
-                    e = launch_finish(s, fa, launches);
-                }
-                if (e != cudaSuccess) break;
-            }
-            if (g_w) {
-                CUtensorMap mg, mx, own;
-                e = gemm::encode_map(&mg, g, 2, false, round_up(rows, 128), ldg, ldg * 2, 64, 64);
-                if (e == cudaSuccess) e = row_maps(&mx, &own, p, o, n, d, first, 64, 64);
-                if (e != cudaSuccess) break;
-                sh.m = here;
-                sh.k = (int)rows;
-                sh.splits = p.splits_w;
-                sh.over_depth = true;
-                sh.alt_b = o.x_whole;
-                uint16_t* out = static_cast<uint16_t*>(g_w) + first_class * ldgw;
-                const Store::Args args = {nullptr, out, ldgw, rows_whole(out, ldgw, BIGCN_BF16, 8), parts_w ? reinterpret_cast<float*>(ws + p.pw) : nullptr, p.pitch,
-                                          round_up(p.cols, 128) * p.pitch, r > 0};
-                ++*launches;
-                e = launch_gradient<true>(s, p.bn_d, mg, mx, own, sh, args);
-                if (e == cudaSuccess && parts_w && r == p.row_pieces - 1) {
-                    const FinishArgs fa = {args.part, p.splits_w, args.split_stride, p.pitch, nullptr, 0, here, d, nullptr, out, ldgw, args.whole};
-                    e = launch_finish(s, fa, launches);
-                }
-            }
-        }
-    }
-    return e;
+    return type == BIGCN_F16 ? backward_as<BIGCN_F16>(s, x, ldx, w, ldw, n, d, classes, labels, lse, g_loss, g_x, ldgx, g_w, ldgw, scratch, launches)
+                             : backward_as<BIGCN_BF16>(s, x, ldx, w, ldw, n, d, classes, labels, lse, g_loss, g_x, ldgx, g_w, ldgw, scratch, launches);
 }
 
 }  // namespace bigcn

@@ -51,7 +51,14 @@ def reference(x, W, labels, g_loss):
     chain = (W.shape[0] / 16 + 20) * 2 * U
     off = G.abs() * (half + chain) + p * g_loss[kept].abs().double()[:, None] * (3 * zerr[:, None] + 300 * U)
     chain_w = (n / 16 + 20) * 2 * U
-    off_w = G.abs() * (half + chain_w) + p * g_loss[kept].abs().double()[:, None] * (3 * zerr[:, None] + 300 * U)
+    once_more = half if x.dtype == torch.float16 else 0.0           # rows of x times g_loss / max |g_loss| are rounded, too
+    off_w = G.abs() * (half + once_more + chain_w) + p * g_loss[kept].abs().double()[:, None] * (3 * zerr[:, None] + 300 * U)
+
+    if x.dtype == torch.float16:                                    # 2^14 G below the normal range: half a step, 2^-25
+        least = 2.0 ** -39 * g_loss[kept].abs().double()[:, None]
+        off, off_w = off + least, off_w + least
+    # and the rows of x, scaled, below theirs: 2^-25 of the largest weight
+    low = (p - one).abs().sum(0)[:, None] * 2.0 ** -25 * g_loss[kept].abs().double().max() if x.dtype == torch.float16 and kept.numel() else 0.0
 
     def whole(v):
         out = torch.zeros((n,) + v.shape[1:], dtype=torch.float64, device=x.device)
@@ -61,7 +68,7 @@ def reference(x, W, labels, g_loss):
     gx, gw = G @ wd, G.t() @ xd
     return {"loss": (whole(lse - at), whole(2 * zerr + 136 * U + 4 * U * (lse.abs() + at.abs()))),
             "lse": (whole(lse), whole(zerr + 136 * U + 4 * U * (lse.abs() + at.abs()))),
-            "g_x": (whole(gx), whole(gx.abs() * half + 1.01 * off @ wd.abs())), "g_w": (gw, gw.abs() * half + 1.01 * off_w.t() @ xd.abs())}
+            "g_x": (whole(gx), whole(gx.abs() * half + 1.01 * off @ wd.abs())), "g_w": (gw, gw.abs() * half + 1.01 * off_w.t() @ xd.abs() + low)}
 
 
 def check(ctx, x, W, labels, g_loss):
@@ -85,6 +92,34 @@ SIZES = [(1, 1, 1), (1, 8, 2), (2, 16, 3), (5, 17, 7), (1, 64, 1000), (3, 100, 3
 @pytest.mark.parametrize("n,d,classes", SIZES)
 def test_loss_and_gradients(ctx, n, d, classes):
     check(ctx, *problem(n, d, classes, n + d))
+
+
+@pytest.mark.parametrize("n,d,classes", SIZES)
+def test_loss_and_gradients_in_fp16(ctx, n, d, classes):
+    x, W, labels, g_loss = problem(n, d, classes, n + d, dtype=torch.float16)
+    check(ctx, x, W, labels, torch.full_like(g_loss, 1.0 / n))
+    check(ctx, x, W, labels, g_loss * torch.where(torch.arange(n, device="cuda") % 3 == 0, -1.0, 1.0))
+
+
+@pytest.mark.parametrize("n,labelled,pad,shift", [(200, 0.0, 0, 0), (200, 0.5, 0, 0), (5000, 0.05, 0, 0), (6000, 0.97, 0, 0), (6000, 1.0, 0, 0), (150, 0.4, 5, 1)])
+def test_fp16_rows_without_a_label(ctx, n, labelled, pad, shift):
+    x, W, labels, g_loss = problem(n, 64, 300, n, labelled, dtype=torch.float16, pad=pad, shift=shift)
+    out = check(ctx, x, W, labels, g_loss)
+    bad = x.clone()
+    bad[labels < 0] = float("nan")
+    g_bad = torch.where(labels < 0, torch.full_like(g_loss, float("nan")), g_loss)
+    loss, lse = ctx.class_loss(bad, W, labels)
+    got = (loss, lse) + ctx.class_loss_backward(bad, W, labels, lse, g_bad)
+    ctx.sync_check()
+    assert all(torch.equal(a, b) for a, b in zip(out, got))
+
+
+def test_fp16_with_a_gradient_of_nothing(ctx):
+    x, W, labels, g_loss = problem(90, 64, 300, 3, dtype=torch.float16)
+    _, lse = ctx.class_loss(x, W, labels)
+    g_x, g_w = ctx.class_loss_backward(x, W, labels, lse, torch.zeros_like(g_loss))
+    ctx.sync_check()
+    assert (g_x == 0).all() and (g_w == 0).all()
 
 
 @pytest.mark.parametrize("n,d,classes", [(1, 8, 2), (5, 17, 7), (140, 64, 7), (300, 130, 260), (5000, 64, 47), (4097, 24, 5), (20000, 16, 3)])

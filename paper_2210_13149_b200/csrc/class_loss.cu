@@ -696,8 +696,8 @@ Plan make_plan(int64_t n, int d, int classes, bool backward, bool half)
         p.col_pieces = (int)ceil_div(classes, p.cols);
         p.bn_d = tile_cols(d);
         p.pitch = round_up(d, 8);
-        p.splits_x = pick_splits(p.rows, d, p.cols / 64, 8);
-        p.splits_w = pick_splits(p.cols, d, p.rows / 64, 148);
+        p.splits_x = pick_splits(std::min<int64_t>(p.rows, std::max<int64_t>(n, 1)), d, p.cols / 64, 148);
+        p.splits_w = pick_splits(std::min<int64_t>(p.cols, classes), d, p.rows / 64, 148);
         p.g = take((size_t)p.rows * p.cols * 2);
         if (p.splits_x > 1 || p.col_pieces > 1) p.px = take((size_t)p.splits_x * p.n_pad * p.pitch * 4);
         if (p.splits_w > 1 || p.row_pieces > 1) p.pw = take((size_t)p.splits_w * round_up(p.cols, 128) * p.pitch * 4);
@@ -779,10 +779,11 @@ cudaError_t launch_logits(cudaStream_t s, const Plan& p, const Operands& o, int6
                           const int* count, int type, const typename Epi::Args& args, int* launches)
 {
     CUtensorMap a, b, own;
-    cudaError_t e = row_maps(&a, &own, p, o, n, d, first_row, 64, gemm::kRows);
+    gemm::Shape sh;
+    if (CTAS == 1) sh.tile_rows = gemm::rows_of_one_tile(rows);
+    cudaError_t e = row_maps(&a, &own, p, o, n, d, first_row, 64, sh.tile_rows);
     if (e == cudaSuccess) e = gemm::encode_map(&b, static_cast<const uint16_t*>(o.w) + first_class * o.ldw, 2, false, classes, d, o.ldw * 2, 64, BN / CTAS);
     if (e != cudaSuccess) return e;
-    gemm::Shape sh;
     sh.m = (int)rows;
     sh.n = classes;
     sh.k = d;
@@ -791,6 +792,7 @@ cudaError_t launch_logits(cudaStream_t s, const Plan& p, const Operands& o, int6
     sh.base = (int)first_row;
     sh.alt_a = o.x_whole;
     sh.half = type == BIGCN_F16;
+    sh.rotate = rows <= gemm::kRows;          // classes are read once
     ++*launches;
     return gemm::launch<false, BN, CTAS, false, false, Epi>(s, a, b, own, sh, args);
 }
@@ -848,7 +850,8 @@ cudaError_t backward_as(cudaStream_t s, const void* x, int64_t ldx, const void* 
             sh.half = half;
             if (g_x) {
                 CUtensorMap mg, mw;
-                e = gemm::encode_map(&mg, g, 2, false, round_up(rows, 128), ldg, ldg * 2, 64, gemm::kRows);
+                sh.tile_rows = gemm::rows_of_one_tile(rows);
+                e = gemm::encode_map(&mg, g, 2, false, round_up(rows, 128), ldg, ldg * 2, 64, sh.tile_rows);
                 if (e == cudaSuccess) e = gemm::encode_map(&mw, static_cast<const uint16_t*>(o.w) + first_class * o.ldw, 2, false, here, d, o.ldw * 2, 64, 64);
                 if (e != cudaSuccess) break;
                 sh.m = (int)rows;
@@ -927,9 +930,10 @@ cudaError_t launch_class_loss(cudaStream_t s, int type, const void* x, int64_t l
         if (e != cudaSuccess || direct) continue;
         ++*launches;
         const auto blocks = [&](int rows_per_block) { return dim3((unsigned)std::min<int64_t>(ceil_div(rows, rows_per_block), 16 * sm_count())); };
-        // rows side by side where there are enough of them, else threads side by side over a row's parts
+        // rows side by side where there are enough of them, else threads side by side over a row's parts (512 parts of 128 rows in us: 26 with
+        // 32 rows to a block, 8 with four)
         if (p.parts <= 16) e = launch_kernel(join_loss_kernel<256>, blocks(256), dim3(256), 0, s, (const float2*)part, p.parts, p.rows, count, (int)first, (int)rows, kept, (const float*)at, loss, lse);
-        else if (rows >= 32) e = launch_kernel(join_loss_kernel<32>, blocks(32), dim3(256), 0, s, (const float2*)part, p.parts, p.rows, count, (int)first, (int)rows, kept, (const float*)at, loss, lse);
+        else if (rows >= 4096) e = launch_kernel(join_loss_kernel<32>, blocks(32), dim3(256), 0, s, (const float2*)part, p.parts, p.rows, count, (int)first, (int)rows, kept, (const float*)at, loss, lse);
         else e = launch_kernel(join_loss_kernel<4>, blocks(4), dim3(256), 0, s, (const float2*)part, p.parts, p.rows, count, (int)first, (int)rows, kept, (const float*)at, loss, lse);
     }
     return e;

@@ -42,6 +42,9 @@ struct Shape {
     int of = 0, base = 0;
     bool over_depth = false, alt_a = false, alt_b = false;
     int tile_rows = kRows;   // rows of a tile that count (a multiple of 8; the accumulators have 128), one block to a tile, K-major A
+    bool rotate = false;     // each block begins with another step of the depth.  For operands that are read once: blocks that all begin at the first
+                             // 128 bytes of rows a power of two apart keep to a part of the memory channels (131,072 8-bit classes x 2,048 for
+                             // eight rows in us: 73, 47 so).  Sums of floats are then taken in an order that depends on the tile.
     bool a_ahead = false;    // A does not come from the kernel before this one (which let this one start early): its first stages are
                              // fetched while that one runs.  No count, one block to a tile.
 };
@@ -347,6 +350,11 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     int* const flag = Epi::flag();
 
     int early = 0;           // stages whose A is on its way
+    const auto depth_at = [&](const Unit& t, int k) {        // of the stage k in [k0, k1)
+        if (!shape.rotate) return k;
+        const int steps = t.k1 - t.k0, at = k - t.k0 + (int)(blockIdx.x % (unsigned)steps);
+        return t.k0 + (at < steps ? at : at - steps);
+    };
     if (CTAS == 1 && !A_MN && shape.a_ahead && threadIdx.x == kProducer * 32) {
         const Walk walk(shape, shape.tile_rows, BN, kDepth);
         if ((int)blockIdx.x < walk.units()) {
@@ -354,7 +362,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             early = min(t.k1 - t.k0, C::kStages);
             for (int i = 0; i < early; ++i) {
                 expect_bytes<CTAS>(&ctl.full[i], shape.tile_rows * kDepthBytes + C::kBBytes);
-                copy_box<CTAS>(tc::smem_u32(stages + i * C::kStage), &map_a, (t.k0 + i) * kDepth, t.row, &ctl.full[i]);
+                copy_box<CTAS>(tc::smem_u32(stages + i * C::kStage), &map_a, depth_at(t, t.k0 + i) * kDepth, t.row, &ctl.full[i]);
             }
         }
     }
@@ -378,21 +386,22 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 for (int k = t.k0; k < t.k1; ++k) {
                     ok = wait(&ctl.empty[slot], phase ^ 1u, abort, flag);
                     if (!ok) break;
+                    const int at = depth_at(t, k) * kDepth;
                     const bool fetched = issued < early;
                     if (rank == 0 && !fetched) expect_bytes<CTAS>(&ctl.full[slot], stage_bytes * CTAS);
                     const uint32_t sa = tc::smem_u32(stages + slot * C::kStage), sb = sa + C::kABytes;
                     if (fetched) {
                     } else if constexpr (A_MN) {
 #pragma unroll
-                        for (int i = 0; i < kRows / 64; ++i) copy_box<CTAS>(sa + i * 8192, ma, arow + 64 * i, k * kDepth, &ctl.full[slot]);
+                        for (int i = 0; i < kRows / 64; ++i) copy_box<CTAS>(sa + i * 8192, ma, arow + 64 * i, at, &ctl.full[slot]);
                     } else {
-                        copy_box<CTAS>(sa, ma, k * kDepth, arow, &ctl.full[slot]);
+                        copy_box<CTAS>(sa, ma, at, arow, &ctl.full[slot]);
                     }
                     if constexpr (B_MN) {
 #pragma unroll
-                        for (int i = 0; i < C::kBRows / 64; ++i) copy_box<CTAS>(sb + i * 8192, mb, brow + 64 * i, k * kDepth, &ctl.full[slot]);
+                        for (int i = 0; i < C::kBRows / 64; ++i) copy_box<CTAS>(sb + i * 8192, mb, brow + 64 * i, at, &ctl.full[slot]);
                     } else {
-                        copy_box<CTAS>(sb, mb, k * kDepth, brow, &ctl.full[slot]);
+                        copy_box<CTAS>(sb, mb, at, brow, &ctl.full[slot]);
                     }
                     ++issued;
                     if (++slot == C::kStages) slot = 0, phase ^= 1u;
@@ -503,6 +512,9 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 }
 
 // ---- host pieces ---------------------------------------------------------------------------------------------------------
+
+// Rows that a tile reads: of few rows no more than there are, since rows past the tensor's end cost their bytes between L2 and shared memory, too.
+inline int rows_of_one_tile(int64_t rows) { return rows >= kRows ? kRows : (int)round_up(rows, 8); }
 
 // Tensor map of a row-major matrix (rows x cols elements of `elt` bytes, `pitch` bytes from row to row; base and pitch on 16-byte
 // boundaries), read in swizzled boxes of box_cols x box_rows.

@@ -368,7 +368,7 @@ template <int BN, int CTAS>
 cudaError_t launch_product_as(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const int8_t* q_w, int64_t ldqw, const gemm::Shape& shape, const ScaledOut::Args& args)
 {
     CUtensorMap ma, mb;
-    cudaError_t e = gemm::encode_map(&ma, q_x, 1, true, shape.m, shape.k, ldqx, 128, gemm::kRows);
+    cudaError_t e = gemm::encode_map(&ma, q_x, 1, true, shape.m, shape.k, ldqx, 128, shape.tile_rows);
     if (e == cudaSuccess) e = gemm::encode_map(&mb, q_w, 1, true, shape.n, shape.k, ldqw, 128, BN / CTAS);
     if (e != cudaSuccess) return e;
     return gemm::launch<true, BN, CTAS, false, false, ScaledOut>(s, ma, mb, ma, shape, args);
@@ -393,15 +393,16 @@ int quant_timeouts()
     return v;
 }
 
-// Whether that is expected to be the faster one, of what each takes in us: a launch from Python, 11 and 14.5; the class rows' bytes; and the
-// steps of a class row in one of 2,368 warps (16 bytes a lane are a load and four dot products a row, and every row's sum a reduction and a store).
-// Measured for 1, 2, 3, 4 rows against what two kernels take: 65,536 classes x 1,024 15.7, 18.6, 23.7, 24.8 against 18.5; 32,768 x 4,096 24, 28,
-// 34, 35 against 32; 200,000 x 256 22, 29, 41, 45 against 20; 30,011 x 602 11.3, 11.3, 14.2, 14.7 against 14.7; 4,096 x 256 11 against 14.6.
+// Whether that is expected to be the faster one, of what each takes in us: from Python 11 for one launch and 14.3 for two; the class rows' bytes; and
+// here the steps of a class row in one of 2,368 warps (16 bytes a lane are a load and four dot products a row, and every row's sum a reduction
+// and a store), there the tiles' own time.  Measured for 1, 2, 3, 4 rows against two kernels: 65,536 classes x 1,024 15.2, 18.6, 23.7, 24.8
+// against 18.3; 32,768 x 4,096 24, 28, 34, 35 against 28; 200,000 x 256 22, 29, 41, 45 against 20; 30,011 x 602 11.3, 11.3, 14.2, 14.7 against 14.3;
+// 4,096 x 256 11 against 14.6.
 bool few_rows_pays(int64_t n, int d, int m)
 {
     if (n > kGemvMax || n * round_up(d, 16) > kGemvBytes) return false;
-    const double bytes = (double)m * d, steps = (double)m * ((double)ceil_div(d, 512) * (4 * n + 4) + 12 * n);
-    return std::max(11.0, 7.0 + std::max(3.7e-6 * steps, bytes / 6e6)) <= std::max(14.5, 8.0 + bytes / 6.4e6);
+    const double bytes = (double)m * d, steps = (double)m * ((double)ceil_div(d, 512) * (4 * n + 6) + 12 * n);
+    return std::max(11.0, 4.5 + std::max(bytes / 6.3e6, 2.5 + 3.7e-6 * steps)) <= std::max(14.3, 7.0 + std::max(bytes / 6.5e6, 6.4e-5 * m));
 }
 cudaError_t launch_few_rows_product(cudaStream_t s, const void* x, int type, int64_t ldx, int64_t n, int d, const int8_t* q_w, int64_t ldqw, const float* s_w, int m,
                                     void* out, int out_type, int64_t ldo, int* launches)
@@ -430,6 +431,8 @@ cudaError_t launch_quantized_product(cudaStream_t s, const int8_t* q_x, int64_t 
     shape.m = (int)n;
     shape.n = m;
     shape.k = d;
+    shape.rotate = n <= gemm::kRows;          // class rows are read once
+    shape.tile_rows = gemm::rows_of_one_tile(n);
     ++*launches;
     if (quantized_across(n, m)) {
         shape.m = m;
@@ -441,6 +444,7 @@ cudaError_t launch_quantized_product(cudaStream_t s, const int8_t* q_x, int64_t 
             const int64_t cost = ceil_div(ceil_div(m, r), sm_count()) * (r + 16);
             if (cost < least) least = cost, shape.tile_rows = r;
         }
+        if (n <= 32) return launch_across<32>(s, q_x, ldqx, q_w, ldqw, shape, args);
         return launch_across<64>(s, q_x, ldqx, q_w, ldqw, shape, args);
     }
     if (m <= 64) return launch_product_as<64, 1>(s, q_x, ldqx, q_w, ldqw, shape, args);

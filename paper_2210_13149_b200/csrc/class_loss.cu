@@ -103,16 +103,18 @@ struct GatherArgs {
     uint16_t* g_x;           // nullable: rows without a label become zero
     int64_t ldgx;
     bool g_whole;
-    bool pairs;              // rows of x and of `to` can be moved in words of two elements
     int span;                // rows of a warp at a time, at most 32
     const float* g_loss;     // fp16's gradients: of every row,
     const float* top;        // and the largest magnitude among the labelled ones;
     uint16_t* scaled;        // rows times g / top, as `to` lies (nullable)
 };
-__device__ void gather_rows(const GatherArgs& a, int count, const int* places, int64_t first, int64_t warps, float top);
+// How rows of x lie: on 16-byte boundaries, up to 32 words of 16 bytes or more; on 4-byte boundaries; anywhere.
+enum Lie : int { kShort = 0, kLong = 1, kPairs = 2, kAnywhere = 3 };
+template <int LIE>
+__device__ __forceinline__ void gather_rows(const GatherArgs& a, int count, const int* places, int64_t first, int64_t warps, float top);
 
 // kGather: at most kScan rows, whose listing every block does for itself (the first one writes it) before it gathers its share: one launch less.
-template <bool kGather>
+template <bool kGather, int LIE>
 __global__ void __launch_bounds__(1024) list_labels_kernel(const ListArgs a, const GatherArgs gather)
 {
     pdl_enter();
@@ -192,13 +194,48 @@ __global__ void __launch_bounds__(1024) list_labels_kernel(const ListArgs a, con
     }
     if constexpr (kGather) {
         __syncthreads();
-        gather_rows(gather, total, here, (int64_t)blockIdx.x * 32 + warp, (int64_t)gridDim.x * 32, __uint_as_float(top));
+        gather_rows<LIE>(gather, total, here, (int64_t)blockIdx.x * 32 + warp, (int64_t)gridDim.x * 32, __uint_as_float(top));
     }
+}
+
+// The next ROWS of the labelled rows that `left` names, copied by words of T, WORDS of them a lane at a time, all on their way before the first
+// is stored; what is left of a row after `words` of them one by one.
+template <int ROWS, int WORDS, class T, class Load>
+__device__ __forceinline__ void copy_rows(const GatherArgs& a, int64_t row0, int place, uint32_t& left, int words, const Load& load)
+{
+    const int lane = threadIdx.x & 31;
+    constexpr int kElts = sizeof(T) / 2;
+    const uint16_t* from[ROWS];
+    uint16_t* to[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        const int at = __ffs(left) - 1;
+        from[r] = left != 0u ? a.x + (row0 + at) * a.ldx : nullptr;
+        to[r] = left != 0u ? a.to + (int64_t)__shfl_sync(0xffffffffu, place, at) * a.ldt : nullptr;
+        left &= left - 1;
+    }
+    for (int base = lane; base < words; base += 32 * WORDS) {
+        T v[ROWS][WORDS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+            for (int j = 0; j < WORDS; ++j)
+                if (from[r] && base + 32 * j < words) v[r][j] = load(from[r], base + 32 * j);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+            for (int j = 0; j < WORDS; ++j)
+                if (from[r] && base + 32 * j < words) reinterpret_cast<T*>(to[r])[base + 32 * j] = v[r][j];
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r)
+        if (from[r] && lane < a.d - words * kElts) to[r][words * kElts + lane] = __ldg(from[r] + words * kElts + lane);
 }
 
 // A warp to `span` rows at a time, whose places its lanes read together: labelled rows are copied together, the gradient of the others is
 // zero; rows up to the next multiple of 128 are zero.
-__device__ __forceinline__ void gather_rows(const GatherArgs& a, int count, const int* places, int64_t first, int64_t warps, float top)
+template <int LIE>
+__device__ void gather_rows(const GatherArgs& a, int count, const int* places, int64_t first, int64_t warps, float top)
 {
     const int lane = threadIdx.x & 31;
     const int64_t end = ((int64_t)count + 127) / 128 * 128;
@@ -214,48 +251,33 @@ __device__ __forceinline__ void gather_rows(const GatherArgs& a, int count, cons
             for (int i = lane; i < a.d; i += 32) a.scaled[row * a.ldt + i] = 0;
     }
     if (a.whole && count == a.n) return;
-    const int words = a.d / 8, rest = a.d - 8 * words;
+    const int words = a.d / 8;
     for (int64_t row0 = first * a.span; row0 < a.n; row0 += warps * a.span) {
         const int rows = (int)min((int64_t)a.span, a.n - row0);
         const int place = lane < rows ? places[row0 + lane] : -1;
         const uint32_t kept = __ballot_sync(0xffffffffu, place >= 0);
         uint32_t left = kept;
-        if (a.whole && rest == 0 && words <= 32) {            // rows of one word a lane: four of them on their way at a time
-            while (left != 0u) {
-                uint4 q[4];
-                int64_t to[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int r = __ffs(left) - 1;
-                    to[i] = left != 0u ? (int64_t)__shfl_sync(0xffffffffu, place, r) * a.ldt : -1;
-                    if (left != 0u && lane < words) q[i] = __ldg(reinterpret_cast<const uint4*>(a.x + (row0 + r) * a.ldx) + lane);
-                    left &= left - 1;
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (to[i] >= 0 && lane < words) reinterpret_cast<uint4*>(a.to + to[i])[lane] = q[i];
-            }
-        }
-        for (; left != 0u; left &= left - 1) {
-            const int r = __ffs(left) - 1;
-            const uint16_t* from = a.x + (row0 + r) * a.ldx;
-            uint16_t* to = a.to + (int64_t)__shfl_sync(0xffffffffu, place, r) * a.ldt;
-            if (a.whole) {
-                for (int w = lane; w < words; w += 32) reinterpret_cast<uint4*>(to)[w] = __ldg(reinterpret_cast<const uint4*>(from) + w);
-                if (lane < rest) to[8 * words + lane] = __ldg(from + 8 * words + lane);
-            } else if (a.pairs) {
-                for (int i = lane; i < a.d / 2; i += 32) reinterpret_cast<uint32_t*>(to)[i] = __ldg(reinterpret_cast<const uint32_t*>(from) + i);
-                if (a.d % 2 && lane == 0) to[a.d - 1] = __ldg(from + a.d - 1);
-            } else {
-                for (int i = lane; i < a.d; i += 32) to[i] = __ldg(from + i);
-            }
+        if constexpr (LIE == kShort) {                        // rows of one word a lane
+            while (left != 0u) copy_rows<2, 1, uint4>(a, row0, place, left, words, [&](const uint16_t* from, int i) { return __ldg(reinterpret_cast<const uint4*>(from) + i); });
+        } else if constexpr (LIE == kLong) {
+            while (left != 0u) copy_rows<1, 4, uint4>(a, row0, place, left, words, [&](const uint16_t* from, int i) { return __ldg(reinterpret_cast<const uint4*>(from) + i); });
+        } else if constexpr (LIE == kPairs) {
+            while (left != 0u) copy_rows<2, 4, uint32_t>(a, row0, place, left, a.d / 2, [&](const uint16_t* from, int i) { return __ldg(reinterpret_cast<const uint32_t*>(from) + i); });
+        } else {
+            // rows that begin anywhere, as words of the destination out of the two aligned ones that hold them; a row with others around it may be
+            // read two bytes past either end
+            while (left != 0u) copy_rows<2, 4, uint32_t>(a, row0, place, left, a.d / 2, [&](const uint16_t* from, int i) {
+                if (from == a.x || from == a.x + (a.n - 1) * a.ldx) return (uint32_t)__ldg(from + 2 * i) | (uint32_t)__ldg(from + 2 * i + 1) << 16;
+                const uint32_t* word = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(from) & ~uintptr_t(3)) + i;
+                return reinterpret_cast<uintptr_t>(from) & 2 ? __funnelshift_r(__ldg(word), __ldg(word + 1), 16) : __ldg(word);
+            });
         }
         if (!a.g_x) continue;
         for (left = ~kept & (rows < 32 ? (1u << rows) - 1u : 0xffffffffu); left != 0u; left &= left - 1) {
             uint16_t* to = a.g_x + (row0 + __ffs(left) - 1) * a.ldgx;
             if (a.g_whole) {
                 for (int w = lane; w < words; w += 32) reinterpret_cast<uint4*>(to)[w] = make_uint4(0u, 0u, 0u, 0u);
-                if (lane < rest) to[8 * words + lane] = 0;
+                if (lane < a.d - 8 * words) to[8 * words + lane] = 0;
             } else {
                 for (int i = lane; i < a.d; i += 32) to[i] = 0;
             }
@@ -264,10 +286,11 @@ __device__ __forceinline__ void gather_rows(const GatherArgs& a, int count, cons
     for (int64_t row = count + first; row < end; row += warps)
         for (int i = lane; i < a.d; i += 32) a.to[row * a.ldt + i] = 0;
 }
-__global__ void __launch_bounds__(256) gather_rows_kernel(const GatherArgs a)
+template <int LIE>
+__global__ void __launch_bounds__(256, LIE == kShort ? 8 : 6) gather_rows_kernel(const GatherArgs a)
 {
     pdl_enter();
-    gather_rows(a, __ldg(a.count), a.place, (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), (int64_t)gridDim.x * 8, a.scaled ? __ldg(a.top) : 0.f);
+    gather_rows<LIE>(a, __ldg(a.count), a.place, (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), (int64_t)gridDim.x * 8, a.scaled ? __ldg(a.top) : 0.f);
 }
 
 // Rows copied to 16-byte boundaries (a class matrix that does not start its rows there), in words of T where the rows allow it.
@@ -289,8 +312,8 @@ __global__ void __launch_bounds__(256) align_rows_kernel(const uint16_t* __restr
 // ---- epilogues -----------------------------------------------------------------------------------------------------------
 
 // Maximum and sum of exp(z - maximum) of a tile's columns, and the label's z.  An argument of exp2 is the difference times
-// log2 e: the difference first, so that the largest term is exactly 1 and a loss near 0 keeps its digits.  The four warps of the same rows
-// join theirs in shared memory (128 threads meet twice a tile), which leaves a quarter of the parts to write and to join.
+// log2 e: the difference first, so that the largest term is exactly 1 and a loss near 0 keeps its digits.  The warps that share the rows
+// join theirs in shared memory (they meet twice a tile), which leaves a quarter of the parts to write and to join.
 struct SumExp {
     struct Args {
         const int* label;    // of the rows
@@ -301,14 +324,20 @@ struct SumExp {
         float* loss;
         float* lse;
     };
+    static constexpr bool kMeets = true;
     static __device__ int* flag() { return &g_loss_timeout; }
-    using Row = int;
-    static __device__ __forceinline__ Row row(const Args& a, int row, int rows) { return row < rows ? __ldg(a.label + row) : INT_MIN; }
+    struct Row {
+        int label, to;
+    };
+    static __device__ __forceinline__ Row row(const Args& a, int row, int rows)
+    {
+        return {row < rows ? __ldg(a.label + row) : INT_MIN, row < rows && a.kept ? __ldg(a.kept + row) : 0};
+    }
     template <int BN, class Done>
     static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit& u, const gemm::Part& p, const Row& of_row, const Done& done)
     {
         const int row = p.row + (threadIdx.x & 31);
-        const int label = of_row >= p.col ? of_row - p.col : INT_MIN;          // far from any column, as the rows that are not there have it
+        const int label = of_row.label >= p.col ? of_row.label - p.col : INT_MIN;          // far from any column, as the rows that are not there have it
         float m = -INFINITY, s = 0.f, at = 0.f;
         bool mine = false;
         gemm::each_chunk<BN>(p, sh.n, done, [&](int c, uint32_t (&v)[32]) {
@@ -335,29 +364,29 @@ struct SumExp {
                 mine |= in < 32u;
             }
         });
-        // each warp's strip holds its own 32 pairs; those of the other three lie kStripBytes * 4 apart
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-        unsigned char* const first = p.strip - (warp >> 2) * (4 * gemm::kStripBytes);
-        gemm::meet(1 + (warp & 3), 32 * gemm::kColumnParts, true);
-        if (warp >= 4) *reinterpret_cast<float2*>(p.strip + 8 * lane) = make_float2(m, s);
+        // each warp's strip holds its own 32 pairs; those of the others that share the rows lie kStripBytes * 4 apart
+        constexpr int kParts = gemm::column_parts(BN);
+        const int lane = threadIdx.x & 31;
+        unsigned char* const first = p.strip - p.part * (4 * gemm::kStripBytes);
+        gemm::meet(p.meeting, 32 * kParts, true);
+        if (p.part > 0) *reinterpret_cast<float2*>(p.strip + 8 * lane) = make_float2(m, s);
         if (mine) {
             if (a.kept) *reinterpret_cast<float*>(first + 256 + 4 * lane) = at;      // in the first warp's
             else a.at[row] = at;
         }
-        gemm::meet(1 + (warp & 3), 32 * gemm::kColumnParts, true);
-        if (warp < 4) {
+        gemm::meet(p.meeting, 32 * kParts, true);
+        if (p.part == 0) {
 #pragma unroll
-            for (int w = 1; w < gemm::kColumnParts; ++w) {
+            for (int w = 1; w < kParts; ++w) {
                 const float2 q = *reinterpret_cast<const float2*>(first + w * (4 * gemm::kStripBytes) + 8 * lane);
                 const float top = fmaxf(m, q.x), t = top == -INFINITY ? 0.f : top;
                 s = s * exp2_fast((m - t) * kLog2e) + q.y * exp2_fast((q.x - t) * kLog2e);
                 m = top;
             }
             if (row < p.rows && a.kept) {
-                const int to = __ldg(a.kept + row);
                 const float l = logf(s);
-                a.loss[to] = (m - *reinterpret_cast<const float*>(first + 256 + 4 * lane)) + l;
-                a.lse[to] = m + l;
+                a.loss[of_row.to] = (m - *reinterpret_cast<const float*>(first + 256 + 4 * lane)) + l;
+                a.lse[of_row.to] = m + l;
             } else if (row < p.rows) {
                 a.part[(int64_t)(u.col / BN) * a.rows + row] = make_float2(m, s);
             }
@@ -378,6 +407,7 @@ struct Gradient {
         uint16_t* g;
         int64_t ldg;         // a multiple of 64
     };
+    static constexpr bool kMeets = false;
     static __device__ int* flag() { return &g_loss_timeout; }
     struct Row {
         int label;
@@ -415,8 +445,8 @@ struct Gradient {
                     else if (2 * i + 1 >= left) w[i] &= 0xffffu;
                 }
             }
-            uint16_t* to = a.g + (int64_t)p.row * a.ldg + p.col + c;
-            gemm::write_strip(p.strip, w, [&](int r, int piece, const uint4& q) { *reinterpret_cast<uint4*>(to + r * a.ldg + 8 * piece) = q; });
+            const int lane = threadIdx.x & 31;
+            gemm::write_strip_whole(p.strip, w, reinterpret_cast<char*>(a.g + (int64_t)(p.row + (lane >> 2)) * a.ldg + p.col + c + 8 * (lane & 3)), 16 * a.ldg);
         });
     }
 };
@@ -436,6 +466,7 @@ struct Store {
         const float* factor;         // nullable
         float constant;
     };
+    static constexpr bool kMeets = false;
     static __device__ int* flag() { return &g_loss_timeout; }
     struct Row {
         int to;
@@ -448,7 +479,7 @@ struct Store {
     template <int BN, class Done>
     static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit& u, const gemm::Part& p, const Row& of_row, const Done& done)
     {
-        if (p.empty && a.part && a.add) return;
+        if (p.empty && a.part && a.add) return done();
         const int mapped = of_row.to;
         const float factor = TYPE == BIGCN_F16 ? of_row.factor * (a.factor ? __ldg(a.factor) : 1.f) : 1.f;
         gemm::each_chunk<BN>(p, sh.n, done, [&](int c, uint32_t (&v)[32]) {
@@ -474,7 +505,10 @@ struct Store {
             } else {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) w[i] = pack2<TYPE>(__uint_as_float(v[2 * i]) * factor, __uint_as_float(v[2 * i + 1]) * factor);
-                if (a.whole) {
+                const int lane = threadIdx.x & 31;
+                if (a.whole && !a.map && p.row + 32 <= p.rows && col + 32 <= sh.n) {
+                    gemm::write_strip_whole(p.strip, w, reinterpret_cast<char*>(a.out + (int64_t)(p.row + (lane >> 2)) * a.ldo + col + 8 * (lane & 3)), 16 * a.ldo);
+                } else if (a.whole) {
                     gemm::write_strip(p.strip, w, [&](int r, int piece, const uint4& q) {
                         const int64_t to_row = __shfl_sync(0xffffffffu, mapped, r);
                         const int at = col + 8 * piece;
@@ -734,18 +768,26 @@ cudaError_t prepare(cudaStream_t s, const Plan& p, char* ws, int type, const voi
                            (reinterpret_cast<uintptr_t>(loss) | reinterpret_cast<uintptr_t>(lse)) % 16 == 0, of_lse, of_g_loss,
                            reinterpret_cast<float*>(ws + p.lse), reinterpret_cast<float*>(ws + p.g_loss), top};
     *o = {x, ldx, rows_whole(x, ldx, BIGCN_BF16, 8), reinterpret_cast<const uint16_t*>(ws + p.x), w, ldw};
-    const int span = (int)std::max<int64_t>(1, std::min<int64_t>(32, n / (64 * sm_count())));     // as many warps as the machine holds, first
+    // rows of a warp at a time: as many times as it takes with 32, and the same each time
+    const int resident = o->x_whole && d <= 256 ? 8 : 6;     // blocks of the kernel on a multiprocessor
+    const int64_t warps = 8 * resident * sm_count();
+    const int span = (int)ceil_div(n, warps * ceil_div(n, warps * 32));
     const GatherArgs gather = {static_cast<const uint16_t*>(x), ldx, n, d, o->x_whole, list.place, list.count, reinterpret_cast<uint16_t*>(ws + p.x), p.ldt,
-                               static_cast<uint16_t*>(g_x), ldgx, rows_whole(g_x, ldgx, BIGCN_BF16, 8), rows_whole(x, ldx, BIGCN_BF16, 2), span, of_g_loss,
+                               static_cast<uint16_t*>(g_x), ldgx, rows_whole(g_x, ldgx, BIGCN_BF16, 8), span, of_g_loss,
                                reinterpret_cast<const float*>(top), top ? reinterpret_cast<uint16_t*>(ws + p.scaled) : nullptr};
     ++*launches;
+    const int lie = o->x_whole ? (d <= 256 ? kShort : kLong) : rows_whole(x, ldx, BIGCN_BF16, 2) ? kPairs : kAnywhere;
     if (n <= kScan) {
-        e = launch_kernel(list_labels_kernel<true>, dim3((unsigned)std::min<int64_t>(ceil_div(n, 32), sm_count())), dim3(1024), 0, s, list, gather);
+        const dim3 grid((unsigned)std::min<int64_t>(ceil_div(n, 32), sm_count()));
+        e = launch_kernel(lie == kShort ? list_labels_kernel<true, kShort> : lie == kLong ? list_labels_kernel<true, kLong> : lie == kPairs ? list_labels_kernel<true, kPairs>
+                          : list_labels_kernel<true, kAnywhere>, grid, dim3(1024), 0, s, list, gather);
     } else {
-        e = launch_kernel(list_labels_kernel<false>, dim3(blocks), dim3(1024), 0, s, list, gather);
+        e = launch_kernel(list_labels_kernel<false, kShort>, dim3(blocks), dim3(1024), 0, s, list, gather);
         if (e != cudaSuccess) return e;
         ++*launches;
-        e = launch_kernel(gather_rows_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(n, 8 * span), 8 * sm_count())), dim3(256), 0, s, gather);
+        const dim3 grid((unsigned)std::min<int64_t>(ceil_div(n, 8 * span), resident * sm_count()));
+        e = launch_kernel(lie == kShort ? gather_rows_kernel<kShort> : lie == kLong ? gather_rows_kernel<kLong> : lie == kPairs ? gather_rows_kernel<kPairs>
+                          : gather_rows_kernel<kAnywhere>, grid, dim3(256), 0, s, gather);
     }
     if (e != cudaSuccess) return e;
     if (!rows_whole(w, ldw, BIGCN_BF16, 8)) {
@@ -851,6 +893,7 @@ cudaError_t backward_as(cudaStream_t s, const void* x, int64_t ldx, const void* 
             if (g_x) {
                 CUtensorMap mg, mw;
                 sh.tile_rows = gemm::rows_of_one_tile(rows);
+                sh.rotate = rows <= gemm::kRows;
                 e = gemm::encode_map(&mg, g, 2, false, round_up(rows, 128), ldg, ldg * 2, 64, sh.tile_rows);
                 if (e == cudaSuccess) e = gemm::encode_map(&mw, static_cast<const uint16_t*>(o.w) + first_class * o.ldw, 2, false, here, d, o.ldw * 2, 64, 64);
                 if (e != cudaSuccess) break;
@@ -882,6 +925,7 @@ cudaError_t backward_as(cudaStream_t s, const void* x, int64_t ldx, const void* 
                 sh.k = (int)rows;
                 sh.splits = p.splits_w;
                 sh.over_depth = true;
+                sh.rotate = false;
                 sh.alt_b = o.x_whole && !half;
                 uint16_t* out = static_cast<uint16_t*>(g_w) + first_class * ldgw;
                 const typename Store<TYPE>::Args args = {nullptr, out, ldgw, rows_whole(out, ldgw, BIGCN_BF16, 8), parts_w ? reinterpret_cast<float*>(ws + p.pw) : nullptr, p.pitch,

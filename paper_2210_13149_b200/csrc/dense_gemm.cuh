@@ -24,7 +24,11 @@ namespace bigcn {
 namespace gemm {
 
 constexpr int kEpiWarps = 16, kProducer = 16, kIssuer = 17, kThreads = 576;
-constexpr int kColumnParts = kEpiWarps / 4;   // a tile's columns are shared among four warps for each 32 rows
+// A tile's columns are shared among four warps for each 32 rows, or among two or one where it is so narrow that four would not have 32 each; then two
+// or four groups of warps take tiles in turn (169,343 rows of 256 against 40 8-bit classes in us: 26, 19 so).
+__host__ __device__ constexpr int column_parts(int bn) { return bn >= 128 ? 4 : bn / 32; }
+__host__ __device__ constexpr int epi_groups(int bn) { return kEpiWarps / 4 / column_parts(bn); }
+__host__ __device__ constexpr int acc_buffers(int bn) { return 2 * epi_groups(bn); }
 constexpr int kRows = 128;                    // rows of a block's tile: the lanes of tensor memory
 constexpr int kDepthBytes = 128;              // depth of a stage
 constexpr int kTries = 1 << 22;               // bound of every wait, in tries of up to about a microsecond
@@ -42,7 +46,7 @@ struct Shape {
     int of = 0, base = 0;
     bool over_depth = false, alt_a = false, alt_b = false;
     int tile_rows = kRows;   // rows of a tile that count (a multiple of 8; the accumulators have 128), one block to a tile, K-major A
-    bool rotate = false;     // each block begins with another step of the depth.  For operands that are read once: blocks that all begin at the first
+    bool rotate = false;     // each block (or pair) begins with another step of the depth.  For operands that are read once: blocks that all begin at the first
                              // 128 bytes of rows a power of two apart keep to a part of the memory channels (131,072 8-bit classes x 2,048 for
                              // eight rows in us: 73, 47 so).  Sums of floats are then taken in an order that depends on the tile.
     bool a_ahead = false;    // A does not come from the kernel before this one (which let this one start early): its first stages are
@@ -80,6 +84,14 @@ struct Walk {
     __device__ Unit at(int u) const
     {
         Unit r;
+        if (tiles_n == 1 && splits == 1) {       // no divisions
+            r.split = 0;
+            r.col = 0;
+            r.row = u * tile_rows;
+            r.k0 = 0;
+            r.k1 = stages;
+            return r;
+        }
         const int tiles = max(1, tiles_m * tiles_n);
         r.split = u / tiles;
         const int t = u - r.split * tiles, band = t / (kBand * tiles_n), in = t - band * kBand * tiles_n;
@@ -113,7 +125,7 @@ __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile in
 {
     for (int it = 0; it < kTries; ++it) {
         uint32_t done;
-        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2, 1000;\nselp.u32 %0, 1, 0, p;\n}\n"
+        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
                      : "=r"(done) : "r"(tc::smem_u32(bar)), "r"(parity) : "memory");
         if (done) return true;
         if ((it & 15) == 15 && *abort) return false;
@@ -201,7 +213,7 @@ struct Config {
 };
 
 struct Control {
-    uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drained;
+    uint64_t full[kMaxStages], empty[kMaxStages], acc_full[8], acc_empty[8], drained;
     uint32_t tmem;
     int abort;
 };
@@ -227,29 +239,30 @@ __device__ __forceinline__ void tmem_wait32(uint32_t (&v)[32])
                  :: "memory");
 }
 
-// What an epilogue warp works with: warp w has lanes 32 (w & 3) .. + 31 of tensor memory (rows of the tile) and columns
-// (w >> 2) BN / 4 .. + BN / 4 - 1 of it (32 at least: in the narrowest tile the upper warps have none).
+// What an epilogue warp works with: warp w has lanes 32 (w & 3) .. + 31 of tensor memory (rows of the tile) and part_cols(BN) columns of it, its
+// `part` of the tile's; the four warps (or fewer) that share the rows are 4 apart, the first of them at `part` 0.
 struct Part {
     int row;                 // first of the warp's 32 rows
     int rows;                // rows of the whole product
     int col;                 // first column
     uint32_t acc;            // its lanes and first column
     bool empty;              // no depth: the accumulators hold nothing, the sums are 0
-    bool there;              // the warp has columns of the tile
+    int part;
+    int meeting;             // barrier of the warps that share the rows
     unsigned char* strip;    // kStripBytes of shared memory
 };
 
 // Columns of a warp's part.
-__host__ __device__ constexpr int part_cols(int bn) { return bn / kColumnParts < 32 ? 32 : bn / kColumnParts; }
+__host__ __device__ constexpr int part_cols(int bn) { return bn / column_parts(bn); }
 
 // body(c, v) for every 32 columns c, c + 1, .. of the warp's, as far as there are `columns`: v is the row of this lane.  done() once all
 // are read from tensor memory.
 template <int BN, class Done, class Body>
 __device__ __forceinline__ void each_chunk(const Part& p, int columns, const Done& done, const Body& body)
 {
-    const int chunks = p.there ? max(0, min(part_cols(BN) / 32, (columns - p.col + 31) >> 5)) : 0;
+    const int chunks = max(0, min(part_cols(BN) / 32, (columns - p.col + 31) >> 5));
     uint32_t v[32];
-    if (!p.empty && chunks == 0) done();
+    if (p.empty || chunks == 0) done();
     for (int c = 0; c < chunks; ++c) {
         __syncwarp();
         if (p.empty) {
@@ -282,6 +295,16 @@ __device__ __forceinline__ void write_strip(unsigned char* strip, const uint32_t
     }
 }
 
+// The same straight to memory, all 32 rows and 64 bytes of them there: `at` is where this lane's first piece goes (row lane >> 2, piece
+// lane & 3), `step` eight rows in bytes.
+__device__ __forceinline__ void write_strip_whole(unsigned char* strip, const uint32_t (&w)[16], char* at, int64_t step)
+{
+    write_strip(strip, w, [&](int, int, const uint4& q) {
+        *reinterpret_cast<uint4*>(at) = q;
+        at += step;
+    });
+}
+
 // The same for rows that start anywhere: put(r, e, bits) for the element e = 0 .. 64 / sizeof(T) - 1 of row r, neighbours to neighbouring lanes.
 template <class T, class Put>
 __device__ __forceinline__ void write_strip_elements(unsigned char* strip, const uint32_t (&w)[16], const Put& put)
@@ -304,8 +327,9 @@ __device__ __forceinline__ void write_strip_elements(unsigned char* strip, const
 //   Row                            what it reads of a row (of the tile, a lane's)
 //   static __device__ Row row(const Args&, int row, int rows)                    fetched while the tile before is worked on
 //   template <int BN, class Done> static __device__ void tile(const Args&, const Shape&, const Unit&, const Part&, const Row&, const Done& done)
-//                                  run by the epilogue warps; done() once the accumulators are read, unless they are empty
+//                                  run by the epilogue warps; done() once, when the accumulators are read
 //   static __device__ int* flag()  raised when a wait ran out
+//   static constexpr bool kMeets   whether the warps of the same rows meet in tile()
 template <bool I8, int BN, int CTAS, bool A_MN, bool B_MN, class Epi>
 __global__ void __launch_bounds__(kThreads, 1)
 product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_alt,
@@ -318,16 +342,16 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     unsigned char* stages = raw + ((1024u - (tc::smem_u32(raw) & 1023u)) & 1023u);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CTAS == 2 ? cluster_rank() : 0u;
-    constexpr int kCols = 2 * BN < 32 ? 32 : 2 * BN;
+    constexpr int kGroups = epi_groups(BN), kBuffers = acc_buffers(BN), kCols = kBuffers * BN;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::kStages; ++i) {
             init_barrier(&ctl.full[i], 1);
             init_barrier(&ctl.empty[i], 1);
         }
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kBuffers; ++i) {
             init_barrier(&ctl.acc_full[i], 1);
-            init_barrier(&ctl.acc_empty[i], kEpiWarps * CTAS);
+            init_barrier(&ctl.acc_empty[i], kEpiWarps / kGroups * CTAS);
         }
         init_barrier(&ctl.drained, 1);
         ctl.abort = 0;
@@ -352,7 +376,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     int early = 0;           // stages whose A is on its way
     const auto depth_at = [&](const Unit& t, int k) {        // of the stage k in [k0, k1)
         if (!shape.rotate) return k;
-        const int steps = t.k1 - t.k0, at = k - t.k0 + (int)(blockIdx.x % (unsigned)steps);
+        const int steps = t.k1 - t.k0, at = k - t.k0 + (int)(blockIdx.x / CTAS % (unsigned)steps);
         return t.k0 + (at < steps ? at : at - steps);
     };
     if (CTAS == 1 && !A_MN && shape.a_ahead && threadIdx.x == kProducer * 32) {
@@ -434,7 +458,6 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             bool ok = true, any = false;
             for (int u = first; u < units && ok; u += step) {
                 const Unit t = walk.at(u);
-                if (t.k0 >= t.k1) continue;
                 ok = wait(&ctl.acc_empty[buf], acc_phase ^ 1u, abort, flag);
                 if (!ok) break;
                 tc::fence_after_sync();
@@ -453,8 +476,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     if (++slot == C::kStages) slot = 0, phase ^= 1u;
                 }
                 if (!ok) break;
-                commit<CTAS>(&ctl.acc_full[buf]);
-                if ((buf ^= 1) == 0) acc_phase ^= 1u;
+                commit<CTAS>(&ctl.acc_full[buf]);        // (at once where there is no depth)
+                if (++buf == kBuffers) buf = 0, acc_phase ^= 1u;
             }
             if (!ok && any) {
                 volatile int none = 0;
@@ -467,38 +490,44 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         }
         __syncwarp();
     } else {
-        int buf = 0;
-        uint32_t acc_phase = 0;
+        constexpr int kParts = column_parts(BN);
+        const int group = (warp >> 2) / kParts, begin = first + group * step, stride = kGroups * step;
         const int own = (int)rank * kRows + (warp & 3) * 32;
-        Unit coming = walk.at(first < units ? first : 0);
-        typename Epi::Row ahead = Epi::row(args, first < units ? coming.row + own + lane : walk.m, walk.m);
-        for (int u = first; u < units; u += step) {
+        Part part;
+        part.rows = walk.m;
+        part.part = (warp >> 2) % kParts;
+        part.meeting = 1 + group * 4 + (warp & 3);
+        part.strip = stages + C::kStages * C::kStage + warp * kStripBytes;
+        int buf = group;
+        uint32_t acc_phase = 0;
+        Unit coming = walk.at(begin < units ? begin : 0);
+        typename Epi::Row ahead = Epi::row(args, begin < units ? coming.row + own + lane : walk.m, walk.m);
+        for (int u = begin; u < units; u += stride) {
             const Unit t = coming;
             const typename Epi::Row now = ahead;
-            if (u + step < units) {
-                coming = walk.at(u + step);
+            if (u + stride < units) {
+                coming = walk.at(u + stride);
                 ahead = Epi::row(args, coming.row + own + lane, walk.m);
             }
-            const bool empty = t.k0 >= t.k1;
-            if (!empty) {
-                // the four warps of the same rows go on or give up together: an epilogue may let them meet
-                if (!meet(1 + (warp & 3), 32 * kColumnParts, wait(&ctl.acc_full[buf], acc_phase, abort, flag))) break;
-                tc::fence_after_sync();
+            // where an epilogue lets the warps of the same rows meet, they go on or give up together
+            const bool there = __all_sync(0xffffffffu, wait(&ctl.acc_full[buf], acc_phase, abort, flag));
+            if constexpr (Epi::kMeets && kParts > 1) {
+                if (!meet(part.meeting, 32 * kParts, there)) break;
+            } else {
+                if (!there) break;
             }
-            Part part;
+            tc::fence_after_sync();
             part.row = t.row + own;
-            part.rows = CTAS == 1 ? min(walk.m, t.row + walk.tile_rows) : walk.m;
-            part.col = t.col + (warp >> 2) * part_cols(BN);
-            part.acc = tmem + (uint32_t)(buf * BN + (warp >> 2) * part_cols(BN)) + ((uint32_t)((warp & 3) * 32) << 16);
-            part.empty = empty;
-            part.there = (warp >> 2) * part_cols(BN) < BN;
-            part.strip = stages + C::kStages * C::kStage + warp * kStripBytes;
+            if (CTAS == 1) part.rows = min(walk.m, t.row + walk.tile_rows);
+            part.col = t.col + part.part * part_cols(BN);
+            part.acc = tmem + (uint32_t)(buf * BN + part.part * part_cols(BN)) + ((uint32_t)((warp & 3) * 32) << 16);
+            part.empty = t.k0 >= t.k1;
             Epi::template tile<BN>(args, shape, t, part, now, [&] {
                 tc::fence_before_sync();
                 __syncwarp();
                 if (lane == 0) arrive_first<CTAS>(&ctl.acc_empty[buf]);
             });
-            if (!empty && (buf ^= 1) == 0) acc_phase ^= 1u;
+            if ((buf += kGroups) >= kBuffers) buf -= kBuffers, acc_phase ^= 1u;
         }
     }
     tc::fence_before_sync();

@@ -97,14 +97,19 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : 256, LANES > 32 ? 1 : NV 
             for (int i = 0; i < V; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
         }
         fetch(row + step);
-        top = __reduce_max_sync(0xffffffffu, top);
+        if constexpr (LANES < 32) {
+#pragma unroll
+            for (int m = LANES / 2; m >= 1; m >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, m));
+        } else {
+            top = __reduce_max_sync(0xffffffffu, top);
+        }
         if constexpr (LANES > 32) {
             uint32_t* slot = slots[trip];
             if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = top;
             __syncthreads();
             top = __reduce_max_sync(0xffffffffu, (threadIdx.x & 31) < LANES / 32 ? slot[threadIdx.x & 31] : 0u);
         }
-        if (row >= a.n) continue;
+        if (row >= a.n) continue;             // (the warp's other rows go on: nothing below is done together)
         const bool finite = top < 0x7f800000u;
         const float t = __uint_as_float(top), factor = 127.f / t;
         const bool tiny = t < 1e-30f;         // 127 / t would overflow
@@ -147,6 +152,8 @@ cudaError_t pick_quantize(cudaStream_t s, const QuantArgs& a, int* launches)
     constexpr int Q = 16 / V;
     const int64_t words = ceil_div(a.d, V);
     const bool many = a.n >= 4096;
+    if (words <= 8) return launch_quantize_as<TYPE, V, 8, 1>(s, a, launches);
+    if (words <= 16) return launch_quantize_as<TYPE, V, 16, 1>(s, a, launches);
     if (words <= 32) return launch_quantize_as<TYPE, V, 32, 1>(s, a, launches);
     if (words <= 64) return launch_quantize_as<TYPE, V, 32, 2>(s, a, launches);
     if (words <= 32 * Q || (many && words <= 128)) return launch_quantize_as<TYPE, V, 32, 4>(s, a, launches);
@@ -157,53 +164,19 @@ cudaError_t pick_quantize(cudaStream_t s, const QuantArgs& a, int* launches)
 }
 
 // Epilogue: the sums times both scales, in the output's type.
+struct ScaledArgs {
+    const float* s_x;
+    const float* s_w;
+    bool s_w_whole;
+    void* out;
+    int type;
+    int64_t ldo;
+    bool whole;              // rows of out on 16-byte boundaries
+};
+template <int TYPE>
 struct ScaledOut {
-    struct Args {
-        const float* s_x;
-        const float* s_w;
-        bool s_w_whole;
-        void* out;
-        int type;
-        int64_t ldo;
-        bool whole;          // rows of out on 16-byte boundaries
-    };
-    // 16 or 32 columns of a strip: 64 bytes of a row
-    template <int TYPE>
-    static __device__ __forceinline__ void write(const Args& a, const gemm::Part& p, int columns, int col, const float (&f)[32])
-    {
-        constexpr int kElts = 16 / type_bytes(TYPE), kStrips = type_bytes(TYPE) / 2;
-        using T = typename Elt<TYPE>::T;
-#pragma unroll
-        for (int h = 0; h < kStrips; ++h) {
-            uint32_t w[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                if constexpr (TYPE == BIGCN_F32) w[i] = __float_as_uint(f[16 * h + i]);
-                else w[i] = pack2<TYPE>(f[2 * i], f[2 * i + 1]);
-            }
-            T* const out = static_cast<T*>(a.out) + col + 16 * h;
-            if (a.whole) {
-                gemm::write_strip(p.strip, w, [&](int r, int piece, const uint4& v) {
-                    const int row = p.row + r, c = piece * kElts, left = columns - (col + 16 * h + c);
-                    if (row >= p.rows || left <= 0) return;
-                    T* to = out + (int64_t)row * a.ldo + c;
-                    if (left >= kElts) {
-                        *reinterpret_cast<uint4*>(to) = v;
-                    } else {
-                        const T* e = reinterpret_cast<const T*>(&v);
-#pragma unroll
-                        for (int i = 0; i < kElts; ++i)
-                            if (i < left) to[i] = e[i];
-                    }
-                });
-            } else {
-                using Bits = typename std::conditional<sizeof(T) == 4, uint32_t, uint16_t>::type;
-                gemm::write_strip_elements<Bits>(p.strip, w, [&](int r, int e, Bits v) {
-                    if (p.row + r < p.rows && col + 16 * h + e < columns) reinterpret_cast<Bits*>(out)[(int64_t)(p.row + r) * a.ldo + e] = v;
-                });
-            }
-        }
-    }
+    using Args = ScaledArgs;
+    static constexpr bool kMeets = false;
     static __device__ int* flag() { return &g_quant_timeout; }
     using Row = float;
     static __device__ __forceinline__ Row row(const Args& a, int row, int rows) { return row < rows ? __ldg(a.s_x + row) : 0.f; }
@@ -213,24 +186,61 @@ struct ScaledOut {
         const int lane = threadIdx.x & 31;
         // the warp's class scales are read by all lanes at once below: from L1 by then
         if (lane < gemm::part_cols(BN) / 32 && p.col + 32 * lane < sh.n) asm volatile("prefetch.global.L1 [%0];\n" ::"l"(a.s_w + p.col + 32 * lane));
+        constexpr int kElts = 16 / type_bytes(TYPE), kStrips = type_bytes(TYPE) / 2;      // of a piece; 32 columns are one strip or two
+        using T = typename Elt<TYPE>::T;
+        using Bits = typename std::conditional<sizeof(T) == 4, uint32_t, uint16_t>::type;
+        T* const at = static_cast<T*>(a.out) + (int64_t)p.row * a.ldo + p.col;
+        const bool rows_there = p.row + 32 <= p.rows;
         gemm::each_chunk<BN>(p, sh.n, done, [&](int c, uint32_t (&v)[32]) {
-            const int col = p.col + c;
-            float f[32];
-            if (a.s_w_whole && col + 32 <= sh.n) {
+            const int left = sh.n - (p.col + c);
+            if (a.s_w_whole && left >= 32) {
 #pragma unroll
                 for (int i = 0; i < 32; i += 4) {
-                    const float4 w = __ldg(reinterpret_cast<const float4*>(a.s_w + col + i));
-                    f[i] = w.x; f[i + 1] = w.y; f[i + 2] = w.z; f[i + 3] = w.w;
+                    const float4 w = __ldg(reinterpret_cast<const float4*>(a.s_w + p.col + c + i));
+                    v[i] = __float_as_uint((float)(int)v[i] * (sx * w.x));
+                    v[i + 1] = __float_as_uint((float)(int)v[i + 1] * (sx * w.y));
+                    v[i + 2] = __float_as_uint((float)(int)v[i + 2] * (sx * w.z));
+                    v[i + 3] = __float_as_uint((float)(int)v[i + 3] * (sx * w.w));
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) f[i] = col + i < sh.n ? __ldg(a.s_w + col + i) : 0.f;
+                for (int i = 0; i < 32; ++i) v[i] = __float_as_uint((float)(int)v[i] * (sx * (i < left ? __ldg(a.s_w + p.col + c + i) : 0.f)));
             }
 #pragma unroll
-            for (int i = 0; i < 32; ++i) f[i] = (float)(int)v[i] * (sx * f[i]);
-            if (a.type == BIGCN_F32) write<BIGCN_F32>(a, p, sh.n, col, f);
-            else if (a.type == BIGCN_BF16) write<BIGCN_BF16>(a, p, sh.n, col, f);
-            else write<BIGCN_F16>(a, p, sh.n, col, f);
+            for (int h = 0; h < kStrips; ++h) {
+                uint32_t w[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    if constexpr (TYPE == BIGCN_F32) w[i] = v[16 * h + i];
+                    else w[i] = pack2<TYPE>(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+                }
+                T* const to = at + c + 16 * h;
+                if (a.whole && rows_there && left >= 32) {
+                    gemm::write_strip_whole(p.strip, w, reinterpret_cast<char*>(to + (int64_t)(lane >> 2) * a.ldo + (lane & 3) * kElts), 8 * a.ldo * (int64_t)sizeof(T));
+                } else if (a.whole) {
+                    gemm::write_strip(p.strip, w, [&](int r, int piece, const uint4& q) {
+                        const int there = left - 16 * h - piece * kElts;
+                        if (p.row + r >= p.rows || there <= 0) return;
+                        T* e = to + r * a.ldo + piece * kElts;
+                        if (there >= kElts) {
+                            *reinterpret_cast<uint4*>(e) = q;
+                        } else {
+                            const T* from = reinterpret_cast<const T*>(&q);
+#pragma unroll
+                            for (int i = 0; i < kElts; ++i)
+                                if (i < there) e[i] = from[i];
+                        }
+                    });
+                } else {
+                    constexpr int kPerRow = 64 / sizeof(T);
+                    Bits* e = reinterpret_cast<Bits*>(to) + (int64_t)(lane / kPerRow) * a.ldo + lane % kPerRow;
+                    const bool mine = lane % kPerRow < left - 16 * h;
+                    gemm::write_strip_elements<Bits>(p.strip, w, [&](int r, int, Bits q) {
+                        if (mine && p.row + r < p.rows) *e = q;
+                        e += (32 / kPerRow) * a.ldo;
+                    });
+                }
+            }
         });
     }
 };
@@ -238,7 +248,8 @@ struct ScaledOut {
 // The same with classes as rows of the tiles and the few rows of x as columns: a lane has a class, so that 32 neighbours of an output row
 // are stored together, and 128 class rows to a tile leave more tiles than 256 columns would.
 struct ScaledAcross {
-    using Args = ScaledOut::Args;
+    using Args = ScaledArgs;
+    static constexpr bool kMeets = false;
     static __device__ int* flag() { return &g_quant_timeout; }
     using Row = float;
     static __device__ __forceinline__ Row row(const Args& a, int row, int rows) { return row < rows ? __ldg(a.s_w + row) : 0.f; }
@@ -365,17 +376,19 @@ cudaError_t launch_few_rows(cudaStream_t s, const GemvArgs& a)
 }
 
 template <int BN, int CTAS>
-cudaError_t launch_product_as(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const int8_t* q_w, int64_t ldqw, const gemm::Shape& shape, const ScaledOut::Args& args)
+cudaError_t launch_product_as(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const int8_t* q_w, int64_t ldqw, const gemm::Shape& shape, const ScaledArgs& args)
 {
     CUtensorMap ma, mb;
     cudaError_t e = gemm::encode_map(&ma, q_x, 1, true, shape.m, shape.k, ldqx, 128, shape.tile_rows);
     if (e == cudaSuccess) e = gemm::encode_map(&mb, q_w, 1, true, shape.n, shape.k, ldqw, 128, BN / CTAS);
     if (e != cudaSuccess) return e;
-    return gemm::launch<true, BN, CTAS, false, false, ScaledOut>(s, ma, mb, ma, shape, args);
+    if (args.type == BIGCN_F32) return gemm::launch<true, BN, CTAS, false, false, ScaledOut<BIGCN_F32>>(s, ma, mb, ma, shape, args);
+    if (args.type == BIGCN_BF16) return gemm::launch<true, BN, CTAS, false, false, ScaledOut<BIGCN_BF16>>(s, ma, mb, ma, shape, args);
+    return gemm::launch<true, BN, CTAS, false, false, ScaledOut<BIGCN_F16>>(s, ma, mb, ma, shape, args);
 }
 
 template <int BN>
-cudaError_t launch_across(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const int8_t* q_w, int64_t ldqw, const gemm::Shape& shape, const ScaledOut::Args& args)
+cudaError_t launch_across(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const int8_t* q_w, int64_t ldqw, const gemm::Shape& shape, const ScaledArgs& args)
 {
     CUtensorMap ma, mb;
     cudaError_t e = gemm::encode_map(&ma, q_w, 1, true, shape.m, shape.k, ldqw, 128, shape.tile_rows);
@@ -426,7 +439,7 @@ cudaError_t launch_quantize_rows(cudaStream_t s, const void* x, int type, int64_
 cudaError_t launch_quantized_product(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const float* s_x, int64_t n, int d, const int8_t* q_w, int64_t ldqw,
                                      const float* s_w, int m, void* out, int out_type, int64_t ldo, bool early, int* launches)
 {
-    const ScaledOut::Args args = {s_x, s_w, reinterpret_cast<uintptr_t>(s_w) % 16 == 0, out, out_type, ldo, rows_whole(out, ldo, out_type, 8)};
+    const ScaledArgs args = {s_x, s_w, reinterpret_cast<uintptr_t>(s_w) % 16 == 0, out, out_type, ldo, rows_whole(out, ldo, out_type, 8)};
     gemm::Shape shape;
     shape.m = (int)n;
     shape.n = m;

@@ -126,8 +126,9 @@ enum {
      * tolerance; their fp32 sums differ in rounding.  In order 2 a row of A_tilde diag(beta) with a NaN or an infinity, or
      * without a fixed point because all of it is below 2^-87 or some of it above 2^104, is summed in fp32 as it is written. */
     BIGCN_OPT_ORDER = 5,
-    /* Bound of every wait of one part of a thread block for another in the product P B of order 2, in tries of up to a
-     * microsecond: 0 = default (2^20), at most 2^20.  A block whose wait runs out ends early, its outputs unwritten, and
+    /* Bound of every wait of one part of a thread block for another in the product P B of order 2, in the products of 8-bit
+     * rows and in those of the class loss, in tries of up to a microsecond: 0 = default (2^20; 2^22 in the latter two), at
+     * most 2^20.  A block whose wait runs out ends early, its outputs unwritten, and
      * bigcn_sync_check() reports BIGCN_ERR_INTERNAL from then on.  For tests of that path. */
     BIGCN_OPT_WAIT_TRIES = 6
 };

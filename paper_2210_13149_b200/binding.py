@@ -485,6 +485,8 @@ class BiGCN:
     def _scratch(self, nbytes: int):
         """Workspace on the context's own stream.  One that a graph capture has used stays alive with the context."""
         if self.workspace is None or self.workspace.numel() < nbytes:
+            if self.workspace is not None and not torch._C._cuda_isCurrentStreamCapturing():
+                self.workspace.record_stream(self.stream)       # it may have been allocated while another stream was current
             with torch.cuda.stream(self.stream):
                 self.ensure_workspace(nbytes)
         if torch._C._cuda_isCurrentStreamCapturing() and not any(w is self.workspace for w in self._captured):

@@ -1081,7 +1081,7 @@ bigcn_status bigcn_class_loss(bigcn_ctx* ctx, const void* x, const void* w, int3
     if (!loss || !lse) return fail(ctx, BIGCN_ERR_NULL, "loss or lse is null");
     const size_t need = class_loss_scratch_bytes(n, d, classes, false);
     if (!ctx->ws || ctx->ws_bytes < need) return fail(ctx, BIGCN_ERR_WORKSPACE, "needs %zu bytes of workspace (bigcn_class_loss_workspace_bytes)", need);
-    cudaError_t e = launch_class_loss(ctx->stream, type, x, ldx, w, ldw, n, d, classes, labels, loss, lse, ctx->ws, &ctx->launches_i);
+    cudaError_t e = launch_class_loss(ctx->stream, type, x, ldx, w, ldw, n, d, classes, labels, loss, lse, ctx->ws, ctx->wait_tries, &ctx->launches_i);
     finish_call(ctx);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "class loss launch");
     return BIGCN_OK;
@@ -1104,7 +1104,7 @@ bigcn_status bigcn_class_loss_backward(bigcn_ctx* ctx, const void* x, const void
     if (!lse || !g_loss) return fail(ctx, BIGCN_ERR_NULL, "lse or g_loss is null");
     const size_t need = class_loss_scratch_bytes(n, d, classes, true);
     if (!ctx->ws || ctx->ws_bytes < need) return fail(ctx, BIGCN_ERR_WORKSPACE, "needs %zu bytes of workspace (bigcn_class_loss_workspace_bytes)", need);
-    cudaError_t e = launch_class_loss_backward(ctx->stream, type, x, ldx, w, ldw, n, d, classes, labels, lse, g_loss, g_x, ldgx, g_w, ldgw, ctx->ws, &ctx->launches_i);
+    cudaError_t e = launch_class_loss_backward(ctx->stream, type, x, ldx, w, ldw, n, d, classes, labels, lse, g_loss, g_x, ldgx, g_w, ldgw, ctx->ws, ctx->wait_tries, &ctx->launches_i);
     finish_call(ctx);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "class loss backward launch");
     return BIGCN_OK;
@@ -1168,7 +1168,7 @@ bigcn_status bigcn_quantized_product(bigcn_ctx* ctx, const void* x, int32_t x_ty
         ldx = ldq;
         s_x = scale;
     }
-    if (e == cudaSuccess) e = launch_quantized_product(ctx->stream, q_x, ldx, s_x, n, d, q_w, ldqw, s_w, m, out, out_type, ldo, early, &ctx->launches_i);
+    if (e == cudaSuccess) e = launch_quantized_product(ctx->stream, q_x, ldx, s_x, n, d, q_w, ldqw, s_w, m, out, out_type, ldo, early, ctx->wait_tries, &ctx->launches_i);
     finish_call(ctx);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "quantized product launch");
     return BIGCN_OK;

@@ -216,7 +216,7 @@ cudaError_t launch_layer_norm_backward(cudaStream_t s, const void* g, int g_type
 // Rows in 8-bit integers and their product with 8-bit class rows (quant.cu).
 cudaError_t launch_quantize_rows(cudaStream_t s, const void* x, int type, int64_t n, int d, int64_t ldx, int8_t* q, int64_t ldq, float* scale, bool early, int* launches);
 cudaError_t launch_quantized_product(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const float* s_x, int64_t n, int d, const int8_t* q_w, int64_t ldqw,
-                                     const float* s_w, int m, void* out, int out_type, int64_t ldo, bool early, int* launches);
+                                     const float* s_w, int m, void* out, int out_type, int64_t ldo, bool early, int tries, int* launches);
 // One to four rows that are not quantised yet, in one launch, where that is expected to be faster.
 bool few_rows_pays(int64_t n, int d, int m);
 cudaError_t launch_few_rows_product(cudaStream_t s, const void* x, int type, int64_t ldx, int64_t n, int d, const int8_t* q_w, int64_t ldqw, const float* s_w, int m,
@@ -229,9 +229,9 @@ int quant_timeouts();
 // Softmax cross entropy of bf16 or fp16 rows against a class matrix, and its gradients (class_loss.cu).
 size_t class_loss_scratch_bytes(int64_t n, int d, int classes, bool backward);
 cudaError_t launch_class_loss(cudaStream_t s, int type, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n, int d, int classes, const int64_t* labels,
-                              float* loss, float* lse, void* scratch, int* launches);
+                              float* loss, float* lse, void* scratch, int tries, int* launches);
 cudaError_t launch_class_loss_backward(cudaStream_t s, int type, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n, int d, int classes, const int64_t* labels,
-                                       const float* lse, const float* g_loss, void* g_x, int64_t ldgx, void* g_w, int64_t ldgw, void* scratch, int* launches);
+                                       const float* lse, const float* g_loss, void* g_x, int64_t ldgx, void* g_w, int64_t ldgw, void* scratch, int tries, int* launches);
 int class_loss_timeouts();
 
 }  // namespace bigcn

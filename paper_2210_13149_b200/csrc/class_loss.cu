@@ -741,6 +741,7 @@ Plan make_plan(int64_t n, int d, int classes, bool backward, bool half)
 }
 
 struct Operands {
+    int tries;               // bound of the products' waits (0 = default)
     const void* x;
     int64_t ldx;
     bool x_whole;
@@ -751,7 +752,7 @@ struct Operands {
 
 // Lists the labelled rows, copies them together where that is needed, and lays the class matrix on 16-byte boundaries.
 cudaError_t prepare(cudaStream_t s, const Plan& p, char* ws, int type, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n, int d, int classes,
-                    const int64_t* labels, float* loss, float* lse, const float* of_lse, const float* of_g_loss, void* g_x, int64_t ldgx, Operands* o, int* launches)
+                    const int64_t* labels, float* loss, float* lse, const float* of_lse, const float* of_g_loss, void* g_x, int64_t ldgx, int tries, Operands* o, int* launches)
 {
     int* counts = reinterpret_cast<int*>(ws + p.counts);
     unsigned* top = type == BIGCN_F16 && of_g_loss ? reinterpret_cast<unsigned*>(ws + p.top) : nullptr;
@@ -767,7 +768,7 @@ cudaError_t prepare(cudaStream_t s, const Plan& p, char* ws, int type, const voi
                            reinterpret_cast<int*>(ws + p.place), reinterpret_cast<int*>(ws + p.count), loss, lse,
                            (reinterpret_cast<uintptr_t>(loss) | reinterpret_cast<uintptr_t>(lse)) % 16 == 0, of_lse, of_g_loss,
                            reinterpret_cast<float*>(ws + p.lse), reinterpret_cast<float*>(ws + p.g_loss), top};
-    *o = {x, ldx, rows_whole(x, ldx, BIGCN_BF16, 8), reinterpret_cast<const uint16_t*>(ws + p.x), w, ldw};
+    *o = {tries, x, ldx, rows_whole(x, ldx, BIGCN_BF16, 8), reinterpret_cast<const uint16_t*>(ws + p.x), w, ldw};
     // rows of a warp at a time: as many times as it takes with 32, and the same each time
     const int resident = o->x_whole && d <= 256 ? 8 : 6;     // blocks of the kernel on a multiprocessor
     const int64_t warps = 8 * resident * sm_count();
@@ -834,6 +835,7 @@ cudaError_t launch_logits(cudaStream_t s, const Plan& p, const Operands& o, int6
     sh.base = (int)first_row;
     sh.alt_a = o.x_whole;
     sh.half = type == BIGCN_F16;
+    sh.tries = o.tries;
     sh.rotate = rows <= gemm::kRows;          // classes are read once
     ++*launches;
     return gemm::launch<false, BN, CTAS, false, false, Epi>(s, a, b, own, sh, args);
@@ -860,7 +862,7 @@ cudaError_t launch_gradient(cudaStream_t s, int bn, const CUtensorMap& g, const 
 
 template <int TYPE>
 cudaError_t backward_as(cudaStream_t s, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n, int d, int classes, const int64_t* labels,
-                                       const float* lse, const float* g_loss, void* g_x, int64_t ldgx, void* g_w, int64_t ldgw, void* scratch, int* launches)
+                                       const float* lse, const float* g_loss, void* g_x, int64_t ldgx, void* g_w, int64_t ldgw, void* scratch, int tries, int* launches)
 {
     char* ws = static_cast<char*>(scratch);
     cudaError_t e;
@@ -868,7 +870,7 @@ cudaError_t backward_as(cudaStream_t s, const void* x, int64_t ldx, const void* 
     constexpr bool half = TYPE == BIGCN_F16;
     const Plan p = make_plan(n, d, classes, true, half);
     Operands o;
-    e = prepare(s, p, ws, type, x, ldx, w, ldw, n, d, classes, labels, nullptr, nullptr, lse, g_loss, g_x, ldgx, &o, launches);
+    e = prepare(s, p, ws, type, x, ldx, w, ldw, n, d, classes, labels, nullptr, nullptr, lse, g_loss, g_x, ldgx, tries, &o, launches);
     const int* count = reinterpret_cast<const int*>(ws + p.count);
     const int* kept = reinterpret_cast<const int*>(ws + p.kept);
     const int* label = reinterpret_cast<const int*>(ws + p.label);
@@ -890,6 +892,7 @@ cudaError_t backward_as(cudaStream_t s, const void* x, int64_t ldx, const void* 
             sh.of = (int)n;
             sh.base = (int)first;
             sh.half = half;
+            sh.tries = tries;
             if (g_x) {
                 CUtensorMap mg, mw;
                 sh.tile_rows = gemm::rows_of_one_tile(rows);
@@ -954,13 +957,13 @@ int class_loss_timeouts()
 size_t class_loss_scratch_bytes(int64_t n, int d, int classes, bool backward) { return make_plan(n, d, classes, backward, true).bytes; }
 
 cudaError_t launch_class_loss(cudaStream_t s, int type, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n, int d, int classes, const int64_t* labels,
-                              float* loss, float* lse, void* scratch, int* launches)
+                              float* loss, float* lse, void* scratch, int tries, int* launches)
 {
     char* ws = static_cast<char*>(scratch);
     cudaError_t e;
     const Plan p = make_plan(n, d, classes, false, false);
     Operands o;
-    e = prepare(s, p, ws, type, x, ldx, w, ldw, n, d, classes, labels, loss, lse, nullptr, nullptr, nullptr, 0, &o, launches);
+    e = prepare(s, p, ws, type, x, ldx, w, ldw, n, d, classes, labels, loss, lse, nullptr, nullptr, nullptr, 0, tries, &o, launches);
     const int* count = reinterpret_cast<const int*>(ws + p.count);
     const int* kept = reinterpret_cast<const int*>(ws + p.kept);
     float* at = reinterpret_cast<float*>(ws + p.at);
@@ -985,10 +988,10 @@ cudaError_t launch_class_loss(cudaStream_t s, int type, const void* x, int64_t l
 
 cudaError_t launch_class_loss_backward(cudaStream_t s, int type, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n, int d, int classes,
                                        const int64_t* labels, const float* lse, const float* g_loss, void* g_x, int64_t ldgx, void* g_w, int64_t ldgw,
-                                       void* scratch, int* launches)
+                                       void* scratch, int tries, int* launches)
 {
-    return type == BIGCN_F16 ? backward_as<BIGCN_F16>(s, x, ldx, w, ldw, n, d, classes, labels, lse, g_loss, g_x, ldgx, g_w, ldgw, scratch, launches)
-                             : backward_as<BIGCN_BF16>(s, x, ldx, w, ldw, n, d, classes, labels, lse, g_loss, g_x, ldgx, g_w, ldgw, scratch, launches);
+    return type == BIGCN_F16 ? backward_as<BIGCN_F16>(s, x, ldx, w, ldw, n, d, classes, labels, lse, g_loss, g_x, ldgx, g_w, ldgw, scratch, tries, launches)
+                             : backward_as<BIGCN_BF16>(s, x, ldx, w, ldw, n, d, classes, labels, lse, g_loss, g_x, ldgx, g_w, ldgw, scratch, tries, launches);
 }
 
 }  // namespace bigcn

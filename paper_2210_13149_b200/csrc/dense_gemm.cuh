@@ -42,6 +42,7 @@ struct Shape {
     int m, n, k;             // rows, columns, depth (elements)
     int splits = 1;          // of the depth
     int half = 0;            // 16-bit operands: 1 for fp16, 0 for bf16
+    int tries = 0;           // bound of the waits inside a block (0 = default)
     const int* count = nullptr;
     int of = 0, base = 0;
     bool over_depth = false, alt_a = false, alt_b = false;
@@ -121,9 +122,9 @@ __device__ __forceinline__ void init_barrier(uint64_t* bar, int count)
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(tc::smem_u32(bar)), "r"(count) : "memory");
 }
 // true once the phase is complete; false when the block gave up
-__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile int* abort, int* flag)
+__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile int* abort, int* flag, int tries)
 {
-    for (int it = 0; it < kTries; ++it) {
+    for (int it = 0; it < tries; ++it) {
         uint32_t done;
         asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
                      : "=r"(done) : "r"(tc::smem_u32(bar)), "r"(parity) : "memory");
@@ -372,6 +373,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     const uint32_t tmem = ctl.tmem;
     volatile int* abort = &ctl.abort;
     int* const flag = Epi::flag();
+    const int tries = shape.tries > 0 ? shape.tries : kTries;
 
     int early = 0;           // stages whose A is on its way
     const auto depth_at = [&](const Unit& t, int k) {        // of the stage k in [k0, k1)
@@ -408,7 +410,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 const Unit t = walk.at(u);
                 const int arow = t.row + (int)rank * kRows, brow = t.col + (int)rank * C::kBRows;
                 for (int k = t.k0; k < t.k1; ++k) {
-                    ok = wait(&ctl.empty[slot], phase ^ 1u, abort, flag);
+                    ok = wait(&ctl.empty[slot], phase ^ 1u, abort, flag, tries);
                     if (!ok) break;
                     const int at = depth_at(t, k) * kDepth;
                     const bool fetched = issued < early;
@@ -433,16 +435,16 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             }
             // every stage handed back: nothing of the cluster touches this block's barriers or stages any more
             for (int i = 0; i < C::kStages && ok; ++i) {
-                ok = wait(&ctl.empty[slot], phase ^ 1u, abort, flag);
+                ok = wait(&ctl.empty[slot], phase ^ 1u, abort, flag, tries);
                 if (++slot == C::kStages) slot = 0, phase ^= 1u;
             }
             if (!ok) {
-                // gave up: the copies that were issued have to land first; a second block's are counted at the first's barriers, so time
-                // (a thousand times what a copy takes) stands in for them
+                // gave up: the copies that were issued have to land first.  A pair's are counted at one block's barriers, which the other block may
+                // have left short, so time (a thousand times what a copy takes) stands in for them
                 volatile int none = 0;
-                if (rank == 0)
+                if (CTAS == 1)
                     for (int64_t j = issued > C::kStages ? issued - C::kStages : 0; j < issued; ++j)
-                        wait(&ctl.full[j % C::kStages], (uint32_t)(j / C::kStages) & 1u, &none, flag);
+                        wait(&ctl.full[j % C::kStages], (uint32_t)(j / C::kStages) & 1u, &none, flag, kTries);
                 for (int i = 0; i < 10; ++i) __nanosleep(1000000);
             }
         }
@@ -458,12 +460,12 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             bool ok = true, any = false;
             for (int u = first; u < units && ok; u += step) {
                 const Unit t = walk.at(u);
-                ok = wait(&ctl.acc_empty[buf], acc_phase ^ 1u, abort, flag);
+                ok = wait(&ctl.acc_empty[buf], acc_phase ^ 1u, abort, flag, tries);
                 if (!ok) break;
                 tc::fence_after_sync();
                 const uint32_t acc = tmem + (uint32_t)(buf * BN);
                 for (int k = t.k0; k < t.k1; ++k) {
-                    ok = wait(&ctl.full[slot], phase, abort, flag);
+                    ok = wait(&ctl.full[slot], phase, abort, flag, tries);
                     if (!ok) break;
                     tc::fence_after_sync();
                     const uint32_t sa = tc::smem_u32(stages + slot * C::kStage), sb = sa + C::kABytes;
@@ -479,13 +481,14 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 commit<CTAS>(&ctl.acc_full[buf]);        // (at once where there is no depth)
                 if (++buf == kBuffers) buf = 0, acc_phase ^= 1u;
             }
-            if (!ok && any) {
+            if (any) {
+                // all products done, whether or not an epilogue warp (which may have given up) waits for the last of them
                 volatile int none = 0;
                 if constexpr (CTAS == 2)
                     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" ::"r"(tc::smem_u32(&ctl.drained)) : "memory");
                 else
                     commit<1>(&ctl.drained);
-                wait(&ctl.drained, 0, &none, flag);
+                wait(&ctl.drained, 0, &none, flag, kTries);
             }
         }
         __syncwarp();
@@ -510,7 +513,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 ahead = Epi::row(args, coming.row + own + lane, walk.m);
             }
             // where an epilogue lets the warps of the same rows meet, they go on or give up together
-            const bool there = __all_sync(0xffffffffu, wait(&ctl.acc_full[buf], acc_phase, abort, flag));
+            const bool there = __all_sync(0xffffffffu, wait(&ctl.acc_full[buf], acc_phase, abort, flag, tries));
             if constexpr (Epi::kMeets && kParts > 1) {
                 if (!meet(part.meeting, 32 * kParts, there)) break;
             } else {

@@ -437,13 +437,14 @@ cudaError_t launch_quantize_rows(cudaStream_t s, const void* x, int type, int64_
 }
 
 cudaError_t launch_quantized_product(cudaStream_t s, const int8_t* q_x, int64_t ldqx, const float* s_x, int64_t n, int d, const int8_t* q_w, int64_t ldqw,
-                                     const float* s_w, int m, void* out, int out_type, int64_t ldo, bool early, int* launches)
+                                     const float* s_w, int m, void* out, int out_type, int64_t ldo, bool early, int tries, int* launches)
 {
     const ScaledArgs args = {s_x, s_w, reinterpret_cast<uintptr_t>(s_w) % 16 == 0, out, out_type, ldo, rows_whole(out, ldo, out_type, 8)};
     gemm::Shape shape;
     shape.m = (int)n;
     shape.n = m;
     shape.k = d;
+    shape.tries = tries;
     shape.rotate = n <= gemm::kRows;          // class rows are read once
     shape.tile_rows = gemm::rows_of_one_tile(n);
     ++*launches;

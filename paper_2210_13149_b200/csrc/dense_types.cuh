@@ -193,15 +193,14 @@ struct Raw {
             pack(f);
         }
     }
-    // the same through shared memory: an asynchronous copy to a place of this thread's own, what does not exist as zeros
-    static __device__ __forceinline__ void copy(void* to, const void* base, int64_t at, int count)
+    // the same through shared memory: an asynchronous copy of `count` elements to a place of this thread's own, zeros behind them
+    static __device__ __forceinline__ void copy_to(void* to, const typename Elt<TYPE < 0 ? 0 : TYPE>::T* from, int count)
     {
         constexpr int kBytes = 4 * kWords;
-        const int bytes = count >= V ? kBytes : count > 0 ? count * type_bytes(TYPE) : 0;
-        const auto* p = static_cast<const typename Elt<TYPE>::T*>(base) + (count > 0 ? at : 0);
+        const int bytes = count * type_bytes(TYPE);
         const uint32_t dst = (uint32_t)__cvta_generic_to_shared(to);
-        if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(p), "r"(bytes) : "memory");
-        else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;\n" ::"r"(dst), "l"(p), "r"(bytes) : "memory");
+        if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(from), "r"(bytes) : "memory");
+        else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;\n" ::"r"(dst), "l"(from), "r"(bytes) : "memory");
     }
     __device__ __forceinline__ void take(const void* from)
     {

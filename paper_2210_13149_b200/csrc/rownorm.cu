@@ -49,23 +49,26 @@ __device__ __forceinline__ void group_sum(float (&v)[COUNT], float* slot)
     }
 }
 
-// The columns' factors of a kernel whose threads own more than 8 columns each: in shared memory, `none` past d and where there are none.
+// The columns' factors of a kernel whose threads own more than 8 columns each: in shared memory, `none` past d and where there are none.  Words of
+// 8 columns lie as two halves `padded` / 2 apart, so that lanes read 16 bytes next to each other.
+template <int V>
 __device__ __forceinline__ void stage_columns(float* to, const float* p, float none, int d, int padded)
 {
-    for (int c = threadIdx.x; c < padded; c += blockDim.x) to[c] = c < d && p ? __ldg(p + c) : none;
+    for (int c = threadIdx.x; c < padded; c += blockDim.x)
+        to[V == 8 ? (c >> 2 & 1) * (padded / 2) + (c >> 3) * 4 + (c & 3) : c] = c < d && p ? __ldg(p + c) : none;
 }
 template <int V>
-__device__ __forceinline__ void staged(const float* from, float (&v)[V])
+__device__ __forceinline__ void staged(const float* from, int c, int padded, float (&v)[V])
 {
     if constexpr (V % 4 == 0) {
 #pragma unroll
         for (int i = 0; i < V; i += 4) {
-            const float4 q = *reinterpret_cast<const float4*>(from + i);
+            const float4 q = *reinterpret_cast<const float4*>(from + (V == 8 ? i / 4 * (padded / 2) + (c >> 3) * 4 : c));
             v[i] = q.x; v[i + 1] = q.y; v[i + 2] = q.z; v[i + 3] = q.w;
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = from[i];
+        for (int i = 0; i < V; ++i) v[i] = from[c + i];
     }
 }
 
@@ -110,8 +113,8 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads, norm_blocks(LAN
                 offset[k * V + i] = c < a.d && a.offset ? __ldg(a.offset + c) : 0.f;
             }
     } else {
-        stage_columns(dyn, a.gain, 1.f, a.d, LANES * V * NV);
-        stage_columns(dyn + LANES * V * NV, a.offset, 0.f, a.d, LANES * V * NV);
+        stage_columns<V>(dyn, a.gain, 1.f, a.d, LANES * V * NV);
+        stage_columns<V>(dyn + LANES * V * NV, a.offset, 0.f, a.d, LANES * V * NV);
         __syncthreads();
     }
     const int64_t step = (int64_t)gridDim.x * GROUPS;
@@ -159,8 +162,8 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads, norm_blocks(LAN
 #pragma unroll
                     for (int i = 0; i < V; ++i) g[i] = gain[k * V + i], o[i] = offset[k * V + i];
                 } else {
-                    staged<V>(dyn + c, g);
-                    staged<V>(dyn + LANES * V * NV + c, o);
+                    staged<V>(dyn, c, LANES * V * NV, g);
+                    staged<V>(dyn + LANES * V * NV, c, LANES * V * NV, o);
                 }
 #pragma unroll
                 for (int i = 0; i < V; ++i) v[k][i] = fmaf(v[k][i] * r, g[i], o[i]);
@@ -229,7 +232,7 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads, BackLayout<GTYP
                 gain[k * V + i] = c < a.d && a.gain ? __ldg(a.gain + c) : 1.f;
             }
     } else {
-        stage_columns(gains, a.gain, 1.f, a.d, LANES * V * NV);
+        stage_columns<V>(gains, a.gain, 1.f, a.d, LANES * V * NV);
     }
     if constexpr (!kShared) {
 #pragma unroll
@@ -258,21 +261,29 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads, BackLayout<GTYP
     auto place = [&](int slot, int k, bool of_g) {
         return raw + (size_t)slot * L::kRowBytes * B + (of_g ? (size_t)NV * kXBytes * B + ((size_t)k * B + threadIdx.x) * kGBytes : ((size_t)k * B + threadIdx.x) * kXBytes);
     };
-    auto send = [&](int64_t r, int slot) {
+    // what a lane copies of a row is the same for all rows; its place in the matrices moves on by a constant
+    int64_t sent = row;
+    const typename Elt<(kRing > 0 ? TYPE : 0)>::T* from_x = static_cast<const typename Elt<(kRing > 0 ? TYPE : 0)>::T*>(a.x) + row * a.ldx + lane * V;
+    const typename Elt<(kRing > 0 ? GTYPE : 0)>::T* from_g = static_cast<const typename Elt<(kRing > 0 ? GTYPE : 0)>::T*>(a.g) + row * a.ldg + lane * V;
+    auto send = [&](int slot) {
         if constexpr (kRing > 0) {
+            const bool live = sent < a.n;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                const int c = (k * LANES + lane) * V, count = r < a.n ? a.d - c : 0;
-                Raw<TYPE, V>::copy(place(slot, k, false), a.x, r * a.ldx + c, count);
-                Raw<GTYPE, V>::copy(place(slot, k, true), a.g, r * a.ldg + c, count);
+                const int there = a.d - (k * LANES + lane) * V, count = live ? max(0, min(there, V)) : 0;
+                Raw<TYPE, V>::copy_to(place(slot, k, false), count > 0 ? from_x + k * LANES * V : static_cast<const typename Elt<TYPE>::T*>(a.x), count);
+                Raw<GTYPE, V>::copy_to(place(slot, k, true), count > 0 ? from_g + k * LANES * V : static_cast<const typename Elt<GTYPE>::T*>(a.g), count);
             }
             asm volatile("cp.async.commit_group;\n" ::: "memory");
+            sent += step;
+            from_x += step * a.ldx;
+            from_g += step * a.ldg;
         }
     };
     int slot = 0;
     if constexpr (kRing > 0) {
 #pragma unroll
-        for (int i = 0; i < kRing - 1; ++i) send(row + i * step, i);
+        for (int i = 0; i < kRing - 1; ++i) send(i);
         nmean = row < a.n ? __ldg(a.mean + row) : 0.f;
         nrstd = row < a.n ? __ldg(a.rstd + row) : 0.f;
     }
@@ -280,7 +291,7 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads, BackLayout<GTYP
     for (int64_t base = (int64_t)blockIdx.x * GROUPS, trip = 0; base < a.n; base += step, row += step, ++trip) {
         float xh[NV][V], gv[NV][V], sums[2] = {0.f, 0.f};
         if constexpr (kRing > 0) {
-            send(row + (kRing - 1) * step, slot == 0 ? kRing - 1 : slot - 1);
+            send(slot == 0 ? kRing - 1 : slot - 1);
             asm volatile("cp.async.wait_group %0;\n" ::"n"(kRing > 0 ? kRing - 1 : 0) : "memory");
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
@@ -310,15 +321,15 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads, BackLayout<GTYP
 #pragma unroll
                 for (int i = 0; i < V; ++i) w[i] = gain[k * V + i];
             } else {
-                staged<V>(gains + c, w);
+                staged<V>(gains, c, LANES * V * NV, w);
             }
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const bool in = row < a.n && c + i < a.d;
-                xh[k][i] = in ? (xh[k][i] - mu) * r : 0.f;
-                const float gi = gv[k][i];                       // 0 where there is no element
+                // (where there is no element x and g are 0: its xhat adds nothing, and nothing is kept of it)
+                xh[k][i] = (xh[k][i] - mu) * r;
+                const float gi = gv[k][i];
                 if constexpr (kShared) {
-                    if (in) {
+                    if (row < a.n && c + i < a.d) {
                         dyn[c + i] = fmaf(gi, xh[k][i], dyn[c + i]);
                         dyn[a.d + c + i] += gi;
                     }
@@ -333,11 +344,11 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads, BackLayout<GTYP
         }
         group_sum<LANES, 2>(sums, slots[trip & 1]);
         if (row < a.n) {
-            const float sa = sums[0] * inv_d, sb = sums[1] * inv_d;
+            const float sa = sums[0] * inv_d * r, sb = sums[1] * inv_d * r;
 #pragma unroll
             for (int k = 0; k < NV; ++k)
 #pragma unroll
-                for (int i = 0; i < V; ++i) gv[k][i] = (gv[k][i] - sa - xh[k][i] * sb) * r;
+                for (int i = 0; i < V; ++i) gv[k][i] = fmaf(-xh[k][i], sb, fmaf(gv[k][i], r, -sa));
             store_row<NV, V>(a.gx, a.gx_type, row * a.ldgx, lane * V, LANES * V, a.d, a.gx_step, gv);
         }
     }

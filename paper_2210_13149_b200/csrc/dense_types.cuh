@@ -163,34 +163,74 @@ __device__ __forceinline__ void store_row(void* base, int type, int64_t row_at, 
     else store_row_of<BIGCN_F16, NV, V>(base, row_at, c, stride, d, step, v);
 }
 
-// V elements as they lie in memory: 8 or 16 bytes of a type known when compiled, or else fp32 values.
+// V elements as they lie in memory, words of 32 bits (a 16-bit element alone in the low half of one).  Nothing is done with them where they are loaded, so
+// that a row asked for ahead of its time is not waited for before it.
 template <int TYPE, int V>
 struct Raw {
-    static constexpr bool kPacked = TYPE != kAnyType && V * type_bytes(TYPE) >= 8;
-    static constexpr int kWords = kPacked ? V * type_bytes(TYPE) / 4 : V;
+    static constexpr int kWords = TYPE == kAnyType || TYPE == BIGCN_F32 ? V : V > 1 ? V / 2 : 1;
     uint32_t w[kWords];
-    // of a type looked up: `whole` as in load_elts(); of a known type the address is aligned to the 16 (or 8) bytes
+
+    // The first `count` of V elements, zeros behind them.  whole: the address is aligned to V elements (or 16 bytes); otherwise to one.
     __device__ __forceinline__ void load(const void* base, int type, int64_t at, int count, bool whole = true)
     {
-        if constexpr (!kPacked) {
-            float f[V];
-            load_as<TYPE, V>(base, type, at, count, whole, f);
+        if (TYPE == BIGCN_F32 || (TYPE == kAnyType && type == BIGCN_F32)) load_words<BIGCN_F32>(static_cast<const float*>(base) + at, count, whole);
+        else load_words<BIGCN_BF16>(reinterpret_cast<const __nv_bfloat16*>(base) + at, count, whole);
+    }
+    template <int T>
+    __device__ __forceinline__ void load_words(const typename Elt<T>::T* p, int count, bool whole)
+    {
+        constexpr int kUsed = T == BIGCN_F32 ? V : V > 1 ? V / 2 : 1;
+        if constexpr (kUsed <= kWords) {
+            const uint32_t* q = reinterpret_cast<const uint32_t*>(p);
+            const unsigned short* h = reinterpret_cast<const unsigned short*>(p);
+            if (count >= V && whole) {
+                if constexpr (T != BIGCN_F32 && V == 1) {
+                    w[0] = *h;
+                } else if constexpr (kUsed == 1) {
+                    w[0] = *q;
+                } else if constexpr (kUsed == 2) {
+                    const uint2 v = *reinterpret_cast<const uint2*>(q);
+                    w[0] = v.x; w[1] = v.y;
+                } else {
 #pragma unroll
-            for (int i = 0; i < V; ++i) w[i] = __float_as_uint(f[i]);
-        } else if (count >= V) {
-            const auto* p = static_cast<const typename Elt<TYPE>::T*>(base) + at;
-            if constexpr (kWords == 4) {
-                const uint4 q = *reinterpret_cast<const uint4*>(p);
-                w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+                    for (int i = 0; i < kUsed; i += 4) {
+                        const uint4 v = *reinterpret_cast<const uint4*>(q + i);
+                        w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+                    }
+                }
+            } else if constexpr (T == BIGCN_F32) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) w[i] = i < count ? q[i] : 0u;
+            } else if (whole) {
+#pragma unroll
+                for (int i = 0; i < kUsed; ++i) w[i] = 2 * i + 1 < count ? q[i] : 2 * i < count ? (uint32_t)h[2 * i] : 0u;
             } else {
-                static_assert(kWords == 2, "");
-                const uint2 q = *reinterpret_cast<const uint2*>(p);
-                w[0] = q.x; w[1] = q.y;
+#pragma unroll
+                for (int i = 0; i < kUsed; ++i) w[i] = (2 * i < count ? (uint32_t)h[2 * i] : 0u) | (V > 1 && 2 * i + 1 < count ? (uint32_t)h[2 * i + 1] << 16 : 0u);
             }
+        }
+    }
+    __device__ __forceinline__ void values(float (&f)[V], int type = TYPE) const
+    {
+        if (TYPE == BIGCN_F32 || (TYPE == kAnyType && type == BIGCN_F32)) {
+            if constexpr (kWords == V) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) f[i] = __uint_as_float(w[i]);
+            }
+        } else if (TYPE == BIGCN_BF16 || (TYPE == kAnyType && type == BIGCN_BF16)) {
+            halves<BIGCN_BF16>(f);
         } else {
-            float f[V];
-            load_elts<TYPE, V>(static_cast<const typename Elt<TYPE>::T*>(base) + at, count, false, f);
-            pack(f);
+            halves<BIGCN_F16>(f);
+        }
+    }
+    template <int T>
+    __device__ __forceinline__ void halves(float (&f)[V]) const
+    {
+#pragma unroll
+        for (int i = 0; i < (V > 1 ? V / 2 : 1); ++i) {
+            const float2 u = unpack2<T>(w[i]);
+            f[2 * i] = u.x;
+            if constexpr (V > 1) f[2 * i + 1] = u.y;
         }
     }
     // the same through shared memory: an asynchronous copy of `count` elements to a place of this thread's own, zeros behind them
@@ -210,30 +250,6 @@ struct Raw {
         } else if constexpr (kWords == 2) {
             const uint2 q = *static_cast<const uint2*>(from);
             w[0] = q.x; w[1] = q.y;
-        }
-    }
-    __device__ __forceinline__ void pack(const float (&f)[V])
-    {
-        if constexpr (kWords == V) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) w[i] = __float_as_uint(f[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < V / 2; ++i) w[i] = pack2<TYPE>(f[2 * i], f[2 * i + 1]);
-        }
-    }
-    __device__ __forceinline__ void values(float (&f)[V]) const
-    {
-        if constexpr (kWords == V) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) f[i] = __uint_as_float(w[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < V / 2; ++i) {
-                const float2 u = unpack2<TYPE>(w[i]);
-                f[2 * i] = u.x;
-                f[2 * i + 1] = u.y;
-            }
         }
     }
 };

@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : 256, LANES > 32 ? 1 : NV 
         for (int k = 0; k < NV; ++k) {
             w[k] = next[k];
             float v[V];
-            w[k].values(v);
+            w[k].values(v, a.type);
 #pragma unroll
             for (int i = 0; i < V; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
         }
@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : 256, LANES > 32 ? 1 : NV 
             const int c = (k * LANES + lane) * V;
             if (c >= a.d) break;
             float v[V];
-            w[k].values(v);
+            w[k].values(v, a.type);
             uint32_t o[V / 4];
 #pragma unroll
             for (int j = 0; j < V / 4; ++j) o[j] = finite && top ? nearest4<TYPE == BIGCN_BF16 || TYPE == BIGCN_F16>(v + 4 * j, factor, t, tiny) : 0u;

@@ -89,6 +89,10 @@ struct NormArgs {
     float* rstd;
 };
 
+// Rows of a lane's words on their way at a time, of what a row takes in registers: 32 warps of a multiprocessor with 12 registers each on their way are
+// 48 KB, which covers a latency of a microsecond at the memory's rate (1,362,217 bf16 rows of 23 columns in us: 110 with one row that is converted where it is loaded, 95 so).
+__host__ __device__ constexpr int rows_ahead(int registers) { return registers <= 2 ? 4 : registers <= 4 ? 3 : 1; }
+
 // Blocks of the forward pass on a multiprocessor: 1,024 threads with 64 registers each, rows going round in all of them.
 constexpr int norm_blocks(int lanes) { return lanes > 32 ? 1024 / lanes : 1024 / kThreads; }
 
@@ -98,6 +102,7 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads, norm_blocks(LAN
     pdl_enter();
     constexpr int B = LANES > 32 ? LANES : kThreads, GROUPS = B / LANES;
     constexpr bool kHold = NV * V <= 8;          // gain and offset stay in registers over the rows
+    constexpr int kAhead = rows_ahead(NV * Raw<TYPE, V>::kWords);
     extern __shared__ float dyn[];               // else [2][LANES V NV]
     __shared__ float slots[2][LANES > 32 ? LANES / 32 : 1];
     const int lane = threadIdx.x % LANES;
@@ -119,24 +124,28 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads, norm_blocks(LAN
     }
     const int64_t step = (int64_t)gridDim.x * GROUPS;
     int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES;
-    Raw<TYPE, V> next[NV];                       // the row after this one is on its way while this one is worked on
-    auto fetch = [&](int64_t r) {
+    Raw<TYPE, V> next[kAhead][NV];               // the rows after this one are on their way while this one is worked on
+    auto fetch = [&](int64_t r, Raw<TYPE, V> (&to)[NV]) {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (k * LANES + lane) * V;
-            next[k].load(a.x, a.x_type, r * a.ldx + c, r < a.n ? a.d - c : 0);
+            to[k].load(a.x, a.x_type, r * a.ldx + c, r < a.n ? a.d - c : 0);
         }
     };
-    fetch(row);
-    for (int64_t base = (int64_t)blockIdx.x * GROUPS; base < a.n; base += step, row += step) {   // the same trips for all threads of a block
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) fetch(row + j * step, next[j]);
+    for (int64_t base = (int64_t)blockIdx.x * GROUPS; base < a.n;)   // the same trips for all threads of a block
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j, base += step, row += step) {
+        if (kAhead > 1 && base >= a.n) break;
         float v[NV][V], sum[1] = {0.f};
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            next[k].values(v[k]);
+            next[j][k].values(v[k], a.x_type);
 #pragma unroll
             for (int i = 0; i < V; ++i) sum[0] += v[k][i];
         }
-        fetch(row + step);
+        fetch(row + kAhead * step, next[j]);
         group_sum<LANES, 1>(sum, slots[0]);
         const float mu = sum[0] * inv_d;
         float sq[1] = {0.f};
@@ -204,7 +213,7 @@ struct BackLayout {
     static constexpr int kRowBytes = NV * 4 * (Raw<GTYPE, V>::kWords + Raw<TYPE, V>::kWords);      // of a thread
     static constexpr int kRing = !kTyped || kShared ? 0 : LANES >= 512 ? 2 : NV * V > 8 ? 3 : 4;
     static constexpr int kBlocks = LANES >= 512 ? 1 : LANES > 32 ? 512 / LANES : kHold ? 3 : 2;    // a multiprocessor, by their registers
-    static constexpr bool kAhead = !kRing && kRowBytes <= 64;                                      // the next row's words fit registers
+    static constexpr int kAhead = kRing || LANES > 32 ? 0 : kRowBytes <= 16 ? 4 : kRowBytes <= 32 ? 2 : 1;    // else: rows of them on their way in registers
     static constexpr int kRingBytes = kRing * kRowBytes * B;
     static size_t smem(int d) { return kRingBytes + (size_t)(kHold ? 0 : LANES * V * NV) * 4 + (LANES > 32 && !kShared ? 0 : (size_t)2 * d * 4); }
 };
@@ -215,7 +224,8 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads, BackLayout<GTYP
     pdl_enter();
     using L = BackLayout<GTYPE, TYPE, V, LANES, NV>;
     constexpr int B = L::B, GROUPS = B / LANES, kRing = L::kRing;
-    constexpr bool kHold = L::kHold, kAhead = L::kAhead, kShared = L::kShared;
+    constexpr bool kHold = L::kHold, kShared = L::kShared;
+    constexpr int kAhead = L::kAhead, kHeld = kAhead > 0 ? kAhead : 1;
     extern __shared__ __align__(16) unsigned char raw[];       // the ring, the gain, [2][d] for the block's sums
     float* const gains = reinterpret_cast<float*>(raw + L::kRingBytes);
     float* const dyn = gains + (kHold ? 0 : LANES * V * NV);
@@ -243,18 +253,18 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads, BackLayout<GTYP
     if constexpr (!kHold || kShared) __syncthreads();
     const int64_t step = (int64_t)gridDim.x * GROUPS;
     int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES;
-    Raw<TYPE, V> nx[NV];
-    Raw<GTYPE, V> ng[NV];
-    float nmean = 0.f, nrstd = 0.f;
-    auto fetch = [&](int64_t r) {
+    Raw<TYPE, V> nx[kHeld][NV];
+    Raw<GTYPE, V> ng[kHeld][NV];
+    float nmean[kHeld], nrstd[kHeld];
+    auto fetch = [&](int64_t r, int j) {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (k * LANES + lane) * V;
-            nx[k].load(a.x, a.x_type, r * a.ldx + c, r < a.n ? a.d - c : 0);
-            ng[k].load(a.g, a.g_type, r * a.ldg + c, r < a.n ? a.d - c : 0);
+            nx[j][k].load(a.x, a.x_type, r * a.ldx + c, r < a.n ? a.d - c : 0);
+            ng[j][k].load(a.g, a.g_type, r * a.ldg + c, r < a.n ? a.d - c : 0);
         }
-        nmean = r < a.n ? __ldg(a.mean + r) : 0.f;
-        nrstd = r < a.n ? __ldg(a.rstd + r) : 0.f;
+        nmean[j] = r < a.n ? __ldg(a.mean + r) : 0.f;
+        nrstd[j] = r < a.n ? __ldg(a.rstd + r) : 0.f;
     };
     // a thread's place in a slot of the ring: its words of x, then of g, 16-byte pieces B threads apart
     constexpr int kXBytes = Raw<TYPE, V>::kWords * 4, kGBytes = Raw<GTYPE, V>::kWords * 4;
@@ -284,35 +294,40 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads, BackLayout<GTYP
     if constexpr (kRing > 0) {
 #pragma unroll
         for (int i = 0; i < kRing - 1; ++i) send(i);
-        nmean = row < a.n ? __ldg(a.mean + row) : 0.f;
-        nrstd = row < a.n ? __ldg(a.rstd + row) : 0.f;
+        nmean[0] = row < a.n ? __ldg(a.mean + row) : 0.f;
+        nrstd[0] = row < a.n ? __ldg(a.rstd + row) : 0.f;
     }
-    if constexpr (kAhead) fetch(row);
-    for (int64_t base = (int64_t)blockIdx.x * GROUPS, trip = 0; base < a.n; base += step, row += step, ++trip) {
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) fetch(row + j * step, j);
+    int trip = 0;
+    for (int64_t base = (int64_t)blockIdx.x * GROUPS; base < a.n;)
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j, base += step, row += step, ++trip) {
+        if (kHeld > 1 && base >= a.n) break;
         float xh[NV][V], gv[NV][V], sums[2] = {0.f, 0.f};
         if constexpr (kRing > 0) {
             send(slot == 0 ? kRing - 1 : slot - 1);
             asm volatile("cp.async.wait_group %0;\n" ::"n"(kRing > 0 ? kRing - 1 : 0) : "memory");
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                nx[k].take(place(slot, k, false));
-                ng[k].take(place(slot, k, true));
+                nx[j][k].take(place(slot, k, false));
+                ng[j][k].take(place(slot, k, true));
             }
             if (++slot == kRing) slot = 0;
-        } else if constexpr (!kAhead) {
-            fetch(row);
+        } else if constexpr (kAhead == 0) {
+            fetch(row, j);
         }
-        const float mu = nmean, r = nrstd;
+        const float mu = nmean[j], r = nrstd[j];
         if constexpr (kRing > 0) {
-            nmean = row + step < a.n ? __ldg(a.mean + row + step) : 0.f;
-            nrstd = row + step < a.n ? __ldg(a.rstd + row + step) : 0.f;
+            nmean[0] = row + step < a.n ? __ldg(a.mean + row + step) : 0.f;
+            nrstd[0] = row + step < a.n ? __ldg(a.rstd + row + step) : 0.f;
         }
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            nx[k].values(xh[k]);
-            ng[k].values(gv[k]);
+            nx[j][k].values(xh[k], a.x_type);
+            ng[j][k].values(gv[k], a.g_type);
         }
-        if constexpr (kAhead) fetch(row + step);
+        if constexpr (kAhead > 0) fetch(row + kAhead * step, j);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (k * LANES + lane) * V;

@@ -473,7 +473,7 @@ class BiGCN:
         if step != 1 and d > 1:
             raise ValueError("%s: the elements of a row must lie next to each other" % name)
         if n <= 1:
-            return d
+            return d if t.dtype != torch.int8 else (d + 15) // 16 * 16      # (8-bit rows start on 16-byte boundaries, also where there is one)
         if ld < d:
             raise ValueError("%s: rows overlap" % name)
         return ld
@@ -492,12 +492,21 @@ class BiGCN:
         if torch._C._cuda_isCurrentStreamCapturing() and not any(w is self.workspace for w in self._captured):
             self._captured.append(self.workspace)
 
-    def _outs(self, *wanted):
-        """Outputs' memory, in the order of the context's stream: (rows, columns or 0 for a vector, dtype) each, or None."""
+    def _outs(self, *wanted, used=()):
+        """Outputs' memory, in the order of the context's stream: (rows, columns or 0 for a vector, dtype) each, or None.  Where another stream is
+        current, neither the call's inputs (`used`) nor its outputs are given away while the other of the two streams works with them."""
         if torch._C._cuda_getCurrentRawStream(self.device.index) == self._raw_stream:
             return [_dense(*w, self.device) if w else None for w in wanted]
+        now = torch.cuda.current_stream(self.device)
+        for t in used:
+            if t is not None:
+                t.record_stream(self.stream)
         with torch.cuda.stream(self.stream):
-            return [_dense(*w, self.device) if w else None for w in wanted]
+            outs = [_dense(*w, self.device) if w else None for w in wanted]
+        for t in outs:
+            if t is not None:
+                t.record_stream(now)
+        return outs
 
     def layer_norm(self, X: torch.Tensor, gain: Optional[torch.Tensor] = None, offset: Optional[torch.Tensor] = None,
                    eps: float = 1e-5, out_dtype: Optional[torch.dtype] = None):
@@ -509,7 +518,7 @@ class BiGCN:
         out_dtype = X.dtype if out_dtype is None else out_dtype
         if out_dtype not in (torch.float32, torch.bfloat16, torch.float16):
             raise ValueError("layer_norm: no output of type %s" % out_dtype)
-        Y, mean, rstd = self._outs((n, d, out_dtype), (n, 0, torch.float32), (n, 0, torch.float32))
+        Y, mean, rstd = self._outs((n, d, out_dtype), (n, 0, torch.float32), (n, 0, torch.float32), used=(X, gain, offset))
         self._check(self.lib.bigcn_layer_norm(self.h, _addr(X), TYPES[X.dtype], n, d, ldx, _addr(gain), _addr(offset), eps, _addr(Y),
                                               TYPES[out_dtype], d, _addr(mean), _addr(rstd)))
         return Y, mean, rstd
@@ -527,7 +536,7 @@ class BiGCN:
         if out_dtype not in (torch.float32, torch.bfloat16, torch.float16):
             raise ValueError("layer_norm_backward: no output of type %s" % out_dtype)
         self._scratch(_sizes("bigcn_layer_norm_workspace_bytes", d))
-        g_x, g_gain, g_offset = self._outs((n, d, out_dtype), (d, 0, torch.float32), (d, 0, torch.float32))
+        g_x, g_gain, g_offset = self._outs((n, d, out_dtype), (d, 0, torch.float32), (d, 0, torch.float32), used=(g_y, X, mean, rstd, gain))
         self._check(self.lib.bigcn_layer_norm_backward(
             self.h, _addr(g_y), TYPES[g_y.dtype], ldg, _addr(X), TYPES[X.dtype], ldx, n, d, _addr(gain), _addr(mean), _addr(rstd),
             _addr(g_x), TYPES[out_dtype], d, _addr(g_gain), _addr(g_offset)))
@@ -545,7 +554,7 @@ class BiGCN:
         A negative label marks a row that takes no part."""
         ldx, ldw, n, d, classes = self._class_rows(X, W, labels)
         self._scratch(_sizes("bigcn_class_loss_workspace_bytes", n, d, classes, 0))
-        loss, lse = self._outs((n, 0, torch.float32), (n, 0, torch.float32))
+        loss, lse = self._outs((n, 0, torch.float32), (n, 0, torch.float32), used=(X, W, labels))
         self._check(self.lib.bigcn_class_loss(self.h, _addr(X), _addr(W), TYPES[X.dtype], n, d, classes, ldx, ldw, _addr(labels), _addr(loss), _addr(lse)))
         return loss, lse
 
@@ -556,7 +565,7 @@ class BiGCN:
         self._vector("lse", lse, n)
         self._vector("g_loss", g_loss, n)
         self._scratch(_sizes("bigcn_class_loss_workspace_bytes", n, d, classes, 1))
-        g_x, g_w = self._outs((n, d, X.dtype) if want_g_x else None, (classes, d, X.dtype) if want_g_w else None)
+        g_x, g_w = self._outs((n, d, X.dtype) if want_g_x else None, (classes, d, X.dtype) if want_g_w else None, used=(X, W, labels, lse, g_loss))
         self._check(self.lib.bigcn_class_loss_backward(self.h, _addr(X), _addr(W), TYPES[X.dtype], n, d, classes, ldx, ldw, _addr(labels), _addr(lse),
                                                        _addr(g_loss), _addr(g_x), d, _addr(g_w), d))
         return g_x, g_w
@@ -566,7 +575,7 @@ class BiGCN:
         ldx = self._rows("X", X)
         n, d = X.shape
         ldq = (d + 15) // 16 * 16
-        q, scale = self._outs((n, ldq, torch.int8), (n, 0, torch.float32))
+        q, scale = self._outs((n, ldq, torch.int8), (n, 0, torch.float32), used=(X,))
         if ldq != d:
             with torch.cuda.stream(self.stream):
                 q[:, d:] = 0
@@ -600,7 +609,7 @@ class BiGCN:
         self._vector("s_w", s_w, m)
         if out_dtype not in (torch.float32, torch.bfloat16, torch.float16):
             raise ValueError("quantized_product: no output of type %s" % out_dtype)
-        out, = self._outs((n, m, out_dtype))
+        out, = self._outs((n, m, out_dtype), used=(X, s_x, q_w, s_w))
         self._check(self.lib.bigcn_quantized_product(self.h, _addr(X), TYPES[X.dtype], _addr(s_x), n, d, ldx, _addr(q_w), ldqw, _addr(s_w), m,
                                                      _addr(out), TYPES[out_dtype], m))
         return out

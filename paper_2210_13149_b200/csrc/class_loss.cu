@@ -421,6 +421,7 @@ struct Gradient {
     template <int BN, class Done>
     static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit&, const gemm::Part& p, const Row& of_row, const Done& done)
     {
+        if (p.row >= (p.rows + 127) / 128 * 128) return done();       // a pair's second block past the last row: G has no such rows
         const bool there = p.row + (int)(threadIdx.x & 31) < p.rows;
         const int label = of_row.label >= a.first_class + p.col ? of_row.label - a.first_class - p.col : INT_MIN;
         const float lse = of_row.lse, weight = TYPE == BIGCN_F16 ? kHalfScale : of_row.weight;

@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads, norm_blocks(LAN
     constexpr int B = LANES > 32 ? LANES : kThreads, GROUPS = B / LANES;
     constexpr bool kHold = NV * V <= 8;          // gain and offset stay in registers over the rows
     constexpr int kAhead = rows_ahead(NV * Raw<TYPE, V>::kWords);
-    extern __shared__ float dyn[];               // else [2][LANES V NV]
+    extern __shared__ __align__(16) float dyn[];  // else [2][LANES V NV]
     __shared__ float slots[2][LANES > 32 ? LANES / 32 : 1];
     const int lane = threadIdx.x % LANES;
     const float inv_d = 1.f / (float)a.d;

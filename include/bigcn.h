@@ -360,8 +360,8 @@ bigcn_status bigcn_col_stats(bigcn_ctx* ctx, const float* H, int64_t n, int32_t 
 /* ---- Dense ends of a classifier that stands on binarized layers --------------------------------------------------------
  * The paper has no counterpart of these calls: it ends at the last layer's H'.  A program that trains or serves a class
  * matrix on top of a hidden layer norms the layer's rows, takes the loss of the class matrix and its gradients, and serves
- * the same matrix in 8-bit integers.  Rows are row-major with any leading dimension >= their length, from any address
- * aligned to their elements; what a type other than fp32 holds is computed in fp32 and rounded once. */
+ * the same matrix in 8-bit integers.  Rows are row-major with any leading dimension >= their length and below 2^38, from
+ * any address aligned to their elements; what a type other than fp32 holds is computed in fp32 and rounded once. */
 enum bigcn_type {
     BIGCN_F32 = 0,
     BIGCN_BF16 = 1,
@@ -391,7 +391,8 @@ bigcn_status bigcn_layer_norm_backward(bigcn_ctx* ctx, const void* g_y, int32_t 
 
 /* Softmax cross entropy of rows against a class matrix: z_ik = sum_j x_ij w_kj over k < classes, lse_i = log sum_k exp z_ik,
  * loss_i = lse_i - z_i,label(i).  The logits z are never stored.  x [n x d], w [classes x d] (a row to a class), both of type
- * BIGCN_BF16 or both BIGCN_F16 (round fp32 rows to one of them: bigcn_layer_norm() writes them), products and sums in fp32; 1 <= d <= BIGCN_MAX_D_IN; n, classes < 2^31 - 512.  labels int64 [n]: a negative
+ * BIGCN_BF16 or both BIGCN_F16 (round fp32 rows to one of them: bigcn_layer_norm() writes them), products and sums in
+ * fp32; 1 <= d <= BIGCN_MAX_D_IN; n, classes < 2^31 - 512.  labels int64 [n]: a negative
  * one marks a row without a label, whose loss and lse are 0 and which takes no part in anything, whatever it holds; one
  * >= classes is an error that shows as NaN in loss_i and lse_i and is otherwise a row without a label.  loss, lse fp32 [n].
  * Needs bigcn_class_loss_workspace_bytes(n, d, classes, 0) of workspace.

@@ -191,11 +191,12 @@ bigcn_status check_type(bigcn_ctx* ctx, const char* name, int32_t type)
 
 // Rows of a dense operator; counts stay far enough below 2^31 for tiles that reach past them.
 constexpr int64_t kMaxRows = (int64_t(1) << 31) - 512;
+constexpr int64_t kMaxLd = int64_t(1) << 38;                  // of rows: a tensor map's stride in bytes stays below 2^40
 bigcn_status check_rows(bigcn_ctx* ctx, const char* name, const void* p, int32_t type, int64_t n, int32_t d, int64_t ld)
 {
     const bigcn_status st = check_type(ctx, name, type);
     if (st != BIGCN_OK) return st;
-    if (n < 0 || n >= kMaxRows || d < 1 || ld < d) return fail(ctx, BIGCN_ERR_SHAPE, "%s: n=%lld d=%d ld=%lld", name, (long long)n, d, (long long)ld);
+    if (n < 0 || n >= kMaxRows || d < 1 || ld < d || ld >= kMaxLd) return fail(ctx, BIGCN_ERR_SHAPE, "%s: n=%lld d=%d ld=%lld", name, (long long)n, d, (long long)ld);
     if (d > BIGCN_MAX_D_IN) return fail(ctx, BIGCN_ERR_UNSUPPORTED, "%s: rows of %d > %d are not supported", name, d, BIGCN_MAX_D_IN);
     if (n > 0 && !p) return fail(ctx, BIGCN_ERR_NULL, "%s is null", name);
     if (!aligned(p, type == BIGCN_F32 ? 4 : 2)) return fail(ctx, BIGCN_ERR_ALIGN, "%s is not aligned to its elements", name);
@@ -204,7 +205,7 @@ bigcn_status check_rows(bigcn_ctx* ctx, const char* name, const void* p, int32_t
 // 8-bit rows and their scales.
 bigcn_status check_quantized(bigcn_ctx* ctx, const char* name, const void* q, int64_t n, int32_t d, int64_t ldq, const float* scale)
 {
-    if (n < 0 || n >= kMaxRows || d < 1 || ldq < d) return fail(ctx, BIGCN_ERR_SHAPE, "%s: n=%lld d=%d ld=%lld", name, (long long)n, d, (long long)ldq);
+    if (n < 0 || n >= kMaxRows || d < 1 || ldq < d || ldq >= kMaxLd) return fail(ctx, BIGCN_ERR_SHAPE, "%s: n=%lld d=%d ld=%lld", name, (long long)n, d, (long long)ldq);
     if (d > BIGCN_MAX_D_IN) return fail(ctx, BIGCN_ERR_UNSUPPORTED, "%s: rows of %d > %d are not supported", name, d, BIGCN_MAX_D_IN);
     if (n > 0 && (!q || !scale)) return fail(ctx, BIGCN_ERR_NULL, "%s or its scales are null", name);
     if (ldq % 16 != 0 || !aligned(q, 16)) return fail(ctx, BIGCN_ERR_ALIGN, "%s: rows must start on 16-byte boundaries (ld=%lld)", name, (long long)ldq);

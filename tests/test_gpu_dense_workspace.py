@@ -77,3 +77,24 @@ def test_layer_norm_backward(ctx, n, d):
     ws = exactly(ctx, need)
     assert all(torch.equal(a, b) for a, b in zip(ctx.layer_norm_backward(g, x, mean, rstd), want))
     assert left(ctx, ws, need)
+
+
+def test_leading_dimensions_that_no_tensor_map_holds_are_refused(ctx):
+    """One row has no next one, so any leading dimension could be given for it; the products' maps take none of 2^40 bytes."""
+    from paper_2210_13149_b200 import binding as B
+    x, W = torch.randn((1, 64), device="cuda").bfloat16(), torch.randn((8, 64), device="cuda").bfloat16()
+    y, out = torch.zeros(1, dtype=torch.int64, device="cuda"), torch.zeros(2, device="cuda")
+    q, s = ctx.quantize_rows(W)
+    ctx._scratch(1 << 20)
+    before = ctx.launch_count()
+    far = 1 << 38
+    P = B._ptr
+    for status in (ctx.lib.bigcn_class_loss(ctx.h, P(x), P(W), 1, 1, 64, 8, far, 64, P(y), P(out), P(out[1:])),
+                   ctx.lib.bigcn_class_loss(ctx.h, P(x), P(W), 1, 1, 64, 1, 64, far, P(y), P(out), P(out[1:])),
+                   ctx.lib.bigcn_quantized_product(ctx.h, P(q), 3, P(s), 1, 64, far, P(q), 64, P(s), 8, P(out), 0, 8),
+                   ctx.lib.bigcn_quantized_product(ctx.h, P(x), 1, None, 1, 64, 64, P(q), far, P(s), 1, P(out), 0, 1)):
+        assert status != 0
+        with pytest.raises(B.BigcnError):
+            ctx._check(status)
+    assert ctx.launch_count() == before
+    ctx.sync_check()

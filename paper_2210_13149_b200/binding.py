@@ -136,12 +136,6 @@ def packed_stride_words(length: int) -> int:
     return int(load().bigcn_packed_stride_words(int(length)))
 
 
-def _dense(rows: int, cols: int, dtype: torch.dtype, device: torch.device) -> torch.Tensor:
-    if cols == 0:
-        return torch.empty_strided((rows,), (1,), dtype=dtype, device=device)
-    return torch.empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device)
-
-
 def _addr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
@@ -493,16 +487,17 @@ class BiGCN:
             self._captured.append(self.workspace)
 
     def _outs(self, *wanted, used=()):
-        """Outputs' memory, in the order of the context's stream: (rows, columns or 0 for a vector, dtype) each, or None.  Where another stream is
+        """Outputs' memory, in the order of the context's stream: (size, stride, dtype) each, or None.  Where another stream is
         current, neither the call's inputs (`used`) nor its outputs are given away while the other of the two streams works with them."""
-        if torch._C._cuda_getCurrentRawStream(self.device.index) == self._raw_stream:
-            return [_dense(*w, self.device) if w else None for w in wanted]
+        empty, device = torch.empty_strided, self.device
+        if torch._C._cuda_getCurrentRawStream(device.index) == self._raw_stream:
+            return [empty(w[0], w[1], dtype=w[2], device=device) if w else None for w in wanted]
         now = torch.cuda.current_stream(self.device)
         for t in used:
             if t is not None:
                 t.record_stream(self.stream)
         with torch.cuda.stream(self.stream):
-            outs = [_dense(*w, self.device) if w else None for w in wanted]
+            outs = [empty(w[0], w[1], dtype=w[2], device=device) if w else None for w in wanted]
         for t in outs:
             if t is not None:
                 t.record_stream(now)
@@ -518,7 +513,7 @@ class BiGCN:
         out_dtype = X.dtype if out_dtype is None else out_dtype
         if out_dtype not in (torch.float32, torch.bfloat16, torch.float16):
             raise ValueError("layer_norm: no output of type %s" % out_dtype)
-        Y, mean, rstd = self._outs((n, d, out_dtype), (n, 0, torch.float32), (n, 0, torch.float32), used=(X, gain, offset))
+        Y, mean, rstd = self._outs(((n, d), (d, 1), out_dtype), ((n,), (1,), torch.float32), ((n,), (1,), torch.float32), used=(X, gain, offset))
         self._check(self.lib.bigcn_layer_norm(self.h, _addr(X), TYPES[X.dtype], n, d, ldx, _addr(gain), _addr(offset), eps, _addr(Y),
                                               TYPES[out_dtype], d, _addr(mean), _addr(rstd)))
         return Y, mean, rstd
@@ -536,7 +531,7 @@ class BiGCN:
         if out_dtype not in (torch.float32, torch.bfloat16, torch.float16):
             raise ValueError("layer_norm_backward: no output of type %s" % out_dtype)
         self._scratch(_sizes("bigcn_layer_norm_workspace_bytes", d))
-        g_x, g_gain, g_offset = self._outs((n, d, out_dtype), (d, 0, torch.float32), (d, 0, torch.float32), used=(g_y, X, mean, rstd, gain))
+        g_x, g_gain, g_offset = self._outs(((n, d), (d, 1), out_dtype), ((d,), (1,), torch.float32), ((d,), (1,), torch.float32), used=(g_y, X, mean, rstd, gain))
         self._check(self.lib.bigcn_layer_norm_backward(
             self.h, _addr(g_y), TYPES[g_y.dtype], ldg, _addr(X), TYPES[X.dtype], ldx, n, d, _addr(gain), _addr(mean), _addr(rstd),
             _addr(g_x), TYPES[out_dtype], d, _addr(g_gain), _addr(g_offset)))
@@ -554,7 +549,7 @@ class BiGCN:
         A negative label marks a row that takes no part."""
         ldx, ldw, n, d, classes = self._class_rows(X, W, labels)
         self._scratch(_sizes("bigcn_class_loss_workspace_bytes", n, d, classes, 0))
-        loss, lse = self._outs((n, 0, torch.float32), (n, 0, torch.float32), used=(X, W, labels))
+        loss, lse = self._outs(((n,), (1,), torch.float32), ((n,), (1,), torch.float32), used=(X, W, labels))
         self._check(self.lib.bigcn_class_loss(self.h, _addr(X), _addr(W), TYPES[X.dtype], n, d, classes, ldx, ldw, _addr(labels), _addr(loss), _addr(lse)))
         return loss, lse
 
@@ -565,7 +560,7 @@ class BiGCN:
         self._vector("lse", lse, n)
         self._vector("g_loss", g_loss, n)
         self._scratch(_sizes("bigcn_class_loss_workspace_bytes", n, d, classes, 1))
-        g_x, g_w = self._outs((n, d, X.dtype) if want_g_x else None, (classes, d, X.dtype) if want_g_w else None, used=(X, W, labels, lse, g_loss))
+        g_x, g_w = self._outs(((n, d), (d, 1), X.dtype) if want_g_x else None, ((classes, d), (d, 1), X.dtype) if want_g_w else None, used=(X, W, labels, lse, g_loss))
         self._check(self.lib.bigcn_class_loss_backward(self.h, _addr(X), _addr(W), TYPES[X.dtype], n, d, classes, ldx, ldw, _addr(labels), _addr(lse),
                                                        _addr(g_loss), _addr(g_x), d, _addr(g_w), d))
         return g_x, g_w
@@ -575,7 +570,7 @@ class BiGCN:
         ldx = self._rows("X", X)
         n, d = X.shape
         ldq = (d + 15) // 16 * 16
-        q, scale = self._outs((n, ldq, torch.int8), (n, 0, torch.float32), used=(X,))
+        q, scale = self._outs(((n, ldq), (ldq, 1), torch.int8), ((n,), (1,), torch.float32), used=(X,))
         if ldq != d:
             with torch.cuda.stream(self.stream):
                 q[:, d:] = 0
@@ -609,7 +604,7 @@ class BiGCN:
         self._vector("s_w", s_w, m)
         if out_dtype not in (torch.float32, torch.bfloat16, torch.float16):
             raise ValueError("quantized_product: no output of type %s" % out_dtype)
-        out, = self._outs((n, m, out_dtype), used=(X, s_x, q_w, s_w))
+        out, = self._outs(((n, m), (m, 1), out_dtype), used=(X, s_x, q_w, s_w))
         self._check(self.lib.bigcn_quantized_product(self.h, _addr(X), TYPES[X.dtype], _addr(s_x), n, d, ldx, _addr(q_w), ldqw, _addr(s_w), m,
                                                      _addr(out), TYPES[out_dtype], m))
         return out

@@ -123,13 +123,13 @@ __global__ void __launch_bounds__(1024) list_labels_kernel(const ListArgs a, con
     __shared__ int total;
     const int block = kGather ? 0 : blockIdx.x;
     const bool write = !kGather || blockIdx.x == 0;
-    int before = 0;
-    for (int b = threadIdx.x; b < block; b += 1024) before += __ldg(a.counts + b);
-    before = !kGather && gridDim.x > 1 ? block_sum(before, slot) : 0;
     const int64_t at = ((int64_t)block * 1024 + threadIdx.x) * 4;
     int64_t v[4];
     bool in[4];
-    read_labels(a.labels, a.n, a.classes, at, v, in);
+    read_labels(a.labels, a.n, a.classes, at, v, in);         // (on their way while the blocks before are summed)
+    int before = 0;
+    for (int b = threadIdx.x; b < block; b += 1024) before += __ldg(a.counts + b);
+    before = !kGather && gridDim.x > 1 ? block_sum(before, slot) : 0;
     const int mine = in[0] + in[1] + in[2] + in[3], lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int upto = mine;
 #pragma unroll
@@ -140,8 +140,7 @@ __global__ void __launch_bounds__(1024) list_labels_kernel(const ListArgs a, con
     __syncthreads();
     if (lane == 31) slot[warp] = upto;
     __syncthreads();
-    int base = before;
-    for (int w = 0; w < warp; ++w) base += slot[w];
+    const int base = before + __reduce_add_sync(0xffffffffu, lane < warp ? slot[lane] : 0);
     int next = base + upto - mine, places[4];
     float none[4];
     unsigned top = 0u;

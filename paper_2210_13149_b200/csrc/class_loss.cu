@@ -524,9 +524,9 @@ struct Store {
                         }
                     });
                 } else {
-                    gemm::write_strip_elements<uint16_t>(p.strip, w, [&](int r, int e, uint16_t bits) {
+                    gemm::write_strip_elements(p.strip, w, [&](int r, uint16_t bits) {
                         const int64_t to_row = __shfl_sync(0xffffffffu, mapped, r);
-                        if (p.row + r < p.rows && col + e < sh.n) a.out[to_row * a.ldo + col + e] = bits;
+                        if (p.row + r < p.rows && col + lane < sh.n) a.out[to_row * a.ldo + col + lane] = bits;
                     });
                 }
             }

@@ -186,9 +186,7 @@ struct ScaledOut {
         const int lane = threadIdx.x & 31;
         // the warp's class scales are read by all lanes at once below: from L1 by then
         if (lane < gemm::part_cols(BN) / 32 && p.col + 32 * lane < sh.n) asm volatile("prefetch.global.L1 [%0];\n" ::"l"(a.s_w + p.col + 32 * lane));
-        constexpr int kElts = 16 / type_bytes(TYPE), kStrips = type_bytes(TYPE) / 2;      // of a piece; 32 columns are one strip or two
         using T = typename Elt<TYPE>::T;
-        using Bits = typename std::conditional<sizeof(T) == 4, uint32_t, uint16_t>::type;
         T* const at = static_cast<T*>(a.out) + (int64_t)p.row * a.ldo + p.col;
         const bool rows_there = p.row + 32 <= p.rows;
         gemm::each_chunk<BN>(p, sh.n, done, [&](int c, uint32_t (&v)[32]) {
@@ -206,38 +204,70 @@ struct ScaledOut {
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] = __float_as_uint((float)(int)v[i] * (sx * (i < left ? __ldg(a.s_w + p.col + c + i) : 0.f)));
             }
+            T* const to = at + c;
+            if constexpr (TYPE == BIGCN_F32) {
+                if (a.whole && rows_there && left >= 32) {
+                    float* e = to + (int64_t)(lane >> 3) * a.ldo + (lane & 7) * 4;
+                    gemm::write_wide(p.strip, v, [&](int, int, const uint4& q) {
+                        *reinterpret_cast<uint4*>(e) = q;
+                        e += 4 * a.ldo;
+                    });
+                } else if (a.whole) {
+                    const auto put = [&](int r, int piece, const uint4& q) {
+                        const int there = left - 4 * piece;
+                        if (p.row + r >= p.rows || there <= 0) return;
+                        float* e = to + r * a.ldo + 4 * piece;
+                        if (there >= 4) {
+                            *reinterpret_cast<uint4*>(e) = q;
+                        } else {
+                            const float* from = reinterpret_cast<const float*>(&q);
 #pragma unroll
-            for (int h = 0; h < kStrips; ++h) {
+                            for (int i = 0; i < 4; ++i)
+                                if (i < there) e[i] = from[i];
+                        }
+                    };
+                    if (left > 16) {
+                        gemm::write_wide(p.strip, v, put);
+                    } else {
+                        uint32_t w[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) w[i] = v[i];
+                        gemm::write_strip(p.strip, w, put);
+                    }
+                } else {
+                    uint32_t* e = reinterpret_cast<uint32_t*>(to) + lane;
+                    const int rows = lane < left ? p.rows - p.row : 0;
+                    gemm::write_wide_elements(p.strip, v, [&](int r, uint32_t q) {
+                        if (r < rows) *e = q;
+                        e += a.ldo;
+                    });
+                }
+            } else {
                 uint32_t w[16];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    if constexpr (TYPE == BIGCN_F32) w[i] = v[16 * h + i];
-                    else w[i] = pack2<TYPE>(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
-                }
-                T* const to = at + c + 16 * h;
+                for (int i = 0; i < 16; ++i) w[i] = pack2<TYPE>(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
                 if (a.whole && rows_there && left >= 32) {
-                    gemm::write_strip_whole(p.strip, w, reinterpret_cast<char*>(to + (int64_t)(lane >> 2) * a.ldo + (lane & 3) * kElts), 8 * a.ldo * (int64_t)sizeof(T));
+                    gemm::write_strip_whole(p.strip, w, reinterpret_cast<char*>(to + (int64_t)(lane >> 2) * a.ldo + (lane & 3) * 8), 16 * a.ldo);
                 } else if (a.whole) {
                     gemm::write_strip(p.strip, w, [&](int r, int piece, const uint4& q) {
-                        const int there = left - 16 * h - piece * kElts;
+                        const int there = left - piece * 8;
                         if (p.row + r >= p.rows || there <= 0) return;
-                        T* e = to + r * a.ldo + piece * kElts;
-                        if (there >= kElts) {
+                        T* e = to + r * a.ldo + piece * 8;
+                        if (there >= 8) {
                             *reinterpret_cast<uint4*>(e) = q;
                         } else {
                             const T* from = reinterpret_cast<const T*>(&q);
 #pragma unroll
-                            for (int i = 0; i < kElts; ++i)
+                            for (int i = 0; i < 8; ++i)
                                 if (i < there) e[i] = from[i];
                         }
                     });
                 } else {
-                    constexpr int kPerRow = 64 / sizeof(T);
-                    Bits* e = reinterpret_cast<Bits*>(to) + (int64_t)(lane / kPerRow) * a.ldo + lane % kPerRow;
-                    const bool mine = lane % kPerRow < left - 16 * h;
-                    gemm::write_strip_elements<Bits>(p.strip, w, [&](int r, int, Bits q) {
-                        if (mine && p.row + r < p.rows) *e = q;
-                        e += (32 / kPerRow) * a.ldo;
+                    uint16_t* e = reinterpret_cast<uint16_t*>(to) + lane;
+                    const int rows = lane < left ? p.rows - p.row : 0;
+                    gemm::write_strip_elements(p.strip, w, [&](int r, uint16_t q) {
+                        if (r < rows) *e = q;
+                        e += a.ldo;
                     });
                 }
             }

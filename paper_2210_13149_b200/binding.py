@@ -268,11 +268,28 @@ class BiGCN:
         arr = (_i32 * len(dims))(*[int(d) for d in dims])
         return int(self.lib.bigcn_workspace_bytes(n, nnz, arr, len(dims) - 1, int(host_io)))
 
+    def _capturing(self) -> bool:
+        """Whether the context's own stream is being captured, whichever stream is current."""
+        if torch._C._cuda_getCurrentRawStream(self.device.index) == self._raw_stream:
+            return torch._C._cuda_isCurrentStreamCapturing()
+        with torch.cuda.stream(self.stream):
+            return torch._C._cuda_isCurrentStreamCapturing()
+
     def ensure_workspace(self, nbytes: int):
+        """Workspace for the call that follows, in the order of the context's own stream.  One that a call under capture uses stays alive with
+        the context, also where a later call (of the same capture or not) needs a larger one: the graph's kernels keep its address."""
+        capturing = self._capturing()
         if self.workspace is None or self.workspace.numel() < nbytes:
+            if self.workspace is not None and not capturing:
+                self.workspace.record_stream(self.stream)       # it may have been allocated while another stream was current
             self.workspace = None
-            self.workspace = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=self.device)
+            with torch.cuda.stream(self.stream):
+                self.workspace = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=self.device)
             self._check(self.lib.bigcn_set_workspace(self.h, _ptr(self.workspace), self.workspace.numel()))
+        if capturing and not any(w is self.workspace for w in self._captured):
+            self._captured.append(self.workspace)
+
+    _scratch = ensure_workspace
 
     # -- the ABI calls
     def normalize_adjacency(self, rowptr_A: torch.Tensor, colidx_A: torch.Tensor) -> Graph:
@@ -475,16 +492,6 @@ class BiGCN:
     def _vector(self, name: str, t: Optional[torch.Tensor], length: int, dtype=torch.float32):
         if t is not None and (t.shape != (length,) or t.dtype != dtype or t.device != self.device or (length > 1 and t.stride(0) != 1)):
             raise ValueError("%s: %d contiguous elements of %s on %s are wanted" % (name, length, dtype, self.device))
-
-    def _scratch(self, nbytes: int):
-        """Workspace on the context's own stream.  One that a graph capture has used stays alive with the context."""
-        if self.workspace is None or self.workspace.numel() < nbytes:
-            if self.workspace is not None and not torch._C._cuda_isCurrentStreamCapturing():
-                self.workspace.record_stream(self.stream)       # it may have been allocated while another stream was current
-            with torch.cuda.stream(self.stream):
-                self.ensure_workspace(nbytes)
-        if torch._C._cuda_isCurrentStreamCapturing() and not any(w is self.workspace for w in self._captured):
-            self._captured.append(self.workspace)
 
     def _outs(self, *wanted, used=()):
         """Outputs' memory, in the order of the context's stream: (size, stride, dtype) each, or None.  Where another stream is

@@ -401,8 +401,9 @@ bigcn_status bigcn_layer_norm_backward(bigcn_ctx* ctx, const void* g_y, int32_t 
  *   G_ik = (exp(z_ik - lse_i) - [k = label(i)]) g_loss_i,  g_x = G w,  g_w = G^T x,
  * g_x [n x ldgx] and g_w [classes x ldgw] in the operands' type, nullable each.  z is computed again and G held a piece of
  * rows and classes at a time, in the operands' type (in fp16 without g_loss, which comes in in fp32 for g_x and by way of
- * rows of x times g_loss_i / max |g_loss| for g_w); sums in fp32.  Rows without a label get zero.  The same call gives the
- * same bits.  Needs bigcn_class_loss_workspace_bytes(n, d, classes, 1) of workspace. */
+ * rows of x times g_loss_i / max |g_loss| for g_w, rounded to fp16 once more; the two share the exponents that a g_loss_i
+ * far below the largest needs, so that it keeps fp16's digits down to about 2^-30 of that); sums in fp32.  Rows without a label get zero.
+ * The same call gives the same bits.  Needs bigcn_class_loss_workspace_bytes(n, d, classes, 1) of workspace. */
 size_t bigcn_class_loss_workspace_bytes(int64_t n, int32_t d, int32_t classes, int32_t backward);
 bigcn_status bigcn_class_loss(bigcn_ctx* ctx, const void* x, const void* w, int32_t type, int64_t n, int32_t d, int32_t classes,
                               int64_t ldx, int64_t ldw, const int64_t* labels, float* loss, float* lse);

@@ -10,7 +10,8 @@
 // rounding besides the outputs' own: a relative error of half a step for each term of sums whose terms' errors are independent,
 // which is the size of the output's rounding.  In bf16 g_i is part of G.  fp16 has no exponents for a g_i of, say, 1 / n times a small
 // probability, so there G holds (exp(z - lse) - [..]) 2^14 (down to 2^-28 in normal numbers), rows of g_x are multiplied by g_i 2^-14 in fp32, and X enters
-// g_w as rows times g_i / max |g| (one more rounding, none where all g_i are the same), the rest in fp32.
+// g_w as rows times g_i / max |g| (one more rounding, none where all g_i are the same), the rest in fp32.  Nor has fp16 the exponents for a g_i far below
+// the largest: such a row of X goes up by a power of two 2^b and its row of G down by it, see lift_of().
 //
 // Rows without a label take no part: the labelled ones are listed first and, unless that is all of them, copied together, so that what
 // the others hold (NaN, infinities) reaches nothing and their work is not done.  How many there are is known on the GPU only; the
@@ -104,10 +105,23 @@ struct GatherArgs {
     int64_t ldgx;
     bool g_whole;
     int span;                // rows of a warp at a time, at most 32
-    const float* g_loss;     // fp16's gradients: of every row,
+    const float* g_loss;     // fp16's gradients (else null): of every row,
     const float* top;        // and the largest magnitude among the labelled ones;
-    uint16_t* scaled;        // rows times g / top, as `to` lies (nullable)
+    float* lift;             // of the labelled rows: what G is multiplied by, kHalfScale 2^-b
+    float* undo;             // g divided by it
+    uint16_t* scaled;        // rows times g / top 2^b, as `to` lies (nullable: g_w is not wanted)
 };
+constexpr float kHalfScale = 16384.f;         // fp16's G is this much larger
+
+// The power b of a row whose g is `ratio` of the largest: X enters g_w as x ratio 2^b and G as G 2^(14 - b).  Of fp16's 14 exponents below 1 in
+// normal numbers rows of X give up five (x ratio 2^b stays within [2^-6, 2^-5) of x where x ratio would lie below), the others are left for small
+// values of x; G, whose largest is 2^14 without b, gives up 18 at most, which leaves it 10.  So a ratio of 2^-30 still has x near 1 in normal
+// numbers; without b they ended at 2^-14, and from 2^-25 on nothing of such a row was left.
+__device__ __forceinline__ int lift_of(float ratio)
+{
+    const float r = fabsf(ratio);
+    return r > 0.f && r < 1.f ? min(18, max(0, -5 - (ilogbf(r) + 1))) : 0;
+}
 // How rows of x lie: on 16-byte boundaries, up to 32 words of 16 bytes or more; on 4-byte boundaries; anywhere.
 enum Lie : int { kShort = 0, kLong = 1, kPairs = 2, kAnywhere = 3 };
 template <int LIE>
@@ -238,15 +252,22 @@ __device__ void gather_rows(const GatherArgs& a, int count, const int* places, i
 {
     const int lane = threadIdx.x & 31;
     const int64_t end = ((int64_t)count + 127) / 128 * 128;
-    if (a.scaled) {
+    if (a.lift) {
         for (int64_t row = first; row < a.n; row += warps) {
             const int p = places[row];
             if (p < 0) continue;
-            const float ratio = top > 0.f ? __ldg(a.g_loss + row) / top : 0.f;
+            const float g = __ldg(a.g_loss + row), ratio = top > 0.f ? g / top : 0.f;
+            const int b = lift_of(ratio);
+            if (lane == 0) {
+                a.lift[p] = ldexpf(kHalfScale, -b);
+                a.undo[p] = ldexpf(g, b) * (1.f / kHalfScale);
+            }
+            if (!a.scaled) continue;
+            const float factor = ldexpf(ratio, b);
             for (int i = lane; i < a.d; i += 32)
-                a.scaled[(int64_t)p * a.ldt + i] = __half_as_ushort(__float2half_rn(__half2float(__ushort_as_half(__ldg(a.x + row * a.ldx + i))) * ratio));
+                a.scaled[(int64_t)p * a.ldt + i] = __half_as_ushort(__float2half_rn(__half2float(__ushort_as_half(__ldg(a.x + row * a.ldx + i))) * factor));
         }
-        for (int64_t row = count + first; row < end; row += warps)
+        for (int64_t row = count + first; a.scaled && row < end; row += warps)
             for (int i = lane; i < a.d; i += 32) a.scaled[row * a.ldt + i] = 0;
     }
     if (a.whole && count == a.n) return;
@@ -289,7 +310,7 @@ template <int LIE>
 __global__ void __launch_bounds__(256, LIE == kShort ? 8 : 6) gather_rows_kernel(const GatherArgs a)
 {
     pdl_enter();
-    gather_rows<LIE>(a, __ldg(a.count), a.place, (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), (int64_t)gridDim.x * 8, a.scaled ? __ldg(a.top) : 0.f);
+    gather_rows<LIE>(a, __ldg(a.count), a.place, (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), (int64_t)gridDim.x * 8, a.lift ? __ldg(a.top) : 0.f);
 }
 
 // Rows copied to 16-byte boundaries (a class matrix that does not start its rows there), in words of T where the rows allow it.
@@ -393,15 +414,13 @@ struct SumExp {
     }
 };
 
-constexpr float kHalfScale = 16384.f;         // fp16's G is this much larger
-
 // G of a tile, rounded to the operands' type; zero past the last class and the last row, which pads the depth of what reads it.
 template <int TYPE>
 struct Gradient {
     struct Args {
         const int* label;
         const float* lse;    // of the labelled rows
-        const float* g_loss;
+        const float* weight; // of the labelled rows: bf16 g_loss, fp16 kHalfScale 2^-b
         int first_class;     // of the piece
         uint16_t* g;
         int64_t ldg;         // a multiple of 64
@@ -415,7 +434,7 @@ struct Gradient {
     static __device__ __forceinline__ Row row(const Args& a, int row, int rows)
     {
         if (row >= rows) return {INT_MIN, 0.f, 0.f};
-        return {__ldg(a.label + row), __ldg(a.lse + row), __ldg(a.g_loss + row)};
+        return {__ldg(a.label + row), __ldg(a.lse + row), __ldg(a.weight + row)};
     }
     template <int BN, class Done>
     static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit&, const gemm::Part& p, const Row& of_row, const Done& done)
@@ -423,7 +442,7 @@ struct Gradient {
         if (p.row >= (p.rows + 127) / 128 * 128) return done();       // a pair's second block past the last row: G has no such rows
         const bool there = p.row + (int)(threadIdx.x & 31) < p.rows;
         const int label = of_row.label >= a.first_class + p.col ? of_row.label - a.first_class - p.col : INT_MIN;
-        const float lse = of_row.lse, weight = TYPE == BIGCN_F16 ? kHalfScale : of_row.weight;
+        const float lse = of_row.lse, weight = of_row.weight;
         gemm::each_chunk<BN>(p, (int)a.ldg, done, [&](int c, uint32_t (&v)[32]) {
             const int left = sh.n - (p.col + c);
             float f[32];
@@ -687,7 +706,7 @@ struct Plan {
     int64_t pitch;                            // of fp32 parts
     size_t bytes;
     // offsets
-    size_t kept, label, place, count, counts, lse, g_loss, x, w, scaled, top, at, part, g, px, pw;
+    size_t kept, label, place, count, counts, lse, g_loss, lift, undo, x, w, scaled, top, at, part, g, px, pw;
 };
 
 Plan make_plan(int64_t n, int d, int classes, bool backward, bool half)
@@ -711,6 +730,8 @@ Plan make_plan(int64_t n, int d, int classes, bool backward, bool half)
     p.w = take((size_t)classes * p.ldt * 2);                    // (the class matrix laid on boundaries, where it is not)
     if (backward && half) {
         p.scaled = take((size_t)p.n_pad * p.ldt * 2);
+        p.lift = take((size_t)p.n_pad * 4);
+        p.undo = take((size_t)p.n_pad * 4);
         p.top = take(sizeof(unsigned));
     }
     if (!backward) {
@@ -752,7 +773,7 @@ struct Operands {
 
 // Lists the labelled rows, copies them together where that is needed, and lays the class matrix on 16-byte boundaries.
 cudaError_t prepare(cudaStream_t s, const Plan& p, char* ws, int type, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n, int d, int classes,
-                    const int64_t* labels, float* loss, float* lse, const float* of_lse, const float* of_g_loss, void* g_x, int64_t ldgx, int tries, Operands* o, int* launches)
+                    const int64_t* labels, float* loss, float* lse, const float* of_lse, const float* of_g_loss, void* g_x, int64_t ldgx, bool want_g_w, int tries, Operands* o, int* launches)
 {
     int* counts = reinterpret_cast<int*>(ws + p.counts);
     unsigned* top = type == BIGCN_F16 && of_g_loss ? reinterpret_cast<unsigned*>(ws + p.top) : nullptr;
@@ -775,7 +796,8 @@ cudaError_t prepare(cudaStream_t s, const Plan& p, char* ws, int type, const voi
     const int span = (int)ceil_div(n, warps * ceil_div(n, warps * 32));
     const GatherArgs gather = {static_cast<const uint16_t*>(x), ldx, n, d, o->x_whole, list.place, list.count, reinterpret_cast<uint16_t*>(ws + p.x), p.ldt,
                                static_cast<uint16_t*>(g_x), ldgx, rows_whole(g_x, ldgx, BIGCN_BF16, 8), span, of_g_loss,
-                               reinterpret_cast<const float*>(top), top ? reinterpret_cast<uint16_t*>(ws + p.scaled) : nullptr};
+                               reinterpret_cast<const float*>(top), top ? reinterpret_cast<float*>(ws + p.lift) : nullptr, top ? reinterpret_cast<float*>(ws + p.undo) : nullptr,
+                               top && want_g_w ? reinterpret_cast<uint16_t*>(ws + p.scaled) : nullptr};
     ++*launches;
     const int lie = o->x_whole ? (d <= 256 ? kShort : kLong) : rows_whole(x, ldx, BIGCN_BF16, 2) ? kPairs : kAnywhere;
     if (n <= kScan) {
@@ -870,7 +892,7 @@ cudaError_t backward_as(cudaStream_t s, const void* x, int64_t ldx, const void* 
     constexpr bool half = TYPE == BIGCN_F16;
     const Plan p = make_plan(n, d, classes, true, half);
     Operands o;
-    e = prepare(s, p, ws, type, x, ldx, w, ldw, n, d, classes, labels, nullptr, nullptr, lse, g_loss, g_x, ldgx, tries, &o, launches);
+    e = prepare(s, p, ws, type, x, ldx, w, ldw, n, d, classes, labels, nullptr, nullptr, lse, g_loss, g_x, ldgx, g_w != nullptr, tries, &o, launches);
     const int* count = reinterpret_cast<const int*>(ws + p.count);
     const int* kept = reinterpret_cast<const int*>(ws + p.kept);
     const int* label = reinterpret_cast<const int*>(ws + p.label);
@@ -883,7 +905,7 @@ cudaError_t backward_as(cudaStream_t s, const void* x, int64_t ldx, const void* 
         for (int r = 0; r < p.row_pieces && e == cudaSuccess; ++r) {
             const int64_t first = r * p.rows, rows = std::min(p.rows, n - first);
             if (rows <= 0) break;
-            const typename Gradient<TYPE>::Args ga = {label + first, reinterpret_cast<const float*>(ws + p.lse) + first, reinterpret_cast<const float*>(ws + p.g_loss) + first, (int)first_class, g, ldg};
+            const typename Gradient<TYPE>::Args ga = {label + first, reinterpret_cast<const float*>(ws + p.lse) + first, reinterpret_cast<const float*>(ws + (half ? p.lift : p.g_loss)) + first, (int)first_class, g, ldg};
             e = pick_logits<Gradient<TYPE>>(s, tile_cols(here), p, o, n, d, here, first, rows, first_class, count, type, ga, launches);
             if (e != cudaSuccess) break;
             gemm::Shape sh;
@@ -905,7 +927,7 @@ cudaError_t backward_as(cudaStream_t s, const void* x, int64_t ldx, const void* 
                 sh.splits = p.splits_x;
                 const typename Store<TYPE>::Args args = {kept + first, static_cast<uint16_t*>(g_x), ldgx, rows_whole(g_x, ldgx, BIGCN_BF16, 8),
                                           parts_x ? reinterpret_cast<float*>(ws + p.px) + first * p.pitch : nullptr, p.pitch, p.n_pad * p.pitch, c > 0,
-                                          half ? reinterpret_cast<const float*>(ws + p.g_loss) + first : nullptr, nullptr, half ? 1.f / kHalfScale : 1.f};
+                                          half ? reinterpret_cast<const float*>(ws + p.undo) + first : nullptr, nullptr, 1.f};
                 ++*launches;
                 e = launch_gradient<TYPE, false>(s, p.bn_d, mg, mw, mw, sh, args);
                 if (e == cudaSuccess && parts_x && c == p.col_pieces - 1) {
@@ -963,7 +985,7 @@ cudaError_t launch_class_loss(cudaStream_t s, int type, const void* x, int64_t l
     cudaError_t e;
     const Plan p = make_plan(n, d, classes, false, false);
     Operands o;
-    e = prepare(s, p, ws, type, x, ldx, w, ldw, n, d, classes, labels, loss, lse, nullptr, nullptr, nullptr, 0, tries, &o, launches);
+    e = prepare(s, p, ws, type, x, ldx, w, ldw, n, d, classes, labels, loss, lse, nullptr, nullptr, nullptr, 0, false, tries, &o, launches);
     const int* count = reinterpret_cast<const int*>(ws + p.count);
     const int* kept = reinterpret_cast<const int*>(ws + p.kept);
     float* at = reinterpret_cast<float*>(ws + p.at);

@@ -12,6 +12,7 @@
 // Lanes read words of 16 bytes where the rows they read start on their boundaries, and otherwise words of 4, 2 or 1 elements, whichever the rows
 // allow (the backward pass, with two types to read, then looks them up); they store what the output's rows allow.
 #include <algorithm>
+#include <cfloat>
 
 #include "dense_types.cuh"
 
@@ -340,7 +341,7 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads, BackLayout<GTYP
             }
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                // (where there is no element x and g are 0: its xhat adds nothing, and nothing is kept of it)
+                // (where there is no element x and g are 0: its xhat adds nothing while it is a number, and nothing is kept of it)
                 xh[k][i] = (xh[k][i] - mu) * r;
                 const float gi = gv[k][i];
                 if constexpr (kShared) {
@@ -356,6 +357,14 @@ __global__ void __launch_bounds__(LANES > 32 ? LANES : kThreads, BackLayout<GTYP
                 sums[0] += gv[k][i];
                 sums[1] = fmaf(gv[k][i], xh[k][i], sums[1]);
             }
+        }
+        if (!(fabsf(mu * r) <= FLT_MAX)) {       // 0 - mean, times rstd, is no number then: the sum of what is there
+            sums[1] = 0.f;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if ((k * LANES + lane) * V + i < a.d) sums[1] = fmaf(gv[k][i], xh[k][i], sums[1]);
         }
         group_sum<LANES, 2>(sums, slots[trip & 1]);
         if (row < a.n) {

@@ -240,6 +240,14 @@ __device__ __forceinline__ void tmem_wait32(uint32_t (&v)[32])
                  :: "memory");
 }
 
+// one column, there when it returns
+__device__ __forceinline__ uint32_t tmem_ld1(uint32_t taddr)
+{
+    uint32_t v;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\ntcgen05.wait::ld.sync.aligned;\n" : "=r"(v) : "r"(taddr) : "memory");
+    return v;
+}
+
 // What an epilogue warp works with: warp w has lanes 32 (w & 3) .. + 31 of tensor memory (rows of the tile) and part_cols(BN) columns of it, its
 // `part` of the tile's; the four warps (or fewer) that share the rows are 4 apart, the first of them at `part` 0.
 struct Part {

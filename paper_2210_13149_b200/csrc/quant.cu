@@ -4,8 +4,9 @@
 //   out_ik = (sum_j q_ij qw_kj) s_i sw_k
 //
 // The integers are exact: the sum of 16,384 products of 127 stays below 2^31.  The three roundings of an output (the sum to fp32, and
-// two products) are fp32's, then one to the output's type.  The scales are multiplied first: a row with fp32's lowest value in it has a
-// scale of 2^121, which times the sum would overflow where the output does not.
+// two products) are fp32's, then one to the output's type.  The sum comes before the scales' product, which may leave fp32's range where the
+// output does not: two scales of 2^-75 lose the digits that a sum of 2^28 brings back, and a sum of 0 times infinity is no number.  The scale
+// of a row with fp32's lowest value in it, 2^121, times the sum would overflow likewise: see row_scale().
 #include <climits>
 #include <type_traits>
 
@@ -163,6 +164,20 @@ cudaError_t pick_quantize(cudaStream_t s, const QuantArgs& a, int* launches)
     return launch_quantize_as<TYPE, V, 1024, Q>(s, a, launches);
 }
 
+// A sum times a row's scale s and a class's t, in this order in every form of the product, so that all give the same bits.  The sum is below 2^28 and so times s
+// in range up to 2^99; of a larger s 2^-64 goes in first, which is 2^32 and more, so that no t loses digits either, and where that overflows without the
+// 2^64 that come last it does with them.
+__device__ __forceinline__ bool large_scale(float s) { return fabsf(s) >= 0x1p96f; }
+struct RowScale {
+    float s, last;
+};
+__device__ __forceinline__ RowScale row_scale(float s)
+{
+    const bool large = large_scale(s);
+    return {large ? s * 0x1p-64f : s, large ? 0x1p64f : 1.f};
+}
+__device__ __forceinline__ float scaled(int sum, const RowScale& r, float t) { return (float)sum * r.s * t * r.last; }
+
 // Epilogue: the sums times both scales, in the output's type.
 struct ScaledArgs {
     const float* s_x;
@@ -173,6 +188,29 @@ struct ScaledArgs {
     int64_t ldo;
     bool whole;              // rows of out on 16-byte boundaries
 };
+
+// A warp's part of a tile with a large scale of a row, a column at a time: so little code that the other tiles take no longer for it (with a function that
+// is called instead, 92 us for 85 at 3,269 x 64 times 34,624 classes in bf16).
+template <int TYPE>
+__device__ __forceinline__ void large_tile(const ScaledArgs& a, const gemm::Part& p, int cols, float s)
+{
+    const int row = p.row + (threadIdx.x & 31);
+    const RowScale scale = row_scale(s);
+    typename Elt<TYPE>::T* to = static_cast<typename Elt<TYPE>::T*>(a.out) + (int64_t)row * a.ldo + p.col;
+#pragma unroll 1
+    for (int c = 0; c < cols; ++c) {
+        const int sum = (int)gemm::tmem_ld1(p.acc + c);
+        if (row < p.rows) to[c] = from_float<TYPE>(scaled(sum, scale, __ldg(a.s_w + p.col + c)));
+        __syncwarp();
+    }
+}
+__device__ __forceinline__ void times(uint32_t (&v)[32], int i, const float4& w)
+{
+    v[i] = __float_as_uint(__uint_as_float(v[i]) * w.x);
+    v[i + 1] = __float_as_uint(__uint_as_float(v[i + 1]) * w.y);
+    v[i + 2] = __float_as_uint(__uint_as_float(v[i + 2]) * w.z);
+    v[i + 3] = __float_as_uint(__uint_as_float(v[i + 3]) * w.w);
+}
 template <int TYPE>
 struct ScaledOut {
     using Args = ScaledArgs;
@@ -183,6 +221,10 @@ struct ScaledOut {
     template <int BN, class Done>
     static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit&, const gemm::Part& p, const Row& sx, const Done& done)
     {
+        if (__any_sync(0xffffffffu, large_scale(sx))) {
+            large_tile<TYPE>(a, p, min(gemm::part_cols(BN), sh.n - p.col), sx);
+            return done();
+        }
         const int lane = threadIdx.x & 31;
         // the warp's class scales are read by all lanes at once below: from L1 by then
         if (lane < gemm::part_cols(BN) / 32 && p.col + 32 * lane < sh.n) asm volatile("prefetch.global.L1 [%0];\n" ::"l"(a.s_w + p.col + 32 * lane));
@@ -192,17 +234,28 @@ struct ScaledOut {
         gemm::each_chunk<BN>(p, sh.n, done, [&](int c, uint32_t (&v)[32]) {
             const int left = sh.n - (p.col + c);
             if (a.s_w_whole && left >= 32) {
+                const float4* from = reinterpret_cast<const float4*>(a.s_w + p.col + c);
+                if constexpr (TYPE == BIGCN_F32) {
+                    // all scales first (8,192 x 256 times 10,000 classes in us: fp32 90 so, 103 with a scale read where it is needed; 3,269 x 64 times 34,624, bf16: 90
+                    // and 86)
+                    float4 w[8];
 #pragma unroll
-                for (int i = 0; i < 32; i += 4) {
-                    const float4 w = __ldg(reinterpret_cast<const float4*>(a.s_w + p.col + c + i));
-                    v[i] = __float_as_uint((float)(int)v[i] * (sx * w.x));
-                    v[i + 1] = __float_as_uint((float)(int)v[i + 1] * (sx * w.y));
-                    v[i + 2] = __float_as_uint((float)(int)v[i + 2] * (sx * w.z));
-                    v[i + 3] = __float_as_uint((float)(int)v[i + 3] * (sx * w.w));
+                    for (int i = 0; i < 8; ++i) w[i] = __ldg(from + i);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = __float_as_uint((float)(int)v[i] * sx);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) times(v, 4 * i, w[i]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) v[4 * i + j] = __float_as_uint((float)(int)v[4 * i + j] * sx);
+                        times(v, 4 * i, __ldg(from + i));
+                    }
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = __float_as_uint((float)(int)v[i] * (sx * (i < left ? __ldg(a.s_w + p.col + c + i) : 0.f)));
+                for (int i = 0; i < 32; ++i) v[i] = __float_as_uint((float)(int)v[i] * sx * (i < left ? __ldg(a.s_w + p.col + c + i) : 0.f));
             }
             T* const to = at + c;
             if constexpr (TYPE == BIGCN_F32) {
@@ -286,14 +339,24 @@ struct ScaledAcross {
     template <int BN, class Done>
     static __device__ __forceinline__ void tile(const Args& a, const gemm::Shape& sh, const gemm::Unit&, const gemm::Part& p, const Row& sw, const Done& done)
     {
-        const int k = p.row + (threadIdx.x & 31);
+        static_assert(gemm::part_cols(BN) == 32, "a lane looks at the scale of one row of x");
+        const int lane = threadIdx.x & 31, k = p.row + lane, cols = min(32, sh.n - p.col);
+        if (__any_sync(0xffffffffu, lane < cols && large_scale(__ldg(a.s_x + p.col + lane)))) {      // a column at a time, as large_tile()
+#pragma unroll 1
+            for (int i = 0; i < cols; ++i) {
+                const float f[1] = {scaled((int)gemm::tmem_ld1(p.acc + i), row_scale(__ldg(a.s_x + p.col + i)), sw)};
+                if (k < p.rows) store_as<1>(a.out, a.type, (int64_t)(p.col + i) * a.ldo + k, 1, true, f);
+                __syncwarp();
+            }
+            return done();
+        }
         gemm::each_chunk<BN>(p, sh.n, done, [&](int c, uint32_t (&v)[32]) {
             if (k >= p.rows) return;
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
                 const int row = p.col + c + i;
                 if (row >= sh.n) break;
-                const float f[1] = {(float)(int)v[i] * (__ldg(a.s_x + row) * sw)};
+                const float f[1] = {(float)(int)v[i] * __ldg(a.s_x + row) * sw};
                 store_as<1>(a.out, a.type, (int64_t)row * a.ldo + k, 1, true, f);
             }
         });
@@ -325,7 +388,7 @@ __global__ void __launch_bounds__(kGemvThreads, 2) few_rows_kernel(const GemvArg
     pdl_enter();
     extern __shared__ uint4 qs[];             // [N][words] the quantised rows
     __shared__ uint32_t slot[kGemvThreads / 32];
-    __shared__ float scales[N];
+    __shared__ RowScale scales[N];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, words = (a.d + 15) / 16;
     const int warps = gridDim.x * (kGemvThreads / 32);
     int k = (blockIdx.x * (kGemvThreads / 32) + warp) * kGemvRows;
@@ -352,7 +415,7 @@ __global__ void __launch_bounds__(kGemvThreads, 2) few_rows_kernel(const GemvArg
         top = __reduce_max_sync(0xffffffffu, lane < kGemvThreads / 32 ? slot[lane] : 0u);
         const bool finite = top < 0x7f800000u;
         const float t = __uint_as_float(top), factor = 127.f / t;
-        if (threadIdx.x == 0) scales[r] = finite ? t / 127.f : __uint_as_float(0x7fc00000u);
+        if (threadIdx.x == 0) scales[r] = row_scale(finite ? t / 127.f : __uint_as_float(0x7fc00000u));
         uint32_t* q = reinterpret_cast<uint32_t*>(qs + r * words);
         for (int c = threadIdx.x * 4; c < words * 16; c += kGemvThreads * 4) {
             float v[4];
@@ -388,7 +451,7 @@ __global__ void __launch_bounds__(kGemvThreads, 2) few_rows_kernel(const GemvArg
             for (int r = 0; r < N; ++r) {
                 const int total = __reduce_add_sync(0xffffffffu, sum[j][r]);
                 if (lane == j * N + r && k + j < a.m && r < a.n) {
-                    const float f[1] = {(float)total * (scales[r] * __ldg(a.s_w + k + j))};
+                    const float f[1] = {scaled(total, scales[r], __ldg(a.s_w + k + j))};
                     store_as<1>(a.out, a.out_type, (int64_t)r * a.ldo + k + j, 1, true, f);
                 }
             }

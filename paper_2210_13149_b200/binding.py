@@ -573,7 +573,8 @@ class BiGCN:
         return g_x, g_w
 
     def quantize_rows(self, X: torch.Tensor):
-        """Rows in 8-bit integers: (q int8 [n x d rounded up to 16], scale [n]); columns of q past d are zero."""
+        """Rows in 8-bit integers: (q int8 [n x d rounded up to 16], scale [n]); columns of q past d are zero, and q.columns is d (of q itself:
+        a part or a copy of it has lost that)."""
         ldx = self._rows("X", X)
         n, d = X.shape
         ldq = (d + 15) // 16 * 16
@@ -582,12 +583,22 @@ class BiGCN:
             with torch.cuda.stream(self.stream):
                 q[:, d:] = 0
         self._check(self.lib.bigcn_quantize_rows(self.h, _addr(X), TYPES[X.dtype], n, d, ldx, _addr(q), ldq, _addr(scale)))
+        q.columns = d
         return q, scale
+
+    @staticmethod
+    def _lengths(t: torch.Tensor) -> range:
+        """How many columns the rows of an 8-bit matrix may have: one number where it says so or is cut between multiples of 16, else up to 15
+        columns of it may be what quantize_rows() adds."""
+        width = t.shape[1]
+        known = getattr(t, "columns", width if width % 16 else None)
+        return range(max(1, width - 15), width + 1) if known is None else range(known, known + 1)
 
     def quantized_product(self, X: torch.Tensor, q_w: torch.Tensor, s_w: torch.Tensor, s_x: Optional[torch.Tensor] = None,
                           out_dtype: torch.dtype = torch.float32):
         """Rows times class rows in 8-bit integers: [n x m].  X in a floating type is quantised on the way; int8 rows come with
-        their scales s_x, both as quantize_rows() returns them; so do q_w and s_w."""
+        their scales s_x, both as quantize_rows() returns them; so do q_w and s_w.  Rows have as many columns as class rows; where neither
+        says how many of its own are added ones (quantize_rows()), that is held to 16."""
         ready = X.dtype == torch.int8
         n = X.shape[0] if X.dim() == 2 else -1
         m = q_w.shape[0] if q_w.dim() == 2 else -1
@@ -596,17 +607,18 @@ class BiGCN:
             ldx = self._rows("X", X, types=(torch.int8,))
             if s_x is None:
                 raise ValueError("X: int8 rows come with their scales s_x")
-            d = min(X.shape[1], q_w.shape[1])
-            if X.shape[1] != q_w.shape[1] and (X.shape[1] + 15) // 16 != (q_w.shape[1] + 15) // 16:
-                raise ValueError("X: rows of %d for class rows of %d" % (X.shape[1], q_w.shape[1]))
+            of_x, of_w = self._lengths(X), self._lengths(q_w)
+            d = min(of_x.stop, of_w.stop) - 1
+            if d not in of_x or d not in of_w:
+                raise ValueError("X: rows of %d for class rows of %d" % (of_x.stop - 1, of_w.stop - 1))
             self._vector("s_x", s_x, n)
         else:
             ldx = self._rows("X", X)
             if s_x is not None:
                 raise ValueError("s_x goes with int8 rows only")
             d = X.shape[1]
-            if (d + 15) // 16 * 16 != (q_w.shape[1] + 15) // 16 * 16 or q_w.shape[1] < d:
-                raise ValueError("X: rows of %d for class rows of %d" % (d, q_w.shape[1]))
+            if d not in self._lengths(q_w):
+                raise ValueError("X: rows of %d for class rows of %d" % (d, self._lengths(q_w).stop - 1))
             self._scratch(_sizes("bigcn_quantized_product_workspace_bytes", n, d))
         self._vector("s_w", s_w, m)
         if out_dtype not in (torch.float32, torch.bfloat16, torch.float16):

@@ -1095,7 +1095,7 @@ bigcn_status bigcn_class_loss_backward(bigcn_ctx* ctx, const void* x, const void
     bigcn_status st = bind_device(ctx);
     if (st != BIGCN_OK) return st;
     if ((st = check_class_loss(ctx, x, w, type, n, d, classes, ldx, ldw, labels)) != BIGCN_OK) return st;
-    if ((g_x && ldgx < d) || (g_w && ldgw < d)) return fail(ctx, BIGCN_ERR_SHAPE, "ldgx=%lld ldgw=%lld for rows of %d", (long long)ldgx, (long long)ldgw, d);
+    if ((g_x && (ldgx < d || ldgx >= kMaxLd)) || (g_w && (ldgw < d || ldgw >= kMaxLd))) return fail(ctx, BIGCN_ERR_SHAPE, "ldgx=%lld ldgw=%lld for rows of %d", (long long)ldgx, (long long)ldgw, d);
     if (!aligned(g_x, 2) || !aligned(g_w, 2)) return fail(ctx, BIGCN_ERR_ALIGN, "g_x or g_w is not aligned to its elements");
     if (!g_x && !g_w) return fail(ctx, BIGCN_ERR_NULL, "neither g_x nor g_w is given: nothing to compute");
     if (n == 0) {                                             // no rows: every sum over them is empty
@@ -1145,7 +1145,7 @@ bigcn_status bigcn_quantized_product(bigcn_ctx* ctx, const void* x, int32_t x_ty
     if (st != BIGCN_OK) return st;
     if ((st = check_quantized(ctx, "q_w", q_w, m, d, ldqw, s_w)) != BIGCN_OK) return st;
     if ((st = check_type(ctx, "out", out_type)) != BIGCN_OK) return st;
-    if (ldo < m) return fail(ctx, BIGCN_ERR_SHAPE, "out: ld=%lld < m=%d", (long long)ldo, m);
+    if (ldo < m || ldo >= kMaxLd) return fail(ctx, BIGCN_ERR_SHAPE, "out: ld=%lld for rows of %d", (long long)ldo, m);
     if (n == 0) return BIGCN_OK;
     if (!out) return fail(ctx, BIGCN_ERR_NULL, "out is null");
     if (!aligned(out, out_type == BIGCN_F32 ? 4 : 2)) return fail(ctx, BIGCN_ERR_ALIGN, "out is not aligned to its elements");

@@ -49,46 +49,34 @@ __device__ __forceinline__ float2 unpack2(uint32_t w)
     else return __half22float2(*reinterpret_cast<const __half2*>(&w));
 }
 
-// V (1, 2, 4 or 8) consecutive elements, of which the first `count` exist; the rest read as 0.  `whole`: the pointer is aligned to V
-// elements (or 16 bytes), and they can be moved as whole words where all of them exist.
-template <int TYPE, int V>
-__device__ __forceinline__ void load_elts(const typename Elt<TYPE>::T* __restrict__ p, int count, bool whole, float (&v)[V])
+// Four consecutive elements, of which the first `count` exist; the rest read as 0.  `whole`: the pointer is aligned to four, and they can be moved as a whole
+// word where all of them exist.
+template <int TYPE>
+__device__ __forceinline__ void load4_of(const typename Elt<TYPE>::T* __restrict__ p, int count, bool whole, float (&v)[4])
 {
-    if (whole && count >= V) {
-        if constexpr (V == 1) {
-            v[0] = to_float<TYPE>(*p);
-        } else if constexpr (V == 2 && TYPE == BIGCN_F32) {
-            const float2 w = *reinterpret_cast<const float2*>(p);
-            v[0] = w.x; v[1] = w.y;
-        } else if constexpr (V == 2) {
-            const float2 w = unpack2<TYPE>(*reinterpret_cast<const uint32_t*>(p));
-            v[0] = w.x; v[1] = w.y;
-        } else if constexpr (TYPE == BIGCN_F32) {
-#pragma unroll
-            for (int i = 0; i < V; i += 4) {
-                const float4 w = *reinterpret_cast<const float4*>(p + i);
-                v[i] = w.x; v[i + 1] = w.y; v[i + 2] = w.z; v[i + 3] = w.w;
-            }
-        } else if constexpr (V == 4) {
+    if (whole && count >= 4) {
+        if constexpr (TYPE == BIGCN_F32) {
+            const float4 w = *reinterpret_cast<const float4*>(p);
+            v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
+        } else {
             const uint2 w = *reinterpret_cast<const uint2*>(p);
             const float2 a = unpack2<TYPE>(w.x), b = unpack2<TYPE>(w.y);
             v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
-        } else {
-            const uint4 w = *reinterpret_cast<const uint4*>(p);
-            const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 a = unpack2<TYPE>(ws[i]);
-                v[2 * i] = a.x;
-                v[2 * i + 1] = a.y;
-            }
         }
         return;
     }
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = i < count ? to_float<TYPE>(p[i]) : 0.f;
+    for (int i = 0; i < 4; ++i) v[i] = i < count ? to_float<TYPE>(p[i]) : 0.f;
+}
+// the same with the type known at run time
+__device__ __forceinline__ void load4(const void* base, int type, int64_t at, int count, bool whole, float (&v)[4])
+{
+    if (type == BIGCN_F32) load4_of<BIGCN_F32>(static_cast<const float*>(base) + at, count, whole, v);
+    else if (type == BIGCN_BF16) load4_of<BIGCN_BF16>(static_cast<const __nv_bfloat16*>(base) + at, count, whole, v);
+    else load4_of<BIGCN_F16>(static_cast<const __half*>(base) + at, count, whole, v);
 }
 
+// The first `count` of V (1, 2, 4 or 8) consecutive elements, `whole` as above for V of them (or 16 bytes).
 template <int TYPE, int V>
 __device__ __forceinline__ void store_elts(typename Elt<TYPE>::T* __restrict__ p, int count, bool whole, const float (&v)[V])
 {
@@ -112,16 +100,6 @@ __device__ __forceinline__ void store_elts(typename Elt<TYPE>::T* __restrict__ p
 #pragma unroll
     for (int i = 0; i < V; ++i)
         if (i < count) p[i] = from_float<TYPE>(v[i]);
-}
-// the same with the type known at run time (TYPE < 0) or not
-constexpr int kAnyType = -1;
-template <int TYPE, int V>
-__device__ __forceinline__ void load_as(const void* base, int type, int64_t at, int count, bool whole, float (&v)[V])
-{
-    if constexpr (TYPE >= 0) load_elts<TYPE, V>(static_cast<const typename Elt<TYPE>::T*>(base) + at, count, whole, v);
-    else if (type == BIGCN_F32) load_elts<BIGCN_F32, V>(static_cast<const float*>(base) + at, count, whole, v);
-    else if (type == BIGCN_BF16) load_elts<BIGCN_BF16, V>(static_cast<const __nv_bfloat16*>(base) + at, count, whole, v);
-    else load_elts<BIGCN_F16, V>(static_cast<const __half*>(base) + at, count, whole, v);
 }
 template <int V>
 __device__ __forceinline__ void store_as(void* base, int type, int64_t at, int count, bool whole, const float (&v)[V])
@@ -162,6 +140,8 @@ __device__ __forceinline__ void store_row(void* base, int type, int64_t row_at, 
     else if (type == BIGCN_BF16) store_row_of<BIGCN_BF16, NV, V>(base, row_at, c, stride, d, step, v);
     else store_row_of<BIGCN_F16, NV, V>(base, row_at, c, stride, d, step, v);
 }
+
+constexpr int kAnyType = -1;                  // a type known at run time
 
 // V elements as they lie in memory, words of 32 bits (a 16-bit element alone in the low half of one).  Nothing is done with them where they are loaded, so
 // that a row asked for ahead of its time is not waited for before it.

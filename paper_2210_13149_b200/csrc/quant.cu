@@ -404,7 +404,7 @@ __global__ void __launch_bounds__(kGemvThreads, 2) few_rows_kernel(const GemvArg
         uint32_t top = 0u;
         for (int c = threadIdx.x * 4; c < a.d; c += kGemvThreads * 4) {
             float v[4];
-            load_as<kAnyType, 4>(a.x, a.type, row + c, r < a.n ? a.d - c : 0, a.whole, v);
+            load4(a.x, a.type, row + c, r < a.n ? a.d - c : 0, a.whole, v);
 #pragma unroll
             for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
         }
@@ -419,7 +419,7 @@ __global__ void __launch_bounds__(kGemvThreads, 2) few_rows_kernel(const GemvArg
         uint32_t* q = reinterpret_cast<uint32_t*>(qs + r * words);
         for (int c = threadIdx.x * 4; c < words * 16; c += kGemvThreads * 4) {
             float v[4];
-            load_as<kAnyType, 4>(a.x, a.type, row + c, r < a.n ? a.d - c : 0, a.whole, v);
+            load4(a.x, a.type, row + c, r < a.n ? a.d - c : 0, a.whole, v);
             q[c / 4] = finite && top ? nearest4<false>(v, factor, t, t < 1e-30f) : 0u;
         }
     }

@@ -116,3 +116,31 @@ def test_rows_of_2_to_the_minus_29_beside_results_past_fp16(ctx):
     for got, want in ((g_x[is_light], gx[is_light]), (g_w[:, d // 2:], gw[:, d // 2:])):
         assert float((got.double() - want).norm() / want.norm()) <= 4 * HALF
     assert torch.isinf(g_x[~is_light]).any() and torch.isinf(g_w[:, :d // 2]).any()
+
+
+def test_captured_and_replayed():
+    """The memory that holds the largest weight is cleared before the kernels that find it: within a graph, too, and again at every replay."""
+    from paper_2210_13149_b200 import binding as B
+    stream = torch.cuda.Stream()
+    first, second = problem(5000, 48, 60, 1e-4, 9, 0.7), problem(5000, 48, 60, 1e-2, 10, 0.4)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        c = B.BiGCN(0)
+        x, W, labels, g, _ = [t.clone() for t in first]
+        _, lse = c.class_loss(x, W, labels)
+        c.class_loss_backward(x, W, labels, lse, g)
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            loss, lse = c.class_loss(x, W, labels)
+            out = (loss, lse) + c.class_loss_backward(x, W, labels, lse, g)
+        for given, factor in ((first, 1.0), (second, 1.0), (second, 2.0 ** -9), (first, 1.0)):
+            for t, v in zip((x, W, labels), given):
+                t.copy_(v)
+            g.copy_(given[3] * factor)
+            graph.replay()
+            stream.synchronize()
+            want = c.class_loss(x, W, labels)
+            want = want + c.class_loss_backward(x, W, labels, want[1], g)
+            assert all(torch.equal(a, b) for a, b in zip(out, want))
+        c.sync_check()

@@ -119,9 +119,10 @@ constexpr float kHalfScale = 16384.f;         // fp16's G is this much larger
 // numbers; without b they ended at 2^-14, and from 2^-25 on nothing of such a row was left.
 __device__ __forceinline__ int lift_of(float ratio)
 {
-    const float r = fabsf(ratio);
-    return r > 0.f && r < 1.f ? min(18, max(0, -5 - (ilogbf(r) + 1))) : 0;
+    const int exponent = (int)(__float_as_uint(ratio) >> 23 & 255u) - 127;       // (128 of infinities and NaN)
+    return min(18, max(0, -6 - exponent));
 }
+__device__ __forceinline__ float power_of_two(int e) { return __int_as_float((127 + e) << 23); }
 // How rows of x lie: on 16-byte boundaries, up to 32 words of 16 bytes or more; on 4-byte boundaries; anywhere.
 enum Lie : int { kShort = 0, kLong = 1, kPairs = 2, kAnywhere = 3 };
 template <int LIE>
@@ -259,11 +260,11 @@ __device__ void gather_rows(const GatherArgs& a, int count, const int* places, i
             const float g = __ldg(a.g_loss + row), ratio = top > 0.f ? g / top : 0.f;
             const int b = lift_of(ratio);
             if (lane == 0) {
-                a.lift[p] = ldexpf(kHalfScale, -b);
-                a.undo[p] = ldexpf(g, b) * (1.f / kHalfScale);
+                a.lift[p] = power_of_two(14 - b);                 // kHalfScale 2^-b
+                a.undo[p] = g * power_of_two(b - 14);
             }
             if (!a.scaled) continue;
-            const float factor = ldexpf(ratio, b);
+            const float factor = ratio * power_of_two(b);
             for (int i = lane; i < a.d; i += 32)
                 a.scaled[(int64_t)p * a.ldt + i] = __half_as_ushort(__float2half_rn(__half2float(__ushort_as_half(__ldg(a.x + row * a.ldx + i))) * factor));
         }

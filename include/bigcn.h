@@ -403,7 +403,10 @@ bigcn_status bigcn_layer_norm_backward(bigcn_ctx* ctx, const void* g_y, int32_t 
  * rows and classes at a time, in the operands' type (in fp16 without g_loss, which comes in in fp32 for g_x and by way of
  * rows of x times g_loss_i / max |g_loss| for g_w, rounded to fp16 once more; the two share the exponents that a g_loss_i
  * far below the largest needs, so that it keeps fp16's digits down to about 2^-30 of that); sums in fp32.  Rows without a label get zero.
- * The same call gives the same bits.  Needs bigcn_class_loss_workspace_bytes(n, d, classes, 1) of workspace. */
+ * What G's rounding costs: each G_ik is off by half a step of the type at most (2^-8 of it in bf16, 2^-11 in fp16), so a gradient
+ * by that share of sum_k |G_ik w_kj|, or of sum_i |G_ik x_ij|.  In the 2-norm that is about as much as the gradient's own rounding
+ * to the type (both together 0.0023 in bf16, the latter alone 0.0016); where the terms nearly cancel, as one column's against
+ * many classes may, it can be as large as what is left.  The same call gives the same bits.  Needs bigcn_class_loss_workspace_bytes(n, d, classes, 1) of workspace. */
 size_t bigcn_class_loss_workspace_bytes(int64_t n, int32_t d, int32_t classes, int32_t backward);
 bigcn_status bigcn_class_loss(bigcn_ctx* ctx, const void* x, const void* w, int32_t type, int64_t n, int32_t d, int32_t classes,
                               int64_t ldx, int64_t ldw, const int64_t* labels, float* loss, float* lse);
@@ -419,7 +422,8 @@ bigcn_status bigcn_class_loss_backward(bigcn_ctx* ctx, const void* x, const void
 bigcn_status bigcn_quantize_rows(bigcn_ctx* ctx, const void* x, int32_t type, int64_t n, int32_t d, int64_t ldx, int8_t* q,
                                  int64_t ldq, float* scale);
 
-/* Product of rows with class rows in 8-bit integers: out_ik = (sum_j q_ij qw_kj) s_i sw_k, k < m, the sum exact.  x of any
+/* Product of rows with class rows in 8-bit integers: out_ik = (sum_j q_ij qw_kj) s_i sw_k, k < m, the sum exact, rounded to fp32 and
+ * times s_i and then sw_k (in range wherever out_ik is).  x of any
  * bigcn_type: BIGCN_I8 with its scales s_x [n] (rows as bigcn_quantize_rows() lays them out), or another type with s_x
  * null, which is quantised on the way.  q_w int8 [m x ldqw], s_w fp32 [m]: the class matrix by bigcn_quantize_rows().  out
  * of any type but BIGCN_I8, [n x ldo].  Serves from one row on.  n, m < 2^31 - 512.  Needs

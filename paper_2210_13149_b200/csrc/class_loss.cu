@@ -16,6 +16,9 @@
 // Rows without a label take no part: the labelled ones are listed first and, unless that is all of them, copied together, so that what
 // the others hold (NaN, infinities) reaches nothing and their work is not done.  How many there are is known on the GPU only; the
 // kernels read it there.
+//
+// Against 64 bits (2-norm, bf16): 0.0022 to 0.0024 for the gradients of few classes, 0.0019 for many, where rounding the exact ones once leaves 0.0016.
+// lse and loss 3e-7: the tensor cores' sums, each cut at its step, and ex2.approx.
 #include <algorithm>
 #include <climits>
 
@@ -678,7 +681,8 @@ size_t up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 
 int tile_cols(int columns) { return columns <= 64 ? 64 : columns <= 128 ? 128 : 256; }
 
-// How many parts a product's depth is split into, so that its tiles fill the machine: what its rounds take, a stage of a pair's 256 x 256 tile
+// How many parts a product's depth is split into, so that its tiles fill the machine.  Its 148 multiprocessors are a constant here, so that the workspace's size is
+// one of the sizes alone, whichever device is current; with another number of them the parts are right and their choice is not the best.  What its rounds take, a stage of a pair's 256 x 256 tile
 // at 0.42 us and of a block's at 0.15 us (measured), and where it is split another 5 us for the kernel that adds the parts and their bytes, written
 // and read, at 5 TB/s.
 int pick_splits(int64_t rows, int64_t columns, int64_t stages, int most)

@@ -365,8 +365,9 @@ struct ScaledAcross {
 
 // One to four rows, not yet quantised, in one launch.  Every block quantises them for itself into shared memory (their bytes times the number of
 // blocks come from L2 and are few) while its first class rows are on their way; then a warp takes kGemvRows class rows at a time, 16 bytes of each a
-// lane, and sums by four-byte dot products.  Bound by the class rows, which are read once: 65,536 classes x 1,024 for one row in us: 19.8 by two
-// kernels with tensor memory to set up, 10.8 so.  More rows cost more dot products: few_rows_pays().
+// lane, and sums by four-byte dot products.  Bound by the class rows, which are read once: 65,536 classes x 1,024 for one row in us, with the
+// 67 MB in L2 from the call before: 19.8 by two kernels with tensor memory to set up, 10.3 so; from memory 15.2 (68 % of a plain copy's rate).  More rows cost
+// more dot products: few_rows_pays().
 constexpr int kGemvThreads = 512, kGemvRows = 4, kGemvMax = 4, kGemvBytes = 64 * 1024;
 struct GemvArgs {
     const void* x;
@@ -499,7 +500,7 @@ int quant_timeouts()
     return v;
 }
 
-// Whether that is expected to be the faster one, of what each takes in us: from Python 11 for one launch and 14.3 for two; the class rows' bytes; and
+// Whether that is expected to be the faster one, on a machine of 148 multiprocessors (either is right on any), of what each takes in us: from Python 11 for one launch and 14.3 for two; the class rows' bytes; and
 // here the steps of a class row in one of 2,368 warps (16 bytes a lane are a load and four dot products a row, and every row's sum a reduction
 // and a store), there the tiles' own time.  Measured for 1, 2, 3, 4 rows against two kernels: 65,536 classes x 1,024 15.2, 18.6, 23.7, 24.8
 // against 18.3; 32,768 x 4,096 24, 28, 34, 35 against 28; 200,000 x 256 22, 29, 41, 45 against 20; 30,011 x 602 11.3, 11.3, 14.2, 14.7 against 14.3;

@@ -4,7 +4,8 @@
 //   g_x_ij = rstd_i (g_ij gain_j - a_i - xhat_ij b_i),  a_i = sum_j g_ij gain_j / d,  b_i = sum_j g_ij gain_j xhat_ij / d
 //   g_gain_j = sum_i g_ij xhat_ij,  g_offset_j = sum_i g_ij                        (g = the gradient of y)
 //
-// Both directions are bound by the bytes of the rows.  A row is held in the registers of the lanes that read it (4 to 32 lanes of a
+// Both directions are bound by the bytes of the rows where these are long (fp32 rows of 256: 85 to 97 % of a plain copy's rate), by latency and instructions where a
+// lane has little of a row (bf16 rows of 24: 44 and 51 %, of 23: 20 and 18 %) or holds much of it in registers (500 columns back: 65 %).  A row is held in the registers of the lanes that read it (4 to 32 lanes of a
 // warp, or a whole block for long rows), so that it is read once: the mean first, then the squares about it, which lose nothing to
 // cancellation.  The columns' sums of the backward pass ride along in registers, one pair per column a thread owns, over the rows that
 // its lanes take; blocks leave theirs in the workspace, and a second kernel adds them in 64 bits in a fixed order.

@@ -400,13 +400,14 @@ bigcn_status bigcn_layer_norm_backward(bigcn_ctx* ctx, const void* g_y, int32_t 
  * bigcn_class_loss_backward(): the gradients for g_loss = dL/dloss (fp32 [n]) and the lse of the forward pass,
  *   G_ik = (exp(z_ik - lse_i) - [k = label(i)]) g_loss_i,  g_x = G w,  g_w = G^T x,
  * g_x [n x ldgx] and g_w [classes x ldgw] in the operands' type, nullable each.  z is computed again and G held a piece of
- * rows and classes at a time, in the operands' type (in fp16 without g_loss, which comes in in fp32 for g_x and by way of
- * rows of x times g_loss_i / max |g_loss| for g_w, rounded to fp16 once more; the two share the exponents that a g_loss_i
- * far below the largest needs, so that it keeps fp16's digits down to about 2^-30 of that); sums in fp32.  Rows without a label get zero.
- * What G's rounding costs: each G_ik is off by half a step of the type at most (2^-8 of it in bf16, 2^-11 in fp16), so a gradient
- * by that share of sum_k |G_ik w_kj|, or of sum_i |G_ik x_ij|.  In the 2-norm that is about as much as the gradient's own rounding
- * to the type (both together 0.0023 in bf16, the latter alone 0.0016); where the terms nearly cancel, as one column's against
- * many classes may, it can be as large as what is left.  The same call gives the same bits.  Needs bigcn_class_loss_workspace_bytes(n, d, classes, 1) of workspace. */
+ * rows and classes at a time, up to 64 classes as the sum of two numbers of the operands' type, from 65 on rounded to it (in fp16
+ * without g_loss, which comes in in fp32 for g_x and by way of rows of x times g_loss_i / max |g_loss| for g_w, rounded to fp16
+ * once more; the two share the exponents that a g_loss_i far below the largest needs, so that it keeps fp16's digits down to
+ * about 2^-30 of that); sums in fp32.  Rows without a label get zero.  What G's rounding costs from 65 classes on: each G_ik is
+ * off by half a step of the type at most (2^-8 of it in bf16, 2^-11 in fp16), so a gradient by that share of sum_k |G_ik w_kj|,
+ * or of sum_i |G_ik x_ij|: in the 2-norm about as much as the gradient's own rounding (both together 0.0019 to 0.0023 in bf16, the
+ * latter alone 0.0016); where the terms nearly cancel, as one column's against many classes may, it can be as large as what is
+ * left.  The same call gives the same bits.  Needs bigcn_class_loss_workspace_bytes(n, d, classes, 1) of workspace. */
 size_t bigcn_class_loss_workspace_bytes(int64_t n, int32_t d, int32_t classes, int32_t backward);
 bigcn_status bigcn_class_loss(bigcn_ctx* ctx, const void* x, const void* w, int32_t type, int64_t n, int32_t d, int32_t classes,
                               int64_t ldx, int64_t ldw, const int64_t* labels, float* loss, float* lse);

@@ -8,7 +8,9 @@
 // (kPieceBytes of G), turns it into G in its epilogue, and multiplies that piece into g_x and g_w; sums over pieces, and over
 // parts of a long depth, are kept in fp32 in the workspace and added in a fixed order.  G is rounded to the operands' type, the one
 // rounding besides the outputs' own: a relative error of half a step for each term of sums whose terms' errors are independent,
-// which is the size of the output's rounding.  In bf16 g_i is part of G.  fp16 has no exponents for a g_i of, say, 1 / n times a small
+// which is the size of the output's rounding.  Up to 64 classes there is no such error: G is the sum of two numbers of the type, a high half and behind it a
+// low one.  Tiles of G's columns are 128 wide in g_w whether or not they hold the low half, and the depth of g_x is one stage, or two from 33 classes on,
+// whose class rows are fetched twice: what it costs are G's bytes, twice as many from 33 classes on (see low_half()).  In bf16 g_i is part of G.  fp16 has no exponents for a g_i of, say, 1 / n times a small
 // probability, so there G holds (exp(z - lse) - [..]) 2^14 (down to 2^-28 in normal numbers), rows of g_x are multiplied by g_i 2^-14 in fp32, and X enters
 // g_w as rows times g_i / max |g| (one more rounding, none where all g_i are the same), the rest in fp32.  Nor has fp16 the exponents for a g_i far below
 // the largest: such a row of X goes up by a power of two 2^b and its row of G down by it, see lift_of().
@@ -17,7 +19,7 @@
 // the others hold (NaN, infinities) reaches nothing and their work is not done.  How many there are is known on the GPU only; the
 // kernels read it there.
 //
-// Against 64 bits (2-norm, bf16): 0.0022 to 0.0024 for the gradients of few classes, 0.0019 for many, where rounding the exact ones once leaves 0.0016.
+// Against 64 bits (2-norm, bf16): 0.0019 for the gradients of many classes, where rounding the exact ones once leaves 0.0016 (as for up to 64).
 // lse and loss 3e-7: the tensor cores' sums, each cut at its step, and ex2.approx.
 #include <algorithm>
 #include <climits>
@@ -426,8 +428,9 @@ struct Gradient {
         const float* lse;    // of the labelled rows
         const float* weight; // of the labelled rows: bf16 g_loss, fp16 kHalfScale 2^-b
         int first_class;     // of the piece
+        int columns;         // with those past the last class: a multiple of 64, or 32
         uint16_t* g;
-        int64_t ldg;         // a multiple of 64
+        int64_t ldg;         // columns, or twice that: then the second half of a row holds what rounding the first one left
     };
     static constexpr bool kMeets = false;
     static __device__ int* flag() { return &g_loss_timeout; }
@@ -447,7 +450,7 @@ struct Gradient {
         const bool there = p.row + (int)(threadIdx.x & 31) < p.rows;
         const int label = of_row.label >= a.first_class + p.col ? of_row.label - a.first_class - p.col : INT_MIN;
         const float lse = of_row.lse, weight = of_row.weight;
-        gemm::each_chunk<BN>(p, (int)a.ldg, done, [&](int c, uint32_t (&v)[32]) {
+        gemm::each_chunk<BN>(p, a.columns, done, [&](int c, uint32_t (&v)[32]) {
             const int left = sh.n - (p.col + c);
             float f[32];
 #pragma unroll
@@ -461,15 +464,33 @@ struct Gradient {
             uint32_t w[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) w[i] = pack2<TYPE>(f[2 * i] * weight, f[2 * i + 1] * weight);
-            if (!there || left < 32) {
+            const auto put = [&](uint16_t* to) {
+                if (!there || left < 32) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    if (!there || 2 * i >= left) w[i] = 0u;
-                    else if (2 * i + 1 >= left) w[i] &= 0xffffu;
+                    for (int i = 0; i < 16; ++i) {
+                        if (!there || 2 * i >= left) w[i] = 0u;
+                        else if (2 * i + 1 >= left) w[i] &= 0xffffu;
+                    }
+                }
+                gemm::write_strip_whole(p.strip, w, reinterpret_cast<char*>(to), 16 * a.ldg);
+            };
+            const int lane = threadIdx.x & 31;
+            uint16_t* const to = a.g + (int64_t)(p.row + (lane >> 2)) * a.ldg + p.col + c + 8 * (lane & 3);
+            if constexpr (BN == 64) {
+                if (a.ldg > a.columns) {
+                    uint32_t low[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float2 high = unpack2<TYPE>(w[i]);
+                        low[i] = pack2<TYPE>(fmaf(f[2 * i], weight, -high.x), fmaf(f[2 * i + 1], weight, -high.y));
+                    }
+                    put(to);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) w[i] = low[i];
+                    return put(to + a.columns);
                 }
             }
-            const int lane = threadIdx.x & 31;
-            gemm::write_strip_whole(p.strip, w, reinterpret_cast<char*>(a.g + (int64_t)(p.row + (lane >> 2)) * a.ldg + p.col + c + 8 * (lane & 3)), 16 * a.ldg);
+            put(to);
         });
     }
 };
@@ -675,7 +696,7 @@ cudaError_t launch_finish(cudaStream_t s, const FinishArgs& a, int* launches)
 
 // ---- plan ------------------------------------------------------------------------------------------------------------------
 
-constexpr int64_t kPieceBytes = int64_t(512) << 20;      // of G, and of the forward pass's parts
+constexpr int64_t kPieceBytes = int64_t(512) << 20;      // of G (of its high half), and of the forward pass's parts
 constexpr size_t kAlign = 256;
 size_t up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 
@@ -700,6 +721,12 @@ int pick_splits(int64_t rows, int64_t columns, int64_t stages, int most)
     return best;
 }
 
+// How far behind its high half G's low one lies (0: there is none).  In us for the gradients without it and with it, bf16: 2,708 x 64 against 7 classes 27 and 27,
+// 219,149 x 232 against 4 144 and 154 (167 with the low half 64 columns on), 2,449,029 x 256 against 47, 8 % labelled, 374 and 387.  From 65 classes on
+// it would be more tiles and more depth, for a rounding that counts less among more terms: in the 2-norm (with the result's 0.0016) 0.0019 against
+// 65,536 classes, 0.0022 to 0.0024 against 7 and 47.
+int low_half(int classes) { return classes <= 32 ? 32 : classes <= 64 ? 64 : 0; }
+
 struct Plan {
     int64_t n_pad, ldt;                       // copied rows
     int64_t rows;                             // of a piece (a multiple of 128)
@@ -707,6 +734,7 @@ struct Plan {
     int row_pieces, col_pieces;
     int bn, parts;                            // forward: column tile and parts of a row
     int splits_x, splits_w;
+    int low;                                  // low_half()
     int bn_d;                                 // column tile of the gradients' products
     int64_t pitch;                            // of fp32 parts
     size_t bytes;
@@ -758,9 +786,10 @@ Plan make_plan(int64_t n, int d, int classes, bool backward, bool half)
         p.pitch = round_up(d, 8);
         p.splits_x = pick_splits(std::min<int64_t>(p.rows, std::max<int64_t>(n, 1)), d, p.cols / 64, 148);
         p.splits_w = pick_splits(std::min<int64_t>(p.cols, classes), d, p.rows / 64, 148);
-        p.g = take((size_t)p.rows * p.cols * 2);
+        p.low = low_half(classes);
+        p.g = take((size_t)p.rows * std::max<int64_t>(p.cols, 2 * p.low) * 2);
         if (p.splits_x > 1 || p.col_pieces > 1) p.px = take((size_t)p.splits_x * p.n_pad * p.pitch * 4);
-        if (p.splits_w > 1 || p.row_pieces > 1) p.pw = take((size_t)p.splits_w * round_up(p.cols, 128) * p.pitch * 4);
+        if (p.splits_w > 1 || p.row_pieces > 1 || p.low) p.pw = take((size_t)p.splits_w * round_up(p.cols, 128) * p.pitch * 4);
     }
     p.bytes = off;
     return p;
@@ -902,15 +931,16 @@ cudaError_t backward_as(cudaStream_t s, const void* x, int64_t ldx, const void* 
     const int* kept = reinterpret_cast<const int*>(ws + p.kept);
     const int* label = reinterpret_cast<const int*>(ws + p.label);
     uint16_t* g = reinterpret_cast<uint16_t*>(ws + p.g);
-    const bool parts_x = p.splits_x > 1 || p.col_pieces > 1, parts_w = p.splits_w > 1 || p.row_pieces > 1;
+    const bool parts_x = p.splits_x > 1 || p.col_pieces > 1, parts_w = p.splits_w > 1 || p.row_pieces > 1 || p.low;
     for (int c = 0; c < p.col_pieces && e == cudaSuccess; ++c) {
         const int64_t first_class = c * p.cols;
         const int here = (int)std::min<int64_t>(p.cols, classes - first_class);
-        const int64_t ldg = round_up(here, 64);
+        const int columns = p.low ? p.low : (int)round_up(here, 64);
+        const int64_t ldg = p.low ? 2 * p.low : columns;
         for (int r = 0; r < p.row_pieces && e == cudaSuccess; ++r) {
             const int64_t first = r * p.rows, rows = std::min(p.rows, n - first);
             if (rows <= 0) break;
-            const typename Gradient<TYPE>::Args ga = {label + first, reinterpret_cast<const float*>(ws + p.lse) + first, reinterpret_cast<const float*>(ws + (half ? p.lift : p.g_loss)) + first, (int)first_class, g, ldg};
+            const typename Gradient<TYPE>::Args ga = {label + first, reinterpret_cast<const float*>(ws + p.lse) + first, reinterpret_cast<const float*>(ws + (half ? p.lift : p.g_loss)) + first, (int)first_class, columns, g, ldg};
             e = pick_logits<Gradient<TYPE>>(s, tile_cols(here), p, o, n, d, here, first, rows, first_class, count, type, ga, launches);
             if (e != cudaSuccess) break;
             gemm::Shape sh;
@@ -925,10 +955,11 @@ cudaError_t backward_as(cudaStream_t s, const void* x, int64_t ldx, const void* 
                 sh.tile_rows = gemm::rows_of_one_tile(rows);
                 sh.rotate = rows <= gemm::kRows;
                 e = gemm::encode_map(&mg, g, 2, false, round_up(rows, 128), ldg, ldg * 2, 64, sh.tile_rows);
-                if (e == cudaSuccess) e = gemm::encode_map(&mw, static_cast<const uint16_t*>(o.w) + first_class * o.ldw, 2, false, here, d, o.ldw * 2, 64, 64);
+                if (e == cudaSuccess) e = gemm::encode_map(&mw, static_cast<const uint16_t*>(o.w) + first_class * o.ldw, 2, false, here, d, o.ldw * 2, 64, p.low == 32 ? 32 : 64);
                 if (e != cudaSuccess) break;
                 sh.m = (int)rows;
-                sh.k = here;
+                sh.k = p.low ? (int)ldg : here;                // (zeros of G meet the classes that are not there)
+                sh.b_depth = p.low;
                 sh.splits = p.splits_x;
                 const typename Store<TYPE>::Args args = {kept + first, static_cast<uint16_t*>(g_x), ldgx, rows_whole(g_x, ldgx, BIGCN_BF16, 8),
                                           parts_x ? reinterpret_cast<float*>(ws + p.px) + first * p.pitch : nullptr, p.pitch, p.n_pad * p.pitch, c > 0,
@@ -951,19 +982,20 @@ cudaError_t backward_as(cudaStream_t s, const void* x, int64_t ldx, const void* 
                     e = row_maps(&mx, &own, p, o, n, d, first, 64, 64);
                 }
                 if (e != cudaSuccess) break;
-                sh.m = here;
+                sh.m = p.low ? (int)ldg : here;                // the halves' sums as rows of their own, added with the other parts
                 sh.k = (int)rows;
+                sh.b_depth = 0;
                 sh.splits = p.splits_w;
                 sh.over_depth = true;
                 sh.rotate = false;
                 sh.alt_b = o.x_whole && !half;
                 uint16_t* out = static_cast<uint16_t*>(g_w) + first_class * ldgw;
                 const typename Store<TYPE>::Args args = {nullptr, out, ldgw, rows_whole(out, ldgw, BIGCN_BF16, 8), parts_w ? reinterpret_cast<float*>(ws + p.pw) : nullptr, p.pitch,
-                                          round_up(p.cols, 128) * p.pitch, r > 0, nullptr, half ? reinterpret_cast<const float*>(ws + p.top) : nullptr, half ? 1.f / kHalfScale : 1.f};
+                                          (p.low ? ldg : round_up(p.cols, 128)) * p.pitch, r > 0, nullptr, half ? reinterpret_cast<const float*>(ws + p.top) : nullptr, half ? 1.f / kHalfScale : 1.f};
                 ++*launches;
                 e = launch_gradient<TYPE, true>(s, p.bn_d, mg, mx, own, sh, args);
                 if (e == cudaSuccess && parts_w && r == p.row_pieces - 1) {
-                    const FinishArgs fa = {args.part, p.splits_w, args.split_stride, p.pitch, nullptr, 0, here, d, nullptr, out, ldgw, args.whole, args.row_factor, args.factor, args.constant};
+                    const FinishArgs fa = {args.part, p.low ? 2 * p.splits_w : p.splits_w, p.low ? p.low * p.pitch : args.split_stride, p.pitch, nullptr, 0, here, d, nullptr, out, ldgw, args.whole, args.row_factor, args.factor, args.constant};
                     e = launch_finish<TYPE>(s, fa, launches);
                 }
             }

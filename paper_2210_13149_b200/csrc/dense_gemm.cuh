@@ -50,6 +50,8 @@ struct Shape {
     bool rotate = false;     // each block (or pair) begins with another step of the depth.  For operands that are read once: blocks that all begin at the first
                              // 128 bytes of rows a power of two apart keep to a part of the memory channels (131,072 8-bit classes x 2,048 for
                              // eight rows in us: 73, 47 so).  Sums of floats are then taken in an order that depends on the tile.
+    int b_depth = 0;         // MN-major B: where its depth begins over again (0: it does not), so that A may come in two halves: a stage's 64, or 32, the half of the
+                             // only stage, in boxes of 32 rows
     bool a_ahead = false;    // A does not come from the kernel before this one (which let this one start early): its first stages are
                              // fetched while that one runs.  No count, one block to a tile.
 };
@@ -469,8 +471,12 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                         copy_box<CTAS>(sa, ma, at, arow, &ctl.full[slot]);
                     }
                     if constexpr (B_MN) {
+                        const int at_b = shape.b_depth > 0 && at >= shape.b_depth ? at - shape.b_depth : at;
 #pragma unroll
-                        for (int i = 0; i < C::kBRows / 64; ++i) copy_box<CTAS>(sb + i * 8192, mb, brow + 64 * i, at, &ctl.full[slot]);
+                        for (int i = 0; i < C::kBRows / 64; ++i) copy_box<CTAS>(sb + i * 8192, mb, brow + 64 * i, at_b, &ctl.full[slot]);
+                        if (shape.b_depth == 32)
+#pragma unroll
+                            for (int i = 0; i < C::kBRows / 64; ++i) copy_box<CTAS>(sb + i * 8192 + 4096, mb, brow + 64 * i, at_b, &ctl.full[slot]);
                     } else {
                         copy_box<CTAS>(sb, mb, at, brow, &ctl.full[slot]);
                     }
